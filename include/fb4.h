@@ -87,7 +87,9 @@ int fb4_version(void);
 /* Static, never-NULL description of a return code. */
 const char* fb4_strerror(int code);
 
-/* Bytes of caller-provided device workspace any call needs: always 0. */
+/* Bytes of caller-provided device workspace any call needs that has no workspace
+ * argument: always 0.  (fb4_select_key_blocks and fb4_block_attention have one,
+ * and a call of their own that says how much.) */
 size_t fb4_workspace_bytes(void);
 
 /*
@@ -472,6 +474,113 @@ int fb4_seda_main_anchor(const float* temporal_scores, const void* qt, const voi
  */
 int fb4_seda_main_anchor_3d(const float* scores, int64_t frames, int heads, int grid_h, int grid_w, int tile_h,
                             int tile_w, int32_t* anchors, void* stream);
+
+/*
+ * Norms of queries and keys per head and the rotation by their positions, in
+ * one pass, between the projection and the attention: what fb4_attention_scores,
+ * fb4_seda_assign, fb4_select_key_blocks and fb4_block_attention take as q and k.
+ * Per row x of dim channels (one head of one token):
+ *   y[c] = x[c] / sqrt(mean(x^2) + eps) * gamma[c]   (norm = 1), y = x (norm = 0)
+ *   pair p of axis a turns by t = positions[token][a] * freqs[p]:
+ *   (u, w) -> (u cos t - w sin t, u sin t + w cos t)
+ * Pairs are numbered through the axes: axis a has axis_pairs[a] of them.  A pair
+ * is the channels (2p, 2p + 1) (FB4_ROPE_ADJACENT) or (p, P + p), P = all pairs
+ * (FB4_ROPE_HALVES); channels from 2P on are not turned.  Norm and rotation run
+ * in fp32 (angles in double, then the hardware's sine and cosine), one rounding
+ * to bf16 at the end.  A row whose mean square leaves [2^-100, 2^100] is
+ * normalized in double (a NaN makes its row NaN, an Inf is NaN and the rest of
+ * its row 0, a zero row with eps = 0 is NaN).
+ *   q, k        device, bf16 [batch][heads][tokens][dim] by strides: the
+ *               channels contiguous, rows 16-byte aligned.  heads_k = 0: no keys
+ *   *_strides   host, (batch, head, token) strides in elements, each a multiple
+ *               of 8, at least 0 and below 2^35 (FB4_ERR_UNSUPPORTED otherwise):
+ *               a packed projection [batch][tokens][q | k | v] is read in place, and one
+ *               call with batch and tokens exchanged serves temporal attention
+ *   dim         a multiple of 8, at most 256; batch * tokens at most 2^25
+ *               (FB4_ERR_UNSUPPORTED otherwise)
+ *   gamma_*     device, float [dim]; NULL = all ones
+ *   eps         >= 0 with norm = 1 (FB4_ERR_INVALID_ARG otherwise)
+ *   positions   device, int32 [batch][tokens][n_axes], any value; with
+ *               positions_shared = 1 [tokens][n_axes] for every sequence
+ *   freqs       device, double [P]: radians per position
+ *   axis_pairs  host, [n_axes], n_axes 0..4 (0: no rotation), each >= 1, 2P <=
+ *               dim (FB4_ERR_INVALID_ARG otherwise); P a multiple of 4 for FB4_ROPE_HALVES
+ *               (FB4_ERR_UNSUPPORTED otherwise)
+ *   q_out, k_out  device, bf16 [batch][heads][tokens][dim], contiguous, 16-byte
+ *               aligned; not the memory of q or k
+ */
+#define FB4_ROPE_ADJACENT 0
+#define FB4_ROPE_HALVES 1
+int fb4_qk_norm_rope(const void* q, const int64_t* q_strides, const void* k, const int64_t* k_strides, int64_t batch,
+                     int64_t tokens, int heads_q, int heads_k, int64_t dim, int norm, const float* gamma_q,
+                     const float* gamma_k, float eps, const int32_t* positions, int positions_shared,
+                     const double* freqs, const int32_t* axis_pairs, int n_axes, int pairing, void* q_out, void* k_out,
+                     void* stream);
+
+/*
+ * Which blocks of keys a block of queries attends: the mean of every block of
+ * block_q queries and of block_k keys, their products s[i][j] = mean_q[i] .
+ * mean_k[j], and of every row i the `top` largest, ties to the lower block, a NaN
+ * below every number.  Means, products and order are in double, so that the choice does
+ * not hang on the order of a sum.
+ *   q       device, bf16 [batch][heads][tokens_q][dim], contiguous, 16-byte aligned
+ *   k       device, bf16 [batch][heads_k][tokens_k][dim], likewise; head h reads
+ *           key head h / (heads / heads_k) (FB4_ERR_INVALID_ARG if heads_k does not
+ *           divide heads)
+ *   dim     a multiple of 8, at most 128 (FB4_ERR_UNSUPPORTED otherwise)
+ *   lens    device, int32 [batch][2]: queries and keys of each sequence of a
+ *           padded batch, clamped to 0 .. tokens; NULL = all.  What lies behind is not read
+ *   block_q, block_k  64 or 128 (FB4_ERR_UNSUPPORTED otherwise); at most 2048
+ *           blocks of keys (FB4_ERR_UNSUPPORTED beyond)
+ *   blocks  device, int32 [batch][heads][ceil(tokens_q / block_q)][top]: the chosen
+ *           blocks, ascending, then -1 (fewer than top blocks with a key; a block without a
+ *           query has none) -- the `blocks` argument of fb4_block_attention
+ *   scores  device, float, like blocks, or NULL: the listed blocks' scores,
+ *           NaN beside -1
+ *   workspace  device, 16-byte aligned, at least
+ *           fb4_select_key_blocks_workspace() bytes (FB4_ERR_INVALID_ARG
+ *           otherwise); free again when the call's work on the stream is done
+ */
+size_t fb4_select_key_blocks_workspace(int64_t batch, int heads, int heads_k, int64_t tokens_q, int64_t tokens_k,
+                                       int64_t dim, int block_q, int block_k);
+int fb4_select_key_blocks(const void* q, const void* k, int64_t batch, int heads, int heads_k, int64_t tokens_q,
+                          int64_t tokens_k, int64_t dim, const int32_t* lens, int block_q, int block_k, int64_t top,
+                          int32_t* blocks, float* scores, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Attention of every query over the keys of its block's listed blocks:
+ *   out[i] = sum_j P[i][j] V[j], P[i] = softmax of scale * Q[i] . K[j]
+ * Products on the matrix cores with fp32 accumulation, the softmax in one pass in fp32,
+ * its weights rounded to bf16 for the second product, the output rounded once.
+ *   q, k, heads, heads_k, dim, lens, block_q, block_k  as in fb4_select_key_blocks
+ *   v       device, bf16 [batch][heads_k][tokens_k][dim] by v_strides: rows
+ *           16-byte aligned, the channels contiguous
+ *   blocks  device, int32 [batch][heads][ceil(tokens_q / block_q)][top]; in any
+ *           order; an entry without a key (negative, or behind the sequence's last
+ *           block) is skipped, one listed twice counts twice
+ *   top     entries of a list, at least 0; FB4_ALL_BLOCKS: all keys, blocks NULL (FB4_ERR_INVALID_ARG
+ *           if it is not, or if it is NULL with entries)
+ *   scale   > 0 and finite (FB4_ERR_INVALID_ARG otherwise)
+ *   out     device, bf16 [batch][heads][tokens_q][dim] by out_strides, rows
+ *           16-byte aligned, none overlapping another or an input: with
+ *           [batch][tokens][heads][dim] the rows that fb4_quantize takes
+ *   lse     device, float [batch][heads][tokens_q] or NULL: log sum_j exp(scale *
+ *           Q[i] . K[j])
+ *   *_strides  host, (batch, head, token), as in fb4_qk_norm_rope
+ *   workspace  as in fb4_select_key_blocks, by fb4_block_attention_workspace; may be
+ *           NULL where that is 0
+ * A query without a key, or all of whose scores are -Inf, gives zeros and lse =
+ * -Inf; rows behind a sequence's last query keep what they held, in out and
+ * in lse.  A row's sums are formed in an order that depends on the sizes in the call
+ * (the same call always gives the same results).
+ */
+#define FB4_ALL_BLOCKS (-1)
+size_t fb4_block_attention_workspace(int64_t batch, int heads, int heads_k, int64_t tokens_q, int64_t tokens_k,
+                                     int64_t dim, int64_t top, int block_q, int block_k);
+int fb4_block_attention(const void* q, const void* k, const void* v, const int64_t* v_strides, int64_t batch, int heads,
+                        int heads_k, int64_t tokens_q, int64_t tokens_k, int64_t dim, const int32_t* lens,
+                        const int32_t* blocks, int64_t top, int block_q, int block_k, float scale, void* out,
+                        const int64_t* out_strides, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Diagnostic, not part of the paper's method: launches a kernel that does

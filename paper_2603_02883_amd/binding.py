@@ -27,6 +27,9 @@ ERR_HIP = -4
 SEL_SSE = 0
 SEL_LUT = 1
 FLAG_TWO_STAGE = 1
+ROPE_ADJACENT = 0
+ROPE_HALVES = 1
+ALL_BLOCKS = -1
 DTYPE_BF16 = 0
 DTYPE_F32 = 1
 
@@ -76,6 +79,15 @@ def _load():
                                     p, p]
     lib.fb4_seda_main_anchor.argtypes = [p, p, p, i64, i32, i32, i32, i64, p, i32, i32, i32, ctypes.c_float, p, p, p, p]
     lib.fb4_seda_main_anchor_3d.argtypes = [p, i64, i32, i32, i32, i32, i32, p, p]
+    st, size = ctypes.POINTER(i64), ctypes.c_size_t
+    lib.fb4_qk_norm_rope.argtypes = [p, st, p, st, i64, i64, i32, i32, i64, i32, p, p, ctypes.c_float, p, i32, p, ctypes.POINTER(ctypes.c_int32),
+                                     i32, i32, p, p, p]
+    lib.fb4_select_key_blocks.argtypes = [p, p, i64, i32, i32, i64, i64, i64, p, i32, i32, i64, p, p, p, size, p]
+    lib.fb4_select_key_blocks_workspace.argtypes = [i64, i32, i32, i64, i64, i64, i32, i32]
+    lib.fb4_select_key_blocks_workspace.restype = size
+    lib.fb4_block_attention.argtypes = [p, p, p, st, i64, i32, i32, i64, i64, i64, p, p, i64, i32, i32, ctypes.c_float, p, st, p, p, size, p]
+    lib.fb4_block_attention_workspace.argtypes = [i64, i32, i32, i64, i64, i64, i64, i32, i32]
+    lib.fb4_block_attention_workspace.restype = size
     lib.fb4_probe_mfma_rate.argtypes = [i64, i64, i32, p, ctypes.POINTER(ctypes.c_double), p]
     lib.fb4_gelu_table_host.argtypes = [i32, p, ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t)]
     lib.fb4_gelu_quantize.argtypes = [p, ctypes.POINTER(fb4_opts), p, i64, i64, i64, i32, p, p, i32, p, p, p]
@@ -91,7 +103,9 @@ EXPORTS = ["fb4_version", "fb4_strerror", "fb4_workspace_bytes", "fb4_build_luts
            "fb4_quantize_decompose", "fb4_seda_profile",
            "fb4_repack_mxfp8", "fb4_layernorm_quantize", "fb4_gelu_quantize",
            "fb4_gelu_table_host", "fb4_attention_scores", "fb4_select_salient_tokens",
-           "fb4_seda_assign", "fb4_seda_main_anchor", "fb4_seda_main_anchor_3d", "fb4_probe_mfma_rate"]
+           "fb4_seda_assign", "fb4_seda_main_anchor", "fb4_seda_main_anchor_3d", "fb4_qk_norm_rope",
+           "fb4_select_key_blocks", "fb4_select_key_blocks_workspace", "fb4_block_attention", "fb4_block_attention_workspace",
+           "fb4_probe_mfma_rate"]
 
 
 def lib():
@@ -386,6 +400,132 @@ def fb4_seda_main_anchor_3d(scores, frames, grid_h, grid_w, tile_h=4, tile_w=4, 
     _check(_lib.fb4_seda_main_anchor_3d(_dp(scores), frames, heads, grid_h, grid_w, tile_h, tile_w, _dp(anchors),
                                         _stream(stream)), "fb4_seda_main_anchor_3d")
     return anchors
+
+
+def _require(ok, where, code=ERR_INVALID_ARG):
+    if not ok:
+        raise Fb4Error(code, where)
+
+
+def _on_device(where, *tensors):
+    """The kernels run on the current device, on its memory: anything else would be a foreign pointer there."""
+    device = None
+    for t, dtype in tensors:
+        if t is not None:
+            if device is None:
+                device = torch.device("cuda", _get_device()) if t.is_cuda else None
+            _require(t.is_cuda and t.device == device and t.dtype is dtype, where)
+
+
+def _strides(t):
+    """(batch, head, token) strides of a [batch][heads][tokens][dim] tensor (a single one's own stride says nothing)."""
+    return (ctypes.c_int64 * 3)(*[t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)])
+
+
+def _workspace(given, size, device, stream):
+    """`size` bytes for the length of a call: memory of the stream that the call runs on, which later work there may reuse."""
+    if given is not None or size == 0:
+        return given
+    if stream is None:
+        return torch.empty(size, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(size, dtype=torch.uint8, device=device)
+
+
+def fb4_qk_norm_rope(q, k, positions, freqs, axis_pairs, gamma_q=None, gamma_k=None, eps=1e-6, norm=True, pairing=ROPE_ADJACENT, q_out=None,
+                     k_out=None, stream=None):
+    """q, k: bf16 cuda [batch][heads][tokens][dim], any strides with contiguous channels (views of a packed projection);
+    k may be None.  positions: int32 cuda [batch or 1][tokens][axes]; freqs: float64 cuda [sum(axis_pairs)], radians per position;
+    axis_pairs: pairs of channels per axis (empty: no rotation, positions and freqs None); gamma_q, gamma_k: float32 cuda [dim] or
+    None; norm=False: rotation alone.  Returns contiguous (q_out, k_out) of the inputs' shapes."""
+    where = "fb4_qk_norm_rope"
+    batch, heads, tokens, dim = q.shape
+    _on_device(where, (q, torch.bfloat16), (k, torch.bfloat16), (positions, torch.int32), (freqs, torch.float64), (gamma_q, torch.float32),
+               (gamma_k, torch.float32), (q_out, torch.bfloat16), (k_out, torch.bfloat16))
+    heads_k = 0 if k is None else k.shape[1]
+    _require(k is None or (k.dim() == 4 and k.shape == (batch, heads_k, tokens, dim)), where)
+    n = len(axis_pairs)
+    if n:
+        _require(positions is not None and freqs is not None and positions.dim() == 3 and positions.shape[0] in (1, batch) and
+                 positions.shape[1:] == (tokens, n) and freqs.shape == (sum(axis_pairs),), where)
+    for t, h in ((q_out, heads), (k_out, heads_k)):
+        _require(t is None or t.shape == (batch, h, tokens, dim), where)
+    for t in (gamma_q, gamma_k):
+        _require(t is None or t.shape == (dim,), where)
+    for t in (positions, freqs, gamma_q, gamma_k, q_out, k_out):
+        _require(t is None or t.is_contiguous(), where, ERR_UNSUPPORTED)
+    for t in (q, k):
+        _require(t is None or dim == 1 or t.numel() == 0 or t.stride(3) == 1, where, ERR_UNSUPPORTED)
+    q_out = torch.empty((batch, heads, tokens, dim), dtype=q.dtype, device=q.device) if q_out is None else q_out
+    if k is not None and k_out is None:
+        k_out = torch.empty((batch, heads_k, tokens, dim), dtype=k.dtype, device=k.device)
+    _check(_lib.fb4_qk_norm_rope(_dp(q), _strides(q), _dp(k), None if k is None else _strides(k), batch, tokens, heads, heads_k, dim, 1 if norm else 0,
+                                 _dp(gamma_q), _dp(gamma_k), float(eps), _dp(positions), 1 if n and positions.shape[0] == 1 else 0, _dp(freqs),
+                                 (ctypes.c_int32 * max(n, 1))(*axis_pairs), n, int(pairing), _dp(q_out), None if k is None else _dp(k_out),
+                                 _stream(stream)), where)
+    return q_out, (None if k is None else k_out)
+
+
+def _heads(where, q, k, lens):
+    """The sizes that the choice of blocks and the attention share, checked."""
+    batch, heads, tokens_q, dim = q.shape
+    _require(k.dim() == 4 and k.shape[0] == batch and k.shape[3] == dim and (lens is None or lens.shape == (batch, 2)), where)
+    for t in (q, k, lens):
+        _require(t is None or t.is_contiguous(), where, ERR_UNSUPPORTED)
+    return batch, heads, k.shape[1], tokens_q, k.shape[2], dim
+
+
+def fb4_select_key_blocks(q, k, top, block_q=128, block_k=128, lens=None, blocks=None, scores=None, want_scores=False, workspace=None, stream=None):
+    """q: bf16 cuda [batch][heads][tokens_q][dim], k: [batch][heads_k][tokens_k][dim], contiguous; lens: int32 cuda [batch][2] (queries, keys)
+    or None.  Returns int32 [batch][heads][query blocks][top], ascending, -1 behind (and the listed blocks' scores, float32, if asked)."""
+    where = "fb4_select_key_blocks"
+    _on_device(where, (q, torch.bfloat16), (k, torch.bfloat16), (lens, torch.int32), (blocks, torch.int32), (scores, torch.float32),
+               (workspace, torch.uint8))
+    batch, heads, heads_k, tokens_q, tokens_k, dim = _heads(where, q, k, lens)
+    _require(block_q > 0 and block_k > 0 and top >= 0, where)
+    shape = (batch, heads, (tokens_q + block_q - 1) // block_q, top)
+    for t in (blocks, scores):
+        _require(t is None or (t.shape == shape and t.is_contiguous()), where)
+    blocks = torch.empty(shape, dtype=torch.int32, device=q.device) if blocks is None else blocks
+    if want_scores and scores is None:
+        scores = torch.empty(shape, dtype=torch.float32, device=q.device)
+    size = _lib.fb4_select_key_blocks_workspace(batch, heads, heads_k, tokens_q, tokens_k, dim, block_q, block_k)
+    workspace = _workspace(workspace, size, q.device, stream)
+    _check(_lib.fb4_select_key_blocks(_dp(q), _dp(k), batch, heads, heads_k, tokens_q, tokens_k, dim, _dp(lens), block_q, block_k, top, _dp(blocks),
+                                      _dp(scores), _dp(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)), where)
+    return blocks if scores is None else (blocks, scores)
+
+
+def fb4_block_attention(q, k, v, blocks=None, scale=None, block_q=128, block_k=128, lens=None, out=None, lse=None, want_lse=False, workspace=None,
+                        stream=None):
+    """q: bf16 cuda [batch][heads][tokens_q][dim], k: [batch][heads_k][tokens_k][dim], contiguous; v: like k with any strides (contiguous
+    channels); blocks: int32 cuda [batch][heads][query blocks][n] or None for all keys; scale: dim ** -0.5 if None; lens: int32 cuda
+    [batch][2] (queries, keys) or None.  Returns bf16 [batch][tokens_q][heads][dim] -- rows of fb4_quantize -- (and the logarithms of the
+    sums, float32 [batch][heads][tokens_q], if asked).  Rows behind a sequence's last query are left as they were (zeros if not given)."""
+    where = "fb4_block_attention"
+    _on_device(where, (q, torch.bfloat16), (k, torch.bfloat16), (v, torch.bfloat16), (blocks, torch.int32), (lens, torch.int32),
+               (out, torch.bfloat16), (lse, torch.float32), (workspace, torch.uint8))
+    batch, heads, heads_k, tokens_q, tokens_k, dim = _heads(where, q, k, lens)
+    _require(block_q > 0 and block_k > 0 and v.shape == k.shape, where)
+    shape, top = (batch, tokens_q, heads, dim), ALL_BLOCKS
+    if blocks is not None:
+        top = blocks.shape[-1]
+        _require(blocks.shape == (batch, heads, (tokens_q + block_q - 1) // block_q, top), where)
+        _require(blocks.is_contiguous(), where, ERR_UNSUPPORTED)
+    _require((out is None or out.shape == shape) and (lse is None or lse.shape == (batch, heads, tokens_q)), where)
+    for t in (v, out):
+        _require(t is None or dim == 1 or t.numel() == 0 or t.stride(3) == 1, where, ERR_UNSUPPORTED)
+    _require(lse is None or lse.is_contiguous(), where, ERR_UNSUPPORTED)
+    empty = torch.empty if lens is None else torch.zeros
+    out = empty(shape, dtype=q.dtype, device=q.device) if out is None else out
+    if want_lse and lse is None:
+        lse = empty((batch, heads, tokens_q), dtype=torch.float32, device=q.device)
+    size = _lib.fb4_block_attention_workspace(batch, heads, heads_k, tokens_q, tokens_k, dim, top, block_q, block_k)
+    workspace = _workspace(workspace, size, q.device, stream)
+    _check(_lib.fb4_block_attention(_dp(q), _dp(k), _dp(v), _strides(v), batch, heads, heads_k, tokens_q, tokens_k, dim, _dp(lens), _dp(blocks), top,
+                                    block_q, block_k, float(dim ** -0.5 if scale is None else scale), _dp(out), _strides(out.transpose(1, 2)),
+                                    _dp(lse), _dp(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)), where)
+    return out if lse is None else (out, lse)
 
 
 def fb4_probe_mfma_rate(workgroups, iterations, random_operands=True, out=None, stream=None):

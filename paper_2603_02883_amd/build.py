@@ -16,7 +16,7 @@ CALL = os.path.join(HERE, "_fb4call" + sysconfig.get_config_var("EXT_SUFFIX"))
 CALL_SOURCE = os.path.join(CSRC, "fb4_pycall.c")
 OBJ_DIR = os.path.join(HERE, "_build")
 # one translation unit per group of entry points, compiled side by side
-SOURCES = [os.path.join(CSRC, f) for f in ("fb4_api.hip", "fb4_producers.hip", "fb4_attention.hip")]
+SOURCES = [os.path.join(CSRC, f) for f in ("fb4_api.hip", "fb4_producers.hip", "fb4_attention.hip", "fb4_heads.hip")]
 HEADER = os.path.join(os.path.dirname(HERE), "include", "fb4.h")
 DEPS = SOURCES + [os.path.join(CSRC, f) for f in sorted(os.listdir(CSRC)) if f.endswith(".hpp")] + [HEADER]
 PYTHON_INCLUDE = sysconfig.get_paths()["include"]

@@ -1,0 +1,181 @@
+// C ABI of the FB4 quantizer library, the attention path itself: norms and rotation of queries and keys, the choice of key
+// blocks, attention over them.  Declarations and contracts are in include/fb4.h.
+#include <algorithm>
+#include <cmath>
+
+#include "fb4_block_attention.hpp"
+#include "fb4_common.hpp"
+#include "fb4_rope.hpp"
+
+using namespace fb4;
+
+namespace {
+
+constexpr int64_t kMaxTokens = 0x7FFFFFFF;
+constexpr int64_t kMaxWorkgroups = (1 << 24) - 1;   // a launch takes fewer than 2^32 threads, 256 per workgroup
+
+// (batch, head, token) strides in elements to units of 8: what the kernels count in.
+template <typename T>
+int strides_of(const int64_t* strides, T* out)
+{
+    for (int i = 0; i < 3; ++i) {
+        if (strides[i] < 0) return FB4_ERR_INVALID_ARG;
+        if (strides[i] % 8 || strides[i] / 8 > 0xFFFFFFFFll) return FB4_ERR_UNSUPPORTED;
+    }
+    *out = T{(uint32_t)(strides[0] / 8), (uint32_t)(strides[1] / 8), (uint32_t)(strides[2] / 8)};
+    return FB4_OK;
+}
+
+// What the choice of blocks and the attention have in common.
+int check_blocks(int64_t batch, int heads, int heads_k, int64_t tokens_q, int64_t tokens_k, int64_t dim, int block_q, int block_k, BlockShape* s)
+{
+    if (batch < 0 || heads < 1 || heads_k < 1 || tokens_q < 0 || tokens_k < 0 || dim < 1 || heads % heads_k) return FB4_ERR_INVALID_ARG;
+    if ((block_q != 64 && block_q != 128) || (block_k != 64 && block_k != 128)) return FB4_ERR_UNSUPPORTED;
+    if (heads > 65535 || dim % 8 || dim > 128 || tokens_q > kMaxTokens || tokens_k > kMaxTokens || batch > kMaxTokens) return FB4_ERR_UNSUPPORTED;
+    *s = BlockShape{(uint32_t)tokens_q, (uint32_t)tokens_k, (uint16_t)heads, (uint16_t)heads_k, (uint16_t)block_q, (uint16_t)block_k,
+                    (uint32_t)((tokens_q + block_q - 1) / block_q), (uint32_t)((tokens_k + block_k - 1) / block_k)};
+    return FB4_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int fb4_qk_norm_rope(const void* q, const int64_t* q_strides, const void* k, const int64_t* k_strides, int64_t batch, int64_t tokens, int heads_q,
+                     int heads_k, int64_t dim, int norm, const float* gamma_q, const float* gamma_k, float eps, const int32_t* positions,
+                     int positions_shared, const double* freqs, const int32_t* axis_pairs, int n_axes, int pairing, void* q_out, void* k_out,
+                     void* stream)
+{
+    if (batch < 0 || tokens < 0 || heads_q < 1 || heads_k < 0 || dim < 1 || (norm != 0 && norm != 1) ||
+        (positions_shared != 0 && positions_shared != 1) || n_axes < 0 || (pairing != FB4_ROPE_ADJACENT && pairing != FB4_ROPE_HALVES))
+        return FB4_ERR_INVALID_ARG;
+    if (norm && !(eps >= 0.0f)) return FB4_ERR_INVALID_ARG;
+    if (n_axes > 4) return FB4_ERR_UNSUPPORTED;
+    if (n_axes > 0 && !axis_pairs) return FB4_ERR_INVALID_ARG;
+    int64_t pairs = 0;
+    uint8_t ends[4] = {0, 0, 0, 0};
+    for (int a = 0; a < 4; ++a) {
+        if (a < n_axes) {
+            if (axis_pairs[a] < 1 || axis_pairs[a] > dim) return FB4_ERR_INVALID_ARG;
+            pairs += axis_pairs[a];
+        }
+        if (2 * pairs > dim) return FB4_ERR_INVALID_ARG;
+        ends[a] = (uint8_t)std::min<int64_t>(pairs, 255);
+    }
+    if (dim % 8 || dim > 256 || heads_q > 65535 || heads_k > 65535 || (pairing == FB4_ROPE_HALVES && pairs % 4)) return FB4_ERR_UNSUPPORTED;
+    if (batch == 0 || tokens == 0) return FB4_OK;
+    if (!q || !q_strides || !q_out || (heads_k > 0 && (!k || !k_strides || !k_out)) || (pairs > 0 && (!positions || !freqs))) return FB4_ERR_INVALID_ARG;
+    RopeStrides sq = {0, 0, 0}, sk = {0, 0, 0};
+    if (int rc = strides_of(q_strides, &sq)) return rc;
+    if (heads_k > 0) {
+        if (int rc = strides_of(k_strides, &sk)) return rc;
+    }
+    if (!aligned(q, 16) || !aligned(q_out, 16) || (heads_k > 0 && (!aligned(k, 16) || !aligned(k_out, 16))) || !aligned(gamma_q, 4) ||
+        !aligned(gamma_k, 4) || !aligned(positions, 4) || !aligned(freqs, 8))
+        return FB4_ERR_UNSUPPORTED;
+    if (batch > (1 << 25) || tokens > (1 << 25) || batch * tokens > (1 << 25)) return FB4_ERR_UNSUPPORTED;   // (2^26 wavefronts to a launch)
+    const int pieces = (int)(dim / 8);
+    int lanes = 1;
+    while (lanes < pieces) lanes *= 2;
+    const int rows = 64 / lanes, steps = (heads_q + rows - 1) / rows + (heads_k + rows - 1) / rows;
+    // A wavefront per token; several while there are few tokens.
+    const int64_t n = batch * tokens;
+    const int64_t chunks = std::min<int64_t>(std::min(steps, 255), std::max<int64_t>(1, 2048 / n));
+    RopeShape s = {(uint32_t)tokens, (uint32_t)n, (uint16_t)heads_q, (uint16_t)heads_k, eps, (uint8_t)pieces, {ends[0], ends[1], ends[2]},
+                   (uint8_t)n_axes, (uint8_t)pairs, (uint8_t)((norm ? kRopeNorm : 0) | (positions_shared ? kRopeShared : 0)), (uint8_t)chunks};
+    const dim3 grid((unsigned)((n * chunks + kRopeThreads / 64 - 1) / (kRopeThreads / 64)));
+#define FB4_ROPE_LAUNCH(pairing_, l) launch(qk_norm_rope_kernel<pairing_, l>, grid, dim3(kRopeThreads), 0, static_cast<hipStream_t>(stream), static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k), static_cast<uint16_t*>(q_out), static_cast<uint16_t*>(k_out), gamma_q, gamma_k, freqs, positions, sq, sk, s)
+#define FB4_ROPE_CASE(l)                                                          \
+    case l:                                                                       \
+        if (pairing == FB4_ROPE_ADJACENT) FB4_ROPE_LAUNCH(kRopeAdjacent, l);      \
+        else FB4_ROPE_LAUNCH(kRopeHalves, l);                                     \
+        break;
+    switch (lanes) {
+        FB4_ROPE_CASE(1) FB4_ROPE_CASE(2) FB4_ROPE_CASE(4) FB4_ROPE_CASE(8) FB4_ROPE_CASE(16) FB4_ROPE_CASE(32)
+    }
+#undef FB4_ROPE_CASE
+#undef FB4_ROPE_LAUNCH
+    return hipGetLastError() == hipSuccess ? FB4_OK : FB4_ERR_HIP;
+}
+
+size_t fb4_select_key_blocks_workspace(int64_t batch, int heads, int heads_k, int64_t tokens_q, int64_t tokens_k, int64_t dim, int block_q, int block_k)
+{
+    BlockShape s;
+    if (check_blocks(batch, heads, heads_k, tokens_q, tokens_k, dim, block_q, block_k, &s) != FB4_OK) return 0;
+    return (size_t)batch * ((size_t)heads * s.blocks_q + (size_t)heads_k * s.blocks_k) * (size_t)dim * sizeof(double);
+}
+
+int fb4_select_key_blocks(const void* q, const void* k, int64_t batch, int heads, int heads_k, int64_t tokens_q, int64_t tokens_k, int64_t dim,
+                          const int32_t* lens, int block_q, int block_k, int64_t top, int32_t* blocks, float* scores, void* workspace,
+                          size_t workspace_bytes, void* stream)
+{
+    BlockShape s;
+    if (int rc = check_blocks(batch, heads, heads_k, tokens_q, tokens_k, dim, block_q, block_k, &s)) return rc;
+    if (top < 0) return FB4_ERR_INVALID_ARG;
+    if (batch == 0 || tokens_q == 0 || top == 0) return FB4_OK;
+    if (!q || (tokens_k > 0 && !k) || !blocks || !workspace) return FB4_ERR_INVALID_ARG;
+    if (workspace_bytes < fb4_select_key_blocks_workspace(batch, heads, heads_k, tokens_q, tokens_k, dim, block_q, block_k)) return FB4_ERR_INVALID_ARG;
+    const int64_t n_q = batch * heads * s.blocks_q, n_k = batch * heads_k * s.blocks_k;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(lens, 4) || !aligned(blocks, 4) || !aligned(scores, 4) || !aligned(workspace, 8)) return FB4_ERR_UNSUPPORTED;
+    if (s.blocks_k > kSelectMaxBlocks || n_q + n_k > kMaxWorkgroups || top > kMaxTokens) return FB4_ERR_UNSUPPORTED;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    double* means = static_cast<double*>(workspace);
+    const uint32_t pieces = (uint32_t)(dim / 8);
+    const dim3 grid((unsigned)(n_q + n_k));
+#define FB4_MEANS(l) launch(block_means_kernel<l>, grid, dim3(kMeanThreads), 0, st, static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k), lens, means, (uint32_t)n_q, pieces, s)
+    if (pieces > 8) FB4_MEANS(16);
+    else if (pieces > 4) FB4_MEANS(8);
+    else FB4_MEANS(4);
+#undef FB4_MEANS
+    launch(select_blocks_kernel, dim3((unsigned)n_q), dim3(64), 0, st, means, lens, blocks, scores, (uint32_t)top, (uint32_t)n_q, (uint32_t)dim, s);
+    return hipGetLastError() == hipSuccess ? FB4_OK : FB4_ERR_HIP;
+}
+
+size_t fb4_block_attention_workspace(int64_t batch, int heads, int heads_k, int64_t tokens_q, int64_t tokens_k, int64_t dim, int64_t top, int block_q,
+                                     int block_k)
+{
+    BlockShape s;
+    if (check_blocks(batch, heads, heads_k, tokens_q, tokens_k, dim, block_q, block_k, &s) != FB4_OK || top < FB4_ALL_BLOCKS) return 0;
+    return 0;
+}
+
+int fb4_block_attention(const void* q, const void* k, const void* v, const int64_t* v_strides, int64_t batch, int heads, int heads_k, int64_t tokens_q,
+                        int64_t tokens_k, int64_t dim, const int32_t* lens, const int32_t* blocks, int64_t top, int block_q, int block_k, float scale,
+                        void* out, const int64_t* out_strides, float* lse, void* workspace, size_t workspace_bytes, void* stream)
+{
+    BlockShape s;
+    if (int rc = check_blocks(batch, heads, heads_k, tokens_q, tokens_k, dim, block_q, block_k, &s)) return rc;
+    if (top < FB4_ALL_BLOCKS || !(scale > 0.0f) || !std::isfinite(scale)) return FB4_ERR_INVALID_ARG;
+    if (top == FB4_ALL_BLOCKS ? blocks != nullptr : top > 0 && !blocks) return FB4_ERR_INVALID_ARG;
+    if (batch == 0 || tokens_q == 0) return FB4_OK;
+    if (!q || !out || !out_strides || (tokens_k > 0 && (!k || !v || !v_strides))) return FB4_ERR_INVALID_ARG;
+    const size_t needed = fb4_block_attention_workspace(batch, heads, heads_k, tokens_q, tokens_k, dim, top, block_q, block_k);
+    if (workspace_bytes < needed || (needed > 0 && !workspace)) return FB4_ERR_INVALID_ARG;
+    TensorStrides sv = {0, 0, 0}, so;
+    if (tokens_k > 0) {
+        if (int rc = strides_of(v_strides, &sv)) return rc;
+    }
+    if (int rc = strides_of(out_strides, &so)) return rc;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) || !aligned(lens, 4) || !aligned(blocks, 4) || !aligned(lse, 4) ||
+        !aligned(workspace, 16))
+        return FB4_ERR_UNSUPPORTED;
+    const int64_t n = batch * heads * s.blocks_q;
+    if (n > kMaxWorkgroups || top > kMaxTokens) return FB4_ERR_UNSUPPORTED;
+    const AttentionShape a = {s.tokens_q, s.tokens_k, (uint32_t)top, s.heads, s.heads_k, (uint8_t)(block_q / 64), (uint8_t)(block_k / 64),
+                              (uint8_t)(dim / 8), 0, s.blocks_q, (uint32_t)n, scale};
+    const dim3 grid((unsigned)n);
+#define FB4_ATTENTION_LAUNCH(d, w) launch(block_attention_kernel<d, w>, grid, dim3(64 * w), 0, static_cast<hipStream_t>(stream), static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), static_cast<uint16_t*>(out), lse, blocks, lens, sv, so, a)
+#define FB4_ATTENTION_CASE(d)                              \
+    case d:                                                \
+        if (block_q == 64) FB4_ATTENTION_LAUNCH(d, 2);     \
+        else FB4_ATTENTION_LAUNCH(d, 4);                   \
+        break;
+    switch ((dim + 31) / 32) {
+        FB4_ATTENTION_CASE(1) FB4_ATTENTION_CASE(2) FB4_ATTENTION_CASE(3) FB4_ATTENTION_CASE(4)
+    }
+#undef FB4_ATTENTION_CASE
+#undef FB4_ATTENTION_LAUNCH
+    return hipGetLastError() == hipSuccess ? FB4_OK : FB4_ERR_HIP;
+}
+
+}  // extern "C"

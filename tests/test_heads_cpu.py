@@ -1,0 +1,97 @@
+"""What the attention path's entry points refuse, before any GPU work: no device is needed (pointers are host buffers that are
+never dereferenced), and what the binding refuses to hand on."""
+
+import ctypes
+
+import pytest
+import torch
+
+import paper_2603_02883_amd as F
+from paper_2603_02883_amd import binding as B
+
+P = ctypes.c_void_p
+BUF = ctypes.create_string_buffer(4096 + 64)
+AL = (ctypes.addressof(BUF) + 63) // 64 * 64
+NAN, INF = float("nan"), float("inf")
+
+
+def strides(*s):
+    return (ctypes.c_int64 * 3)(*s)
+
+
+def rope(q=P(AL), sq=strides(2048, 64, 256), k=P(AL), sk=strides(2048, 64, 256), batch=2, tokens=4, hq=2, hk=2, dim=64, norm=1, gq=None, gk=None,
+         eps=1e-6, pos=P(AL), shared=0, freqs=P(AL), pairs=(8, 24), axes=None, pairing=0, qo=P(AL), ko=P(AL)):
+    p = (ctypes.c_int32 * max(len(pairs), 1))(*pairs) if pairs is not None else None
+    return B.lib().fb4_qk_norm_rope(q, sq, k, sk, batch, tokens, hq, hk, dim, norm, gq, gk, eps, pos, shared, freqs, p,
+                                    len(pairs) if axes is None else axes, pairing, qo, ko, None)
+
+
+def test_rope_refusals():
+    assert rope(batch=0) == F.OK and rope(tokens=0, q=None, k=None) == F.OK
+    for bad in (dict(batch=-1), dict(tokens=-1), dict(hq=0), dict(hk=-1), dict(dim=0), dict(norm=2), dict(eps=-1.0), dict(eps=NAN), dict(shared=2),
+                dict(pairing=2), dict(pairs=(), axes=-1), dict(pairs=(0, 8)), dict(pairs=(16, 17)), dict(pairs=(2 ** 31 - 1, 2 ** 31 - 1)),
+                dict(pairs=None, axes=1), dict(q=None), dict(k=None), dict(sq=None), dict(sk=None), dict(qo=None), dict(ko=None), dict(pos=None),
+                dict(freqs=None), dict(sq=strides(-8, 64, 256))):
+        assert rope(**bad) == F.ERR_INVALID_ARG, bad
+    for bad in (dict(dim=60, pairs=(8,)), dict(dim=264), dict(pairs=(6, 8), pairing=1), dict(pairs=(4,) * 5), dict(sq=strides(2048, 60, 256)),
+                dict(sk=strides(2048, 64, 2 ** 36)), dict(q=P(AL + 8)), dict(k=P(AL + 2)), dict(qo=P(AL + 8)), dict(ko=P(AL + 4)), dict(gq=P(AL + 2)),
+                dict(pos=P(AL + 2)), dict(freqs=P(AL + 4)), dict(tokens=2 ** 25), dict(batch=2 ** 62, tokens=2 ** 62), dict(hq=70000)):
+        assert rope(**bad) == F.ERR_UNSUPPORTED, bad
+
+
+def select(q=P(AL), k=P(AL), batch=1, heads=4, hk=2, tq=200, tk=300, dim=64, lens=None, bq=64, bk=128, top=2, blocks=P(AL), scores=None, ws=P(AL),
+           size=1 << 20):
+    return B.lib().fb4_select_key_blocks(q, k, batch, heads, hk, tq, tk, dim, lens, bq, bk, top, blocks, scores, ws, size, None)
+
+
+def test_select_refusals():
+    assert select(batch=0) == F.OK and select(tq=0) == F.OK and select(top=0, blocks=None) == F.OK
+    size = B.lib().fb4_select_key_blocks_workspace(1, 4, 2, 200, 300, 64, 64, 128)
+    assert size == (4 * 4 + 2 * 3) * 64 * 8
+    for bad in (dict(batch=-1), dict(heads=0), dict(hk=0), dict(hk=3), dict(tq=-1), dict(tk=-1), dict(dim=0), dict(top=-1), dict(q=None), dict(k=None),
+                dict(blocks=None), dict(ws=None), dict(size=size - 1)):
+        assert select(**bad) == F.ERR_INVALID_ARG, bad
+    for bad in (dict(dim=60), dict(dim=136), dict(bq=32), dict(bk=96), dict(bk=0), dict(q=P(AL + 8)), dict(k=P(AL + 8)), dict(lens=P(AL + 2)),
+                dict(blocks=P(AL + 1)), dict(scores=P(AL + 2)), dict(ws=P(AL + 4)), dict(tk=128 * 2049, size=1 << 40), dict(heads=70000, hk=1),
+                dict(tq=2 ** 31), dict(tk=2 ** 31), dict(batch=2 ** 32)):
+        assert select(**bad) == F.ERR_UNSUPPORTED, bad
+    assert B.lib().fb4_select_key_blocks_workspace(1, 4, 3, 200, 300, 64, 64, 128) == 0
+
+
+def attention(q=P(AL), k=P(AL), v=P(AL), sv=strides(0, 64, 128), batch=1, heads=4, hk=2, tq=200, tk=300, dim=64, lens=None, blocks=P(AL), top=2, bq=64,
+              bk=128, scale=0.125, out=P(AL), so=strides(0, 64, 256), lse=None, ws=None, size=0):
+    return B.lib().fb4_block_attention(q, k, v, sv, batch, heads, hk, tq, tk, dim, lens, blocks, top, bq, bk, scale, out, so, lse, ws, size, None)
+
+
+def test_attention_refusals():
+    assert attention(batch=0) == F.OK and attention(tq=0, out=None) == F.OK
+    big = dict(ws=P(AL), size=1 << 40)   # (enough for any of these)
+    for bad in (dict(batch=-1), dict(heads=0), dict(hk=0), dict(hk=3), dict(tq=-1), dict(tk=-1), dict(dim=0), dict(top=-2), dict(q=None), dict(k=None),
+                dict(v=None), dict(blocks=None), dict(top=-1), dict(sv=None), dict(out=None), dict(so=None), dict(scale=0.0), dict(scale=-1.0), dict(scale=NAN), dict(scale=INF),
+                dict(sv=strides(0, -8, 128)), dict(so=strides(0, 64, -8))):
+        assert attention(**{**big, **bad}) == F.ERR_INVALID_ARG, bad
+    for bad in (dict(dim=60), dict(dim=136), dict(bq=32), dict(bk=96), dict(bk=0), dict(q=P(AL + 8)), dict(k=P(AL + 8)), dict(v=P(AL + 8)),
+                dict(out=P(AL + 8)), dict(lens=P(AL + 2)), dict(blocks=P(AL + 1)), dict(lse=P(AL + 2)), dict(sv=strides(0, 64, 132)),
+                dict(so=strides(4, 64, 256)), dict(heads=70000, hk=1), dict(tq=2 ** 31), dict(batch=2 ** 24)):
+        assert attention(**{**big, **bad}) == F.ERR_UNSUPPORTED, bad
+    # a workspace that is too small, or none where there has to be one
+    need = B.lib().fb4_block_attention_workspace(1, 1, 1, 1, 1 << 20, 64, -1, 64, 64)
+    one = dict(heads=1, hk=1, tq=1, tk=1 << 20, blocks=None, top=-1, bk=64)
+    if need:
+        assert attention(**one, ws=P(AL), size=need - 1) == F.ERR_INVALID_ARG
+        assert attention(**one, ws=None, size=need) == F.ERR_INVALID_ARG
+        assert attention(**one, ws=P(AL + 4), size=need) == F.ERR_UNSUPPORTED
+    assert B.lib().fb4_block_attention_workspace(1, 4, 3, 1, 1 << 20, 64, -1, 64, 64) == 0
+
+
+def test_binding_hands_on_no_host_tensors_and_no_other_types():
+    """A host pointer or another type's would be read as the device's bf16."""
+    q = torch.zeros((1, 2, 4, 8), dtype=torch.bfloat16)
+    for call in (lambda: F.fb4_qk_norm_rope(q, q, None, None, ()), lambda: F.fb4_select_key_blocks(q, q, 1), lambda: F.fb4_block_attention(q, q, q)):
+        with pytest.raises(F.Fb4Error) as e:
+            call()
+        assert e.value.code == F.ERR_INVALID_ARG
+
+
+def test_empty_calls_need_no_pointers_in_the_binding_either():
+    assert F.strerror(F.OK) and B.lib().fb4_block_attention_workspace(0, 1, 1, 0, 0, 8, 0, 64, 64) == 0
