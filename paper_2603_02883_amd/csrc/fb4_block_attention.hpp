@@ -52,11 +52,18 @@ __global__ __launch_bounds__(kMeanThreads) void block_means_kernel(const uint16_
     const uint32_t first = block * size, n = len > first ? min(len - first, size) : 0u;
     const uint32_t l = threadIdx.x % kLanes, sub = threadIdx.x / kLanes;
     double sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (l < pieces) {
-        const uint16_t* base = (is_k ? k : q) + ((size_t)g * tokens + first) * (pieces * 8u) + 8u * l;
-        for (uint32_t r = sub; r < n; r += kRows) {
-            const uint4 v = *reinterpret_cast<const uint4*>(base + (size_t)r * (pieces * 8u));
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    const uint16_t* base = (is_k ? k : q) + ((size_t)g * tokens + first) * (pieces * 8u) + 8u * l;
+    for (uint32_t r0 = 0; r0 < n; r0 += 4u * kRows) {
+        uint4 v[4];   // (a thread's reads before its sums)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t r = r0 + i * kRows + sub;
+            v[i] = make_uint4(0, 0, 0, 0);
+            if (l < pieces && r < n) v[i] = *reinterpret_cast<const uint4*>(base + (size_t)r * (pieces * 8u));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 sum[2 * j] += (double)__builtin_bit_cast(float, w[j] << 16);
@@ -88,55 +95,139 @@ __device__ __forceinline__ double score_of(uint64_t order)
     return __builtin_bit_cast(double, order >> 63 ? order & 0x7FFFFFFFFFFFFFFFull : ~order);
 }
 
-// One workgroup of one wavefront per block of queries.
-__global__ __launch_bounds__(64) void select_blocks_kernel(const double* means, const int32_t* lens, int32_t* chosen, float* scores, uint32_t top,
-                                                           uint32_t n_q, uint32_t dim, BlockShape s)
+typedef double select_f64x2 __attribute__((ext_vector_type(2)));
+typedef double select_f64x4 __attribute__((ext_vector_type(4)));
+
+// Rows (blocks of queries) of a workgroup: what a row of scores leaves of LDS.
+constexpr uint32_t select_rows(int values) { return values > 16 ? 8 : 16; }
+
+// A workgroup takes up to 16 blocks of queries of one head: their scores with all the head's blocks of keys by 16x16x4 MFMAs in
+// double, kept in LDS by their order, then the largest `top` of every row.  The channels of a product may come in any order as
+// long as both operands have the same: lane group k of 16 holds channels 16 c + 4 k .. + 3 for the four steps of chunk c, which are
+// 32 bytes of its row.
+// D16: channels / 16, rounded up; kValues: scores of a row per lane.
+template <int D16, int kValues>
+__global__ __launch_bounds__(256) void select_blocks_kernel(const double* means, const int32_t* lens, int32_t* chosen, float* scores, uint32_t top,
+                                                            uint32_t n_q, uint32_t dim, uint32_t row_tiles, uint32_t n_workgroups, BlockShape s)
 {
-    __shared__ uint64_t order[kSelectMaxBlocks];
-    const uint32_t lane = threadIdx.x;
-    const uint32_t g = blockIdx.x / s.blocks_q, block = blockIdx.x - g * s.blocks_q;
+    constexpr uint32_t kRows = select_rows(kValues);
+    __shared__ uint64_t order[kRows][64 * kValues];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t pos = xcd_local_position(blockIdx.x, n_workgroups);
+    const uint32_t g = pos / row_tiles, block0 = (pos - g * row_tiles) * kRows;
     const uint32_t b = g / s.heads, h = g - b * s.heads, gk = b * s.heads_k + h / (s.heads / s.heads_k);
     const uint32_t len_q = length_of(lens, b, 0, s.tokens_q), len_k = length_of(lens, b, 1, s.tokens_k);
-    const uint32_t n = block * s.block_q < len_q ? (len_k + s.block_k - 1) / s.block_k : 0u;   // blocks with a key; none for no query
-    const double* mq = means + (size_t)blockIdx.x * dim;
+    const uint32_t n = (len_k + s.block_k - 1) / s.block_k;   // blocks with a key
+    const uint32_t rows = min(s.blocks_q - block0, kRows);
+    const double* mq = means + ((size_t)g * s.blocks_q + block0) * dim;
     const double* mk = means + ((size_t)n_q + (size_t)gk * s.blocks_k) * dim;
-    for (uint32_t j = lane; j < n; j += 64) {
-        double sum = 0.0;
-        for (uint32_t c = 0; c < dim; ++c) sum = fma(mq[c], mk[(size_t)j * dim + c], sum);
-        order[j] = score_order(sum);
+    // ---- scores
+    {
+        const uint32_t r = lane & 15u, k4 = 4u * (lane >> 4);
+        double qa[4 * D16];
+        auto load = [&](const double* row, bool there, double* to) {
+#pragma unroll
+            for (int c = 0; c < D16; ++c) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    select_f64x2 w = {0.0, 0.0};
+                    if (there && (c < D16 - 1 || 16u * c + k4 < dim)) w = *reinterpret_cast<const select_f64x2*>(row + 16 * c + k4 + 2 * i);
+                    to[4 * c + 2 * i] = w[0];
+                    to[4 * c + 2 * i + 1] = w[1];
+                }
+            }
+        };
+        load(mq + (size_t)r * dim, r < rows, qa);
+        const uint32_t tiles = (n + 15u) / 16u;
+        double kb[4 * D16];
+        load(mk + (size_t)(16u * wave + r) * dim, 16u * wave + r < n, kb);
+        for (uint32_t t = wave; t < tiles; t += 4) {
+            double next[4 * D16];
+            load(mk + (size_t)(16u * (t + 4) + r) * dim, 16u * (t + 4) + r < n, next);
+            select_f64x4 acc = {0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < 4 * D16; ++i) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(qa[i], kb[i], acc, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {   // accumulator i: row lane / 16 + 4 i, column lane % 16
+                const uint32_t row = (lane >> 4) + 4u * i, j = 16u * t + r;
+                if (row < kRows) order[row][j] = j < n ? score_order(acc[i]) : 0;
+            }
+#pragma unroll
+            for (int i = 0; i < 4 * D16; ++i) kb[i] = next[i];
+        }
     }
     __syncthreads();
-    const uint32_t want = min(top, n);
-    // the want-th largest: bit by bit, how many are at least as large
-    uint64_t bound = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-        const uint64_t trial = bound | 1ull << bit;
-        uint32_t count = 0;
-        for (uint32_t j0 = 0; j0 < n; j0 += 64) count += __popcll(__ballot(j0 + lane < n && order[j0 + lane] >= trial));
-        if (count >= want) bound = trial;
-    }
-    uint32_t above = 0;
-    for (uint32_t j0 = 0; j0 < n; j0 += 64) above += __popcll(__ballot(j0 + lane < n && order[j0 + lane] > bound));
-    uint32_t ties = want - above, out = 0;   // of those at the bound, the first
-    int32_t* to = chosen + (size_t)blockIdx.x * top;
-    float* to_score = scores ? scores + (size_t)blockIdx.x * top : nullptr;
+    // ---- the largest of every row
     const uint64_t before = (1ull << lane) - 1;
-    for (uint32_t j0 = 0; j0 < n; j0 += 64) {
-        const uint64_t mine = j0 + lane < n ? order[j0 + lane] : 0;
-        const uint64_t equal = __ballot(j0 + lane < n && mine == bound);
-        const bool taken = j0 + lane < n && (mine > bound || (mine == bound && (uint32_t)__popcll(equal & before) < ties));
-        const uint64_t all = __ballot(taken);
-        if (taken) {
-            const uint32_t at = out + (uint32_t)__popcll(all & before);
-            to[at] = (int32_t)(j0 + lane);
-            if (to_score) to_score[at] = (float)score_of(mine);
+    for (uint32_t row = wave; row < rows; row += 4) {
+        const uint32_t have = (block0 + row) * s.block_q < len_q ? n : 0u;   // (no query: no blocks)
+        const uint32_t want = min(top, have);
+        uint32_t high[kValues], low[kValues];   // (0, 0: no block)
+#pragma unroll
+        for (int i = 0; i < kValues; ++i) {
+            const uint64_t v = 64u * i + lane < have ? order[row][64u * i + lane] : 0;
+            high[i] = (uint32_t)(v >> 32);
+            low[i] = (uint32_t)v;
         }
-        out += (uint32_t)__popcll(all);
-        ties -= min(ties, (uint32_t)__popcll(equal));
-    }
-    for (uint32_t at = want + lane; at < top; at += 64) {
-        to[at] = -1;
-        if (to_score) to_score[at] = __builtin_nanf("");
+        // The want-th largest, bit by bit from the first in which the upper halves differ: is it at least as large as with this
+        // bit set?  When exactly `want` are, they are the ones; else the lower halves of those with its upper half decide.
+        uint32_t bound = 0, bound_low = 0, above = 0;
+        bool found = false;
+        if (want > 0) {
+            const uint32_t first = __builtin_amdgcn_readfirstlane(high[0]);
+            uint32_t differ = 0;
+#pragma unroll
+            for (int i = 0; i < kValues; ++i) differ |= 64u * i + lane < have ? high[i] ^ first : 0;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) differ |= __shfl_xor(differ, d);
+            differ = __builtin_amdgcn_readfirstlane(differ);
+            int bit = differ ? 31 - __builtin_clz(differ) : -1;
+            bound = bit < 0 ? first : bit == 31 ? 0u : first >> (bit + 1) << (bit + 1);
+            for (; bit >= 0 && !found; --bit) {
+                const uint32_t trial = bound | 1u << bit;
+                uint32_t count = 0;
+#pragma unroll
+                for (int i = 0; i < kValues; ++i) count += (uint32_t)__popcll(__ballot(high[i] >= trial));
+                if (count >= want) bound = trial;
+                found = count == want;
+            }
+            if (!found) {
+#pragma unroll
+                for (int i = 0; i < kValues; ++i) above += (uint32_t)__popcll(__ballot(high[i] > bound));
+                for (bit = 31; bit >= 0; --bit) {
+                    const uint32_t trial = bound_low | 1u << bit;
+                    uint32_t count = above;
+#pragma unroll
+                    for (int i = 0; i < kValues; ++i) count += (uint32_t)__popcll(__ballot(high[i] == bound && low[i] >= trial));
+                    if (count >= want) bound_low = trial;
+                }
+#pragma unroll
+                for (int i = 0; i < kValues; ++i) above += (uint32_t)__popcll(__ballot(high[i] == bound && low[i] > bound_low));
+            }
+        }
+        uint32_t ties = found ? want : want - above, out = 0;   // of those at the bound, the first (found: all that are left)
+        const size_t at_row = ((size_t)g * s.blocks_q + block0 + row) * top;
+        int32_t* to = chosen + at_row;
+        float* to_score = scores ? scores + at_row : nullptr;
+#pragma unroll
+        for (int i = 0; i < kValues; ++i) {
+            if (64u * i >= have) break;
+            const bool larger = found ? high[i] >= bound : high[i] > bound || (high[i] == bound && low[i] > bound_low);
+            const uint64_t equal = __ballot(!found && 64u * i + lane < have && high[i] == bound && low[i] == bound_low);
+            const bool taken = want > 0 && 64u * i + lane < have && (larger || (equal >> lane & 1 && (uint32_t)__popcll(equal & before) < ties));
+            const uint64_t all = __ballot(taken);
+            if (taken) {
+                const uint32_t at = out + (uint32_t)__popcll(all & before);
+                to[at] = (int32_t)(64u * i + lane);
+                if (to_score) to_score[at] = (float)score_of((uint64_t)high[i] << 32 | low[i]);
+            }
+            out += (uint32_t)__popcll(all);
+            ties -= min(ties, (uint32_t)__popcll(equal));
+        }
+        for (uint32_t at = want + lane; at < top; at += 64) {
+            to[at] = -1;
+            if (to_score) to_score[at] = __builtin_nanf("");
+        }
     }
 }
 

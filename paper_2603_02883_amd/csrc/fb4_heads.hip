@@ -116,7 +116,7 @@ int fb4_select_key_blocks(const void* q, const void* k, int64_t batch, int heads
     if (!q || (tokens_k > 0 && !k) || !blocks || !workspace) return FB4_ERR_INVALID_ARG;
     if (workspace_bytes < fb4_select_key_blocks_workspace(batch, heads, heads_k, tokens_q, tokens_k, dim, block_q, block_k)) return FB4_ERR_INVALID_ARG;
     const int64_t n_q = batch * heads * s.blocks_q, n_k = batch * heads_k * s.blocks_k;
-    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(lens, 4) || !aligned(blocks, 4) || !aligned(scores, 4) || !aligned(workspace, 8)) return FB4_ERR_UNSUPPORTED;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(lens, 4) || !aligned(blocks, 4) || !aligned(scores, 4) || !aligned(workspace, 16)) return FB4_ERR_UNSUPPORTED;
     if (s.blocks_k > kSelectMaxBlocks || n_q + n_k > kMaxWorkgroups || top > kMaxTokens) return FB4_ERR_UNSUPPORTED;
     hipStream_t st = static_cast<hipStream_t>(stream);
     double* means = static_cast<double*>(workspace);
@@ -127,7 +127,22 @@ int fb4_select_key_blocks(const void* q, const void* k, int64_t batch, int heads
     else if (pieces > 4) FB4_MEANS(8);
     else FB4_MEANS(4);
 #undef FB4_MEANS
-    launch(select_blocks_kernel, dim3((unsigned)n_q), dim3(64), 0, st, means, lens, blocks, scores, (uint32_t)top, (uint32_t)n_q, (uint32_t)dim, s);
+    const uint32_t rows = s.blocks_k > 1024 ? select_rows(32) : select_rows(16), row_tiles = (s.blocks_q + rows - 1) / rows;
+    const dim3 sgrid((unsigned)(batch * heads * row_tiles));
+#define FB4_SELECT_LAUNCH(d, v) launch(select_blocks_kernel<d, v>, sgrid, dim3(256), 0, st, means, lens, blocks, scores, (uint32_t)top, (uint32_t)n_q, (uint32_t)dim, row_tiles, sgrid.x, s)
+#define FB4_SELECT_CASE(d)                                       \
+    case d:                                                      \
+        if (s.blocks_k <= 128) FB4_SELECT_LAUNCH(d, 2);          \
+        else if (s.blocks_k <= 512) FB4_SELECT_LAUNCH(d, 8);     \
+        else if (s.blocks_k <= 1024) FB4_SELECT_LAUNCH(d, 16);   \
+        else FB4_SELECT_LAUNCH(d, 32);                           \
+        break;
+    switch ((dim + 15) / 16) {
+        FB4_SELECT_CASE(1) FB4_SELECT_CASE(2) FB4_SELECT_CASE(3) FB4_SELECT_CASE(4)
+        FB4_SELECT_CASE(5) FB4_SELECT_CASE(6) FB4_SELECT_CASE(7) FB4_SELECT_CASE(8)
+    }
+#undef FB4_SELECT_CASE
+#undef FB4_SELECT_LAUNCH
     return hipGetLastError() == hipSuccess ? FB4_OK : FB4_ERR_HIP;
 }
 
