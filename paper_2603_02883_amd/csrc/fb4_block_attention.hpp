@@ -81,148 +81,184 @@ __global__ __launch_bounds__(kMeanThreads) void block_means_kernel(const uint16_
     }
 }
 
-// A score's place in the order: larger is better, a NaN below every number (and above 0, which is no block).
-__device__ __forceinline__ uint64_t score_order(double score)
+// A number's place in the order: larger is better, a NaN below every number (and above 0, which is no block), -0 is 0.
+__device__ __forceinline__ uint32_t order_of(float x)
 {
-    const uint64_t u = __builtin_bit_cast(uint64_t, score);
-    if (score != score) return 1ull;
-    // (-0 is 0; the smallest number, -Inf, comes to 0x000FFFFFFFFFFFFF)
-    return score == 0.0 ? 0x8000000000000000ull : u >> 63 ? ~u : u | 0x8000000000000000ull;
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    return x != x ? 1u : x == 0.0f ? 0x80000000u : u >> 31 ? ~u : u | 0x80000000u;   // (-Inf comes to 0x007FFFFF)
 }
-__device__ __forceinline__ double score_of(uint64_t order)
+__device__ __forceinline__ float number_of(uint32_t order)
 {
-    if (order == 1ull) return __builtin_nan("");
-    return __builtin_bit_cast(double, order >> 63 ? order & 0x7FFFFFFFFFFFFFFFull : ~order);
+    return order == 1u ? __builtin_nanf("") : __builtin_bit_cast(float, order >> 31 ? order & 0x7FFFFFFFu : ~order);
+}
+__device__ __forceinline__ uint64_t order_of(double x)
+{
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    return x != x ? 1ull : x == 0.0 ? 0x8000000000000000ull : u >> 63 ? ~u : u | 0x8000000000000000ull;
 }
 
 typedef double select_f64x2 __attribute__((ext_vector_type(2)));
 typedef double select_f64x4 __attribute__((ext_vector_type(4)));
+constexpr int kSelectThreads = 512;
+constexpr uint32_t kSelectRows = 16;   // blocks of queries to a workgroup
 
-// Rows (blocks of queries) of a workgroup: what a row of scores leaves of LDS.
-constexpr uint32_t select_rows(int values) { return values > 16 ? 8 : 16; }
-
-// A workgroup takes up to 16 blocks of queries of one head: their scores with all the head's blocks of keys by 16x16x4 MFMAs in
-// double, kept in LDS by their order, then the largest `top` of every row.  The channels of a product may come in any order as
-// long as both operands have the same: lane group k of 16 holds channels 16 c + 4 k .. + 3 for the four steps of chunk c, which are
-// 32 bytes of its row.
+// A workgroup takes 16 blocks of queries of one head: their scores with all the head's blocks of keys by 16x16x4 MFMAs in double,
+// then the largest `top` of every row.  The channels of a product may come in any order as long as both operands have the same:
+// lane group k of 16 holds channels 16 c + 4 k .. + 3 for the four steps of chunk c, which are 32 bytes of its row.
+// LDS keeps the scores rounded to fp32, half of what the doubles would take, so that one workgroup's search runs beside another's
+// products.  Rounding keeps the order but for what becomes equal, so the fp32 values decide unless the border falls between
+// equal ones; those blocks' scores are then formed again in double.
 // D16: channels / 16, rounded up; kValues: scores of a row per lane.
+// Measured: 24 heads x 1024 x 1024 blocks x 128 channels 424 us with doubles in LDS and a search bit by bit on four wavefronts.
 template <int D16, int kValues>
-__global__ __launch_bounds__(256) void select_blocks_kernel(const double* means, const int32_t* lens, int32_t* chosen, float* scores, uint32_t top,
-                                                            uint32_t n_q, uint32_t dim, uint32_t row_tiles, uint32_t n_workgroups, BlockShape s)
+__global__ __launch_bounds__(kSelectThreads) __attribute__((amdgpu_waves_per_eu(kValues > 16 ? 2 : 4)))
+void select_blocks_kernel(const double* means, const int32_t* lens, int32_t* chosen, float* scores, uint32_t top, uint32_t n_q, uint32_t dim,
+                          uint32_t row_tiles, uint32_t n_workgroups, BlockShape s)
 {
-    constexpr uint32_t kRows = select_rows(kValues);
-    __shared__ uint64_t order[kRows][64 * kValues];
+    constexpr uint32_t kWaves = kSelectThreads / 64, kRowDoubles = 16 * D16, kPieces = kRowDoubles / 2;
+    __shared__ __align__(16) uint32_t order[kSelectRows][64 * kValues];
+    __shared__ __align__(16) double queries[kSelectRows * kRowDoubles];   // 16-byte piece p of row r at p ^ (r % 8)
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t pos = xcd_local_position(blockIdx.x, n_workgroups);
-    const uint32_t g = pos / row_tiles, block0 = (pos - g * row_tiles) * kRows;
+    const uint32_t g = pos / row_tiles, block0 = (pos - g * row_tiles) * kSelectRows;
     const uint32_t b = g / s.heads, h = g - b * s.heads, gk = b * s.heads_k + h / (s.heads / s.heads_k);
     const uint32_t len_q = length_of(lens, b, 0, s.tokens_q), len_k = length_of(lens, b, 1, s.tokens_k);
     const uint32_t n = (len_k + s.block_k - 1) / s.block_k;   // blocks with a key
-    const uint32_t rows = min(s.blocks_q - block0, kRows);
+    const uint32_t rows = min(s.blocks_q - block0, kSelectRows);
     const double* mq = means + ((size_t)g * s.blocks_q + block0) * dim;
     const double* mk = means + ((size_t)n_q + (size_t)gk * s.blocks_k) * dim;
+    for (uint32_t i = threadIdx.x; i < kSelectRows * kPieces; i += kSelectThreads) {
+        const uint32_t r = i / kPieces, p = i - r * kPieces;
+        select_f64x2 w = {0.0, 0.0};
+        if (r < rows && 2u * p < dim) w = *reinterpret_cast<const select_f64x2*>(mq + (size_t)r * dim + 2u * p);
+        *reinterpret_cast<select_f64x2*>(queries + r * kRowDoubles + 2u * (p ^ (r & 7u))) = w;
+    }
+    __syncthreads();
     // ---- scores
-    {
-        const uint32_t r = lane & 15u, k4 = 4u * (lane >> 4);
-        double qa[4 * D16];
-        auto load = [&](const double* row, bool there, double* to) {
+    const uint32_t r = lane & 15u, k4 = 4u * (lane >> 4);
+    for (uint32_t t = wave; 16u * t < n; t += kWaves) {
+        const double* row = mk + (size_t)(16u * t + r) * dim;
+        const bool there = 16u * t + r < n;
+        select_f64x4 acc = {0, 0, 0, 0};
+        constexpr int kChunks = D16 > 6 ? (D16 + 1) / 2 : D16;   // read at a time (128 registers hold no 8)
+#pragma unroll 1
+        for (int c0 = 0; c0 < D16; c0 += kChunks) {
+            select_f64x2 keys[2 * kChunks];
 #pragma unroll
-            for (int c = 0; c < D16; ++c) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    select_f64x2 w = {0.0, 0.0};
-                    if (there && (c < D16 - 1 || 16u * c + k4 < dim)) w = *reinterpret_cast<const select_f64x2*>(row + 16 * c + k4 + 2 * i);
-                    to[4 * c + 2 * i] = w[0];
-                    to[4 * c + 2 * i + 1] = w[1];
-                }
-            }
-        };
-        load(mq + (size_t)r * dim, r < rows, qa);
-        const uint32_t tiles = (n + 15u) / 16u;
-        double kb[4 * D16];
-        load(mk + (size_t)(16u * wave + r) * dim, 16u * wave + r < n, kb);
-        for (uint32_t t = wave; t < tiles; t += 4) {
-            double next[4 * D16];
-            load(mk + (size_t)(16u * (t + 4) + r) * dim, 16u * (t + 4) + r < n, next);
-            select_f64x4 acc = {0, 0, 0, 0};
-#pragma unroll
-            for (int i = 0; i < 4 * D16; ++i) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(qa[i], kb[i], acc, 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {   // accumulator i: row lane / 16 + 4 i, column lane % 16
-                const uint32_t row = (lane >> 4) + 4u * i, j = 16u * t + r;
-                if (row < kRows) order[row][j] = j < n ? score_order(acc[i]) : 0;
+            for (int i = 0; i < 2 * kChunks; ++i) {
+                const uint32_t c = 16u * (c0 + i / 2) + k4 + 2u * (i % 2);
+                keys[i] = select_f64x2{0.0, 0.0};
+                if (there && c < dim) keys[i] = *reinterpret_cast<const select_f64x2*>(row + c);
             }
 #pragma unroll
-            for (int i = 0; i < 4 * D16; ++i) kb[i] = next[i];
+            for (int i = 0; i < 2 * kChunks; ++i) {
+                if (D16 % kChunks && c0 + i / 2 >= D16) break;
+                const uint32_t p = 8u * (c0 + i / 2) + k4 / 2u + i % 2;
+                const select_f64x2 a = *reinterpret_cast<const select_f64x2*>(queries + r * kRowDoubles + 2u * (p ^ (r & 7u)));
+                acc = __builtin_amdgcn_mfma_f64_16x16x4f64(a[0], keys[i][0], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f64_16x16x4f64(a[1], keys[i][1], acc, 0, 0, 0);
+            }
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)   // accumulator i: row lane / 16 + 4 i, column lane % 16
+            order[(lane >> 4) + 4u * i][16u * t + r] = there ? order_of((float)acc[i]) : 0;
     }
     __syncthreads();
     // ---- the largest of every row
     const uint64_t before = (1ull << lane) - 1;
-    for (uint32_t row = wave; row < rows; row += 4) {
+    for (uint32_t row = wave; row < rows; row += kWaves) {
         const uint32_t have = (block0 + row) * s.block_q < len_q ? n : 0u;   // (no query: no blocks)
         const uint32_t want = min(top, have);
-        uint32_t high[kValues], low[kValues];   // (0, 0: no block)
+        uint32_t mine[kValues];   // (0: no block)
 #pragma unroll
-        for (int i = 0; i < kValues; ++i) {
-            const uint64_t v = 64u * i + lane < have ? order[row][64u * i + lane] : 0;
-            high[i] = (uint32_t)(v >> 32);
-            low[i] = (uint32_t)v;
-        }
-        // The want-th largest, bit by bit from the first in which the upper halves differ: is it at least as large as with this
-        // bit set?  When exactly `want` are, they are the ones; else the lower halves of those with its upper half decide.
-        uint32_t bound = 0, bound_low = 0, above = 0;
-        bool found = false;
-        if (want > 0) {
-            const uint32_t first = __builtin_amdgcn_readfirstlane(high[0]);
-            uint32_t differ = 0;
+        for (int i = 0; i < kValues; ++i) mine[i] = 64u * i + lane < have ? order[row][64u * i + lane] : 0;
+        auto at_least = [&](uint32_t bound) {
+            uint32_t count = 0;
 #pragma unroll
-            for (int i = 0; i < kValues; ++i) differ |= 64u * i + lane < have ? high[i] ^ first : 0;
+            for (int i = 0; i < kValues; ++i) count += (uint32_t)__popcll(__ballot(mine[i] >= bound));
+            return count;
+        };
+        // Where the want-th largest lies: at_least(low) >= want > at_least(high).  By halves of the numbers' range (ten steps for
+        // 1024 scores) until exactly `want` are at least `low`, or two numbers are left with none between them; then by halves of their
+        // places in the order.
+        uint32_t low = 1, high = 0, count = have;
+        if (want > 0 && want < have) {
 #pragma unroll
-            for (int d = 1; d < 64; d *= 2) differ |= __shfl_xor(differ, d);
-            differ = __builtin_amdgcn_readfirstlane(differ);
-            int bit = differ ? 31 - __builtin_clz(differ) : -1;
-            bound = bit < 0 ? first : bit == 31 ? 0u : first >> (bit + 1) << (bit + 1);
-            for (; bit >= 0 && !found; --bit) {
-                const uint32_t trial = bound | 1u << bit;
-                uint32_t count = 0;
-#pragma unroll
-                for (int i = 0; i < kValues; ++i) count += (uint32_t)__popcll(__ballot(high[i] >= trial));
-                if (count >= want) bound = trial;
-                found = count == want;
+            for (int i = 0; i < kValues; ++i) {
+                high = max(high, mine[i]);
+                low = max(low, mine[i] ? ~mine[i] : 0u);
             }
-            if (!found) {
 #pragma unroll
-                for (int i = 0; i < kValues; ++i) above += (uint32_t)__popcll(__ballot(high[i] > bound));
-                for (bit = 31; bit >= 0; --bit) {
-                    const uint32_t trial = bound_low | 1u << bit;
-                    uint32_t count = above;
-#pragma unroll
-                    for (int i = 0; i < kValues; ++i) count += (uint32_t)__popcll(__ballot(high[i] == bound && low[i] >= trial));
-                    if (count >= want) bound_low = trial;
+            for (int d = 1; d < 64; d *= 2) {
+                high = max(high, (uint32_t)__shfl_xor(high, d));
+                low = max(low, (uint32_t)__shfl_xor(low, d));
+            }
+            low = ~__builtin_amdgcn_readfirstlane(low);
+            high = __builtin_amdgcn_readfirstlane(high) + 1u;   // (a NaN's or number's place: no overflow)
+            bool numbers = true;
+            while (count != want && high - low > 1u) {
+                uint32_t trial = low + (high - low) / 2u;
+                if (numbers) {
+                    const uint32_t half = __builtin_amdgcn_readfirstlane(order_of(0.5f * number_of(low) + 0.5f * number_of(high - 1u)));
+                    numbers = half > low && half < high;   // (not for a NaN, nor between neighbours)
+                    if (numbers) trial = half;
                 }
-#pragma unroll
-                for (int i = 0; i < kValues; ++i) above += (uint32_t)__popcll(__ballot(high[i] == bound && low[i] > bound_low));
+                const uint32_t c = at_least(trial);
+                if (c >= want) {
+                    low = trial;
+                    count = c;
+                } else {
+                    high = trial;
+                }
             }
         }
-        uint32_t ties = found ? want : want - above, out = 0;   // of those at the bound, the first (found: all that are left)
+        // Those above `low` are in; of those equal to it all, or -- more than there is room for -- the best in double, ties to the
+        // lower block.
+        uint32_t ties = want - (want > 0 && count != want ? at_least(low + 1u) : 0u), out = 0;
+        const bool all_equal = count == want;
+        uint64_t bound = 0;
+        uint64_t exact[kValues];
+        if (!all_equal && want > 0) {
+            const double* x = mq + (size_t)row * dim;
+#pragma unroll
+            for (int i = 0; i < kValues; ++i) {
+                exact[i] = 0;
+                if (mine[i] != low) continue;
+                const double* y = mk + (size_t)(64u * i + lane) * dim;
+                double sum = 0.0;
+                for (uint32_t c = 0; c < dim; ++c) sum = fma(x[c], y[c], sum);
+                exact[i] = order_of(sum);
+            }
+            for (int bit = 63; bit >= 0; --bit) {
+                const uint64_t trial = bound | 1ull << bit;
+                uint32_t c = 0;
+#pragma unroll
+                for (int i = 0; i < kValues; ++i) c += (uint32_t)__popcll(__ballot(exact[i] >= trial));
+                if (c >= ties) bound = trial;
+            }
+#pragma unroll
+            for (int i = 0; i < kValues; ++i) ties -= (uint32_t)__popcll(__ballot(exact[i] > bound));
+        }
         const size_t at_row = ((size_t)g * s.blocks_q + block0 + row) * top;
         int32_t* to = chosen + at_row;
         float* to_score = scores ? scores + at_row : nullptr;
 #pragma unroll
         for (int i = 0; i < kValues; ++i) {
-            if (64u * i >= have) break;
-            const bool larger = found ? high[i] >= bound : high[i] > bound || (high[i] == bound && low[i] > bound_low);
-            const uint64_t equal = __ballot(!found && 64u * i + lane < have && high[i] == bound && low[i] == bound_low);
-            const bool taken = want > 0 && 64u * i + lane < have && (larger || (equal >> lane & 1 && (uint32_t)__popcll(equal & before) < ties));
+            if (64u * i >= have || out >= want) break;
+            bool taken = mine[i] >= low && mine[i];
+            if (!all_equal) {
+                const bool here = mine[i] == low;
+                const uint64_t equal = __ballot(here && exact[i] == bound);
+                taken = (taken && !here) || (here && (exact[i] > bound || (exact[i] == bound && (uint32_t)__popcll(equal & before) < ties)));
+                ties -= min(ties, (uint32_t)__popcll(equal));
+            }
             const uint64_t all = __ballot(taken);
             if (taken) {
                 const uint32_t at = out + (uint32_t)__popcll(all & before);
                 to[at] = (int32_t)(64u * i + lane);
-                if (to_score) to_score[at] = (float)score_of((uint64_t)high[i] << 32 | low[i]);
+                if (to_score) to_score[at] = number_of(mine[i]);
             }
             out += (uint32_t)__popcll(all);
-            ties -= min(ties, (uint32_t)__popcll(equal));
         }
         for (uint32_t at = want + lane; at < top; at += 64) {
             to[at] = -1;

@@ -127,9 +127,9 @@ int fb4_select_key_blocks(const void* q, const void* k, int64_t batch, int heads
     else if (pieces > 4) FB4_MEANS(8);
     else FB4_MEANS(4);
 #undef FB4_MEANS
-    const uint32_t rows = s.blocks_k > 1024 ? select_rows(32) : select_rows(16), row_tiles = (s.blocks_q + rows - 1) / rows;
+    const uint32_t row_tiles = (s.blocks_q + kSelectRows - 1) / kSelectRows;
     const dim3 sgrid((unsigned)(batch * heads * row_tiles));
-#define FB4_SELECT_LAUNCH(d, v) launch(select_blocks_kernel<d, v>, sgrid, dim3(256), 0, st, means, lens, blocks, scores, (uint32_t)top, (uint32_t)n_q, (uint32_t)dim, row_tiles, sgrid.x, s)
+#define FB4_SELECT_LAUNCH(d, v) launch(select_blocks_kernel<d, v>, sgrid, dim3(kSelectThreads), 0, st, means, lens, blocks, scores, (uint32_t)top, (uint32_t)n_q, (uint32_t)dim, row_tiles, sgrid.x, s)
 #define FB4_SELECT_CASE(d)                                       \
     case d:                                                      \
         if (s.blocks_k <= 128) FB4_SELECT_LAUNCH(d, 2);          \
