@@ -268,7 +268,6 @@ void select_blocks_kernel(const double* means, const int32_t* lens, int32_t* cho
 }
 
 // ------------------------------------------------------------------------------------------------ attention
-constexpr uint32_t kTileKeys = 64;
 constexpr uint32_t kAllBlocks = 0xFFFFFFFFu;   // no list (FB4_ALL_BLOCKS in 32 bits)
 
 typedef float attn_f32x2 __attribute__((ext_vector_type(2)));
@@ -278,8 +277,8 @@ typedef short attn_s16x4 __attribute__((ext_vector_type(4)));
 struct AttentionShape {
     uint32_t tokens_q, tokens_k, top;
     uint16_t heads, heads_k;
-    uint8_t block_q, block_k, pieces;   // (block sizes in units of 64 tokens; dim / 8)
-    uint8_t spare;
+    uint8_t block_q, block_k;     // in units of 64 tokens
+    uint16_t parts;               // workgroups that share a block of queries, each with a run of its list
     uint32_t blocks_q, n_workgroups;
     float scale;
 };
@@ -288,141 +287,236 @@ struct TensorStrides {
     uint32_t batch, head, token;
 };
 
+// Keys between two barriers.  Two buffers of keys and values: with 128 channels a workgroup of two wavefronts would keep others off
+// its compute unit with 64.
+constexpr int attention_keys(int pieces, int waves) { return waves == 2 && pieces > 8 ? 32 : 64; }
+
 // A workgroup of kWaves wavefronts takes one block of 32 * kWaves queries of one head; every wavefront holds 32 of them as B
-// operands and walks the listed blocks' tiles of 64 keys, which the workgroup stages in LDS.
-// D32: channels / 32, rounded up (channels beyond dim are zero).
-template <int D32, int kWaves>
-__global__ __launch_bounds__(64 * kWaves) void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t* v, uint16_t* out, float* lse,
-                                                                      const int32_t* blocks, const int32_t* lens, TensorStrides sv, TensorStrides so,
-                                                                      AttentionShape s)
+// operands and walks the listed blocks kKeys keys at a time.
+// kP: 16-byte pieces per row (dim / 8).  Keys and values go from memory straight into LDS (1 KiB per wavefront and load, lane i's 16
+// bytes at place i), the next tile's while this one's are used.  Those places are contiguous, so rows cannot be padded; instead
+// piece p of a row lies at p ^ f(row): for the keys f as in attention_scores_dma_kernel, which spreads the 16 rows that one pass of
+// an operand read takes over all 64 banks; for the values, of whose rows a pass takes four pieces of four successive ones, so
+// that these fall into different banks (16 pieces: 4 (r % 4), 8: 4 (r / 2 % 2); other lengths spread by themselves, or nearly).
+// With an odd kP the upper half of the last step of 16 channels lies past the row: its lanes read a zeroed piece.
+// The running maximum moves only when a power would pass 2^8: until then the accumulators need not be scaled, and the two
+// half-wavefronts, which hold different keys of the same query, need not meet.
+// kSplit: a part of the list; the accumulators, maximum and sum go to `out` as floats (see join_parts_kernel).
+template <int kP, int kWaves, bool kSplit>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2)))
+void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t* v, uint16_t* out, float* lse, const int32_t* blocks,
+                            const int32_t* lens, TensorStrides sv, TensorStrides so, AttentionShape s)
 {
-    constexpr int kSteps = D32 * 2;
-    constexpr uint32_t kPitch = D32 * 64 + 16;   // bytes of a row in LDS
-    __shared__ __align__(16) uint8_t lds_k[kTileKeys * kPitch], lds_v[kTileKeys * kPitch];
+    constexpr int kSteps = (kP + 1) / 2, kTiles = (kP + 3) / 4;   // of 16 channels; of 32
+    constexpr int kKeys = attention_keys(kP, kWaves), kGroups = kKeys / 32;
+    constexpr uint32_t kRowBytes = kP * 16, kBytes = kKeys * kRowBytes, kPositions = kKeys * kP, kLoads = (kPositions + 63) / 64;
+    constexpr uint32_t kG = kP % 16 == 0 ? 16 : kP % 8 == 0 ? 8 : kP % 4 == 0 ? 4 : kP % 2 == 0 ? 2 : 1;
+    // Two buffers, as two arrays: the compiler then sees that the loads into one do not touch the reads from the other.  Keys,
+    // values, 64 bytes that reads of unused channels may touch (zeros at their start).
+    __shared__ __align__(1024) uint8_t lds_a[2 * kBytes + 64];
+    __shared__ __align__(1024) uint8_t lds_b[2 * kBytes + 64];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t half = lane >> 5, col = lane & 31u;
     const uint32_t pos = xcd_local_position(blockIdx.x, s.n_workgroups);
-    const uint32_t g = pos / s.blocks_q, block = pos - g * s.blocks_q;   // g = batch * heads + head
+    const uint32_t item = kSplit ? pos / s.parts : pos, part = kSplit ? pos - item * s.parts : 0u;
+    const uint32_t g = item / s.blocks_q, block = item - g * s.blocks_q;   // g = batch * heads + head
     const uint32_t b = g / s.heads, h = g - b * s.heads, hk = h / (s.heads / s.heads_k);
     const uint32_t len_q = length_of(lens, b, 0, s.tokens_q), len_k = length_of(lens, b, 1, s.tokens_k);
-    const uint32_t dim = s.pieces * 8u, first_q = block * s.block_q * 64u;
+    const uint32_t first_q = block * s.block_q * 64u;
     if (first_q >= len_q) return;
     const uint32_t block_keys = s.block_k * 64u, blocks_k = (len_k + block_keys - 1) / block_keys;   // blocks with a key
-    const uint16_t* kg = k + (size_t)(b * s.heads_k + hk) * s.tokens_k * dim;
-    const uint16_t* vg = v + ((size_t)b * sv.batch + (size_t)hk * sv.head) * 8u;
-    const uint32_t row = first_q + wave * 32u + col;   // this lane's query
+    const uint8_t* kg = reinterpret_cast<const uint8_t*>(k) + (size_t)(b * s.heads_k + hk) * s.tokens_k * kRowBytes;
+    const uint8_t* vg = reinterpret_cast<const uint8_t*>(v) + ((size_t)b * sv.batch + (size_t)hk * sv.head) * 16u;
+    const uint32_t end_q = min(len_q, first_q + s.block_q * 64u);
+    const uint32_t row = first_q + wave * 32u + col;                 // this lane's query
+    const bool works = first_q + wave * 32u < end_q;                 // (a wavefront without a query helps to load)
+
+    // ---- the tiles: entries of the list, and of each the tiles with a key
+    const bool all = s.top == kAllBlocks;
+    const int32_t* list = blocks + (size_t)item * s.top;
+    const uint32_t n_entries = all ? blocks_k : s.top;
+    uint32_t entry = kSplit ? (uint32_t)((uint64_t)n_entries * part / s.parts) : 0u;
+    const uint32_t last_entry = kSplit ? (uint32_t)((uint64_t)n_entries * (part + 1) / s.parts) : n_entries;
+    uint32_t key0 = 0, end = 0;   // the next tile's first key, the end of its block's keys
+    auto seek = [&]() {           // to the next entry with a key; false: there is none
+        for (; entry < last_entry; ++entry) {
+            const uint32_t which = all ? entry : (uint32_t)list[entry];
+            if (which < blocks_k) {   // (a negative one is not either)
+                key0 = __builtin_amdgcn_readfirstlane(which * block_keys);
+                end = min(key0 + block_keys, len_k);
+                ++entry;
+                return true;
+            }
+        }
+        return false;
+    };
+    bool more = seek();
+
+    auto fetch = [&](uint8_t* buffer) {   // the tile at key0, and on to the next
+        const uint8_t* kt = kg + (size_t)key0 * kRowBytes;
+        const uint8_t* vt = vg + (size_t)key0 * sv.token * 16u;
+        const uint32_t valid = min(end - key0, (uint32_t)kKeys);
+        uint32_t l = lane;
+        asm volatile("" : "+v"(l));   // (opaque: else every load's offset is kept in a register of its own)
+#pragma unroll
+        for (uint32_t i0 = 0; i0 < kLoads; i0 += kWaves) {
+            const uint32_t i = i0 + wave;
+            if (i0 + kWaves > kLoads && i >= kLoads) break;
+            const uint32_t j = 64u * i + l, r = j / kP, p = j - r * kP;
+            const uint32_t pk = p ^ ((r / (16u / kG)) & (kG - 1u)), pv = p ^ (kP == 16 ? 4u * (r & 3u) : kP == 8 ? 4u * ((r >> 1) & 1u) : 0u);
+            const uint32_t at = __builtin_amdgcn_readfirstlane(i * 1024u);
+            if (r < valid) {   // (a lane that takes no part leaves its 16 bytes alone)
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(kt + r * kRowBytes + pk * 16u),
+                                                 (__attribute__((address_space(3))) void*)(buffer + at), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(vt + (size_t)r * sv.token * 16u + pv * 16u),
+                                                 (__attribute__((address_space(3))) void*)(buffer + kBytes + at), 16, 0, 0);
+            } else if (j < kPositions) {
+                // values behind the last key: zeros, which their weights of 0 leave zeros (the keys' scores are replaced)
+                *reinterpret_cast<uint4*>(buffer + kBytes + j * 16u) = make_uint4(0, 0, 0, 0);
+            }
+        }
+        key0 += kKeys;
+        if (key0 >= end) more = seek();
+    };
+
+    // ---- this wavefront's queries as B operands
     mfma_bf16x8 qf[kSteps];
     {
-        const uint16_t* from = q + ((size_t)g * s.tokens_q + min(row, s.tokens_q - 1u)) * dim;
+        const uint16_t* from = q + ((size_t)g * s.tokens_q + min(row, s.tokens_q - 1u)) * (kP * 8);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            const uint32_t c = 16u * i + 8u * half;
             uint4 w = make_uint4(0, 0, 0, 0);
-            if (c < dim) w = *reinterpret_cast<const uint4*>(from + c);
+            if (!(kP % 2 && i == kSteps - 1) || half == 0) w = *reinterpret_cast<const uint4*>(from + 16 * i + 8 * half);
             qf[i] = __builtin_bit_cast(mfma_bf16x8, w);
         }
     }
     const float factor = s.scale * 1.44269504088896340736f;   // to powers of two
-    mfma_f32x16 o[D32];
+    mfma_f32x16 o[kTiles];
 #pragma unroll
-    for (int d = 0; d < D32; ++d) o[d] = mfma_f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-    float most = -__builtin_inff(), sum = 0.0f;   // of this lane's query: largest product so far, sum over this lane's keys
-    const int32_t* list = blocks + (size_t)pos * s.top;
-    const bool all = s.top == kAllBlocks;
-    const uint32_t entries = all ? blocks_k : s.top;
-    for (uint32_t e = 0; e < entries; ++e) {
-        const uint32_t which = all ? e : (uint32_t)list[e];
-        if (which >= blocks_k) continue;   // (a negative one too)
-        const uint32_t end = min((which + 1) * block_keys, len_k);
-        for (uint32_t key0 = which * block_keys; key0 < end; key0 += kTileKeys) {
-            __syncthreads();
-            for (uint32_t i = threadIdx.x; i < kTileKeys * D32 * 4; i += 64 * kWaves) {
-                const uint32_t r = i / (D32 * 4), p = i - r * (D32 * 4);
-                uint4 kw = make_uint4(0, 0, 0, 0), vw = make_uint4(0, 0, 0, 0);
-                if (key0 + r < end && p < s.pieces) {
-                    kw = *reinterpret_cast<const uint4*>(kg + (size_t)(key0 + r) * dim + 8u * p);
-                    vw = *reinterpret_cast<const uint4*>(vg + ((size_t)(key0 + r) * sv.token + p) * 8u);
-                }
-                *reinterpret_cast<uint4*>(lds_k + r * kPitch + 16u * p) = kw;
-                *reinterpret_cast<uint4*>(lds_v + r * kPitch + 16u * p) = vw;
+    for (int d = 0; d < kTiles; ++d) o[d] = mfma_f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+    float most = -__builtin_inff(), sum = 0.0f;   // of this lane's query: what is taken off its products; sum over this lane's keys
+
+    // LDS offsets: the keys' operand, row lane % 32 of 32, piece 2 step + lane / 32; the values', 8 bytes of row (lane % 16) / 4
+    const uint32_t k_row = col * kRowBytes, k_swz = (col / (16u / kG)) & (kG - 1u);
+    const uint32_t v_r = 4u * half + (lane & 15u) / 4u;
+    const uint32_t v_swz = kP == 16 ? 4u * (v_r & 3u) : kP == 8 ? 4u * ((v_r >> 1) & 1u) : 0u;   // (8 and 16 rows further the same)
+    const uint32_t v_piece = 2u * ((lane >> 4) & 1u) + ((lane & 3u) >> 1), v_at = v_r * kRowBytes + 8u * (lane & 1u);
+
+    auto compute = [&](const uint8_t* buffer, uint32_t n) {   // n: keys of the tile
+        if (!works) return;
+        mfma_f32x16 sc[kGroups];
+#pragma unroll
+        for (int j = 0; j < kGroups; ++j) {
+            sc[j] = mfma_f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const uint32_t at = 32u * j * kRowBytes + k_row + (((2u * i + half) ^ k_swz) << 4);
+                const uint4 a = *reinterpret_cast<const uint4*>(buffer + ((kP % 2 && i == kSteps - 1 && half) ? 2u * kBytes : at));
+                sc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(mfma_bf16x8, a), qf[i], sc[j], 0, 0, 0);
             }
-            __syncthreads();
-            mfma_f32x16 sc[2];
+        }
+        if (n < (uint32_t)kKeys) {   // (a sequence's last tile)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                sc[j] = mfma_f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+            for (int j = 0; j < kGroups; ++j) {
 #pragma unroll
-                for (int i = 0; i < kSteps; ++i) {
-                    const uint4 a = *reinterpret_cast<const uint4*>(lds_k + (32u * j + col) * kPitch + 32u * i + 16u * half);
-                    sc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(mfma_bf16x8, a), qf[i], sc[j], 0, 0, 0);
+                for (int i = 0; i < 16; ++i) {
+                    if (32u * j + 8u * (i / 4) + 4u * half + i % 4 >= n) sc[j][i] = -__builtin_inff();
                 }
             }
-            if (key0 + kTileKeys > end) {   // (the sequence's last tile)
+        }
+        float larger = sc[0][0];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < kGroups; ++j) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        if (key0 + 32u * j + 8u * (i / 4) + 4u * half + i % 4 >= end) sc[j][i] = -__builtin_inff();
-                    }
-                }
-            }
-            float larger = most;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) larger = fmaxf(larger, sc[j][i]);
-            }
+            for (int i = 0; i < 16; ++i) larger = fmaxf(larger, sc[j][i]);
+        }
+        if (__any((larger - most) * factor > 8.0f)) {
+            larger = fmaxf(larger, most);
             larger = fmaxf(larger, __shfl_xor(larger, 32));
-            // (nothing but -Inf so far: 0 in the place of the maximum, so that the powers are 0.  The powers are of differences: a
-            // product with the maximum taken off by a fused multiply-add keeps the product's rounding, which is no small
-            // number for large scores)
-            const float base = larger == -__builtin_inff() ? 0.0f : larger;
+            // (of the difference: 1 where the maximum stays)
             const float shrink = most == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((most - larger) * factor);
             most = larger;
-            float tile_sum = 0.0f;   // (added to the row's at the end: one rounding per tile and not per key)
+            sum *= shrink;
 #pragma unroll
-            for (int d = 0; d < D32; ++d) {
+            for (int d = 0; d < kTiles; ++d) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[d][i] *= shrink;
             }
+        }
+        const float base = most == -__builtin_inff() ? 0.0f : most;   // (nothing but -Inf so far: the powers are to be 0)
+        float tile_sum = 0.0f;   // (one rounding of the row's sum per tile and not per key)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < kGroups; ++j) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    sc[j][i] = __builtin_amdgcn_exp2f((sc[j][i] - base) * factor);
-                    tile_sum += sc[j][i];
-                }
+            for (int i = 0; i < 16; ++i) {
+                // (of a difference: a fused product less the maximum's would keep that product's rounding, large for large scores)
+                sc[j][i] = __builtin_amdgcn_exp2f((sc[j][i] - base) * factor);
+                tile_sum += sc[j][i];
+            }
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    // P in bf16 for the matrix cores, the sum from the unrounded values: a rounding is half a bf16 step of a
-                    // weight, as the output's own is of the result
-                    uint32_t w[4];
+            for (int i = 0; i < 2; ++i) {
+                // P in bf16 for the matrix cores, the sum from the unrounded values: a rounding is half a bf16 step of a
+                // weight, as the output's own is of the result
+                uint32_t w[4];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        w[c] = __builtin_bit_cast(uint32_t, __builtin_convertvector((attn_f32x2{sc[j][8 * i + 2 * c], sc[j][8 * i + 2 * c + 1]}), attn_bf16x2));
-                    const mfma_bf16x8 p = __builtin_bit_cast(mfma_bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+                for (int c = 0; c < 4; ++c)
+                    w[c] = __builtin_bit_cast(uint32_t, __builtin_convertvector((attn_f32x2{sc[j][8 * i + 2 * c], sc[j][8 * i + 2 * c + 1]}), attn_bf16x2));
+                const mfma_bf16x8 p = __builtin_bit_cast(mfma_bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
 #pragma unroll
-                    for (int d = 0; d < D32; ++d) {
-                        // lane t of 16 reads 8 bytes of row t / 4 and gets column t of the four rows
-                        const uint32_t r = 32u * j + 16u * i + 4u * half + (lane & 15u) / 4u, c = 32u * d + 16u * ((lane >> 4) & 1u) + 4u * (lane & 3u);
-                        typedef __attribute__((address_space(3))) attn_s16x4* lds_s16x4;
-                        const attn_s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(lds_v + r * kPitch + 2u * c));
-                        const attn_s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(lds_v + (r + 8u) * kPitch + 2u * c));
-                        const uint4 a = make_uint4(__builtin_bit_cast(uint2, v0).x, __builtin_bit_cast(uint2, v0).y, __builtin_bit_cast(uint2, v1).x,
-                                                   __builtin_bit_cast(uint2, v1).y);
-                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(mfma_bf16x8, a), p, o[d], 0, 0, 0);
-                    }
+                for (int d = 0; d < kTiles; ++d) {
+                    // lane t of 16 reads 8 bytes of row t / 4 and gets column t of the four rows.  (Channels past the row: what lies
+                    // behind, in accumulators that nobody reads)
+                    typedef __attribute__((address_space(3))) attn_s16x4* lds_s16x4;
+                    const uint8_t* from = buffer + kBytes + (32u * j + 16u * i) * kRowBytes + v_at + (((4u * d + v_piece) ^ v_swz) << 4);
+                    const uint2 v0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(from)));
+                    const uint2 v1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(from + 8u * kRowBytes)));
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(mfma_bf16x8, make_uint4(v0.x, v0.y, v1.x, v1.y)), p, o[d], 0, 0, 0);
                 }
             }
-            sum = fmaf(sum, shrink, tile_sum);
         }
+        sum += tile_sum;
+    };
+
+    if (kP % 2 && threadIdx.x < 8) reinterpret_cast<uint32_t*>((threadIdx.x & 4u ? lds_b : lds_a) + 2 * kBytes)[threadIdx.x & 3u] = 0;   // the zeroed pieces
+    uint32_t n_a = 0, n_b = 0;   // keys of the tiles in the buffers, 0: none
+    if (more) {
+        n_a = min(end - key0, (uint32_t)kKeys);
+        fetch(lds_a);
+    }
+    while (n_a) {
+        __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wavefront's part of the tile is in LDS
+        __syncthreads();                      // ... and everyone's; the other buffer is free
+        n_b = more ? min(end - key0, (uint32_t)kKeys) : 0u;
+        if (more) fetch(lds_b);
+        compute(lds_a, n_a);
+        if (!n_b) break;
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+        __syncthreads();
+        n_a = more ? min(end - key0, (uint32_t)kKeys) : 0u;
+        if (more) fetch(lds_a);
+        compute(lds_b, n_b);
     }
     sum += __shfl_xor(sum, 32);
-    if (row >= min(len_q, first_q + s.block_q * 64u)) return;
+    if (row >= end_q) return;
+    const size_t at_row = (size_t)g * s.tokens_q + row;
+    if (kSplit) {
+        const size_t n_rows = (size_t)(s.n_workgroups / s.parts / s.blocks_q) * s.tokens_q;
+        float* to = reinterpret_cast<float*>(out) + (part * n_rows + at_row) * (kP * 8);
+#pragma unroll
+        for (int d = 0; d < kTiles; ++d) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t c = 32u * d + 8u * i + 4u * half;
+                if (c < kP * 8u) *reinterpret_cast<float4*>(to + c) = make_float4(o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]);
+            }
+        }
+        if (half == 0) *reinterpret_cast<float2*>(reinterpret_cast<float*>(out) + s.parts * n_rows * (kP * 8) + 2 * (part * n_rows + at_row)) = make_float2(most, sum);
+        return;
+    }
     const float inverse = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;   // (a NaN stays; no key: zeros)
     uint16_t* to = out + ((size_t)b * so.batch + (size_t)h * so.head + (size_t)row * so.token) * 8u;
 #pragma unroll
-    for (int d = 0; d < D32; ++d) {
+    for (int d = 0; d < kTiles; ++d) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t c = 32u * d + 8u * i + 4u * half;
@@ -430,11 +524,42 @@ __global__ __launch_bounds__(64 * kWaves) void block_attention_kernel(const uint
 #pragma unroll
             for (int x = 0; x < 2; ++x)
                 w[x] = __builtin_bit_cast(uint32_t, __builtin_convertvector((attn_f32x2{o[d][4 * i + 2 * x] * inverse, o[d][4 * i + 2 * x + 1] * inverse}), attn_bf16x2));
-            if (c < dim) *reinterpret_cast<uint2*>(to + c) = make_uint2(w[0], w[1]);
+            if (c < kP * 8u) *reinterpret_cast<uint2*>(to + c) = make_uint2(w[0], w[1]);
         }
     }
-    if (lse && half == 0)
-        lse[(size_t)g * s.tokens_q + row] = sum == 0.0f ? -__builtin_inff() : most * s.scale + 0.69314718055994530942f * __builtin_amdgcn_logf(sum);
+    if (lse && half == 0) lse[at_row] = sum == 0.0f ? -__builtin_inff() : most * s.scale + 0.69314718055994530942f * __builtin_amdgcn_logf(sum);
+}
+
+// The parts of a row's list meet: accumulators and sums relative to the parts' own maxima.  Workspace: float [parts][rows][dim], then
+// {maximum, sum} [parts][rows].  A wavefront per row.
+__global__ __launch_bounds__(256) void join_parts_kernel(const float* workspace, const int32_t* lens, uint16_t* out, float* lse, TensorStrides so,
+                                                         uint32_t parts, uint32_t n_rows, uint32_t tokens_q, uint32_t heads, uint32_t dim, float scale)
+{
+    const uint32_t lane = threadIdx.x & 63, at = blockIdx.x * 4u + (threadIdx.x >> 6);
+    if (at >= n_rows) return;
+    const uint32_t g = at / tokens_q, row = at - g * tokens_q, b = g / heads, h = g - b * heads;
+    if (row >= length_of(lens, b, 0, tokens_q)) return;
+    const float2* state = reinterpret_cast<const float2*>(workspace + (size_t)parts * n_rows * dim);
+    float most = -__builtin_inff();
+    for (uint32_t p = 0; p < parts; ++p) most = fmaxf(most, state[(size_t)p * n_rows + at].x);
+    const float base = most == -__builtin_inff() ? 0.0f : most;
+    float sum = 0.0f, o[2] = {0.0f, 0.0f};
+    for (uint32_t p = 0; p < parts; ++p) {
+        const float2 st = state[(size_t)p * n_rows + at];
+        const float w = __builtin_amdgcn_exp2f((st.x - base) * (scale * 1.44269504088896340736f));
+        sum = fmaf(st.y, w, sum);
+#pragma unroll
+        for (uint32_t i = 0; i < 2; ++i) {
+            if (64u * i + lane < dim) o[i] = fmaf(workspace[((size_t)p * n_rows + at) * dim + 64u * i + lane], w, o[i]);
+        }
+    }
+    const float inverse = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
+    uint16_t* to = out + ((size_t)b * so.batch + (size_t)h * so.head + (size_t)row * so.token) * 8u;
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) {
+        if (64u * i + lane < dim) reinterpret_cast<__bf16*>(to)[64u * i + lane] = (__bf16)(o[i] * inverse);
+    }
+    if (lse && lane == 0) lse[at] = sum == 0.0f ? -__builtin_inff() : most * scale + 0.69314718055994530942f * __builtin_amdgcn_logf(sum);
 }
 
 }  // namespace fb4

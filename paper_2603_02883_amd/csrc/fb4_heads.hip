@@ -37,6 +37,16 @@ int check_blocks(int64_t batch, int heads, int heads_k, int64_t tokens_q, int64_
     return FB4_OK;
 }
 
+// Parts of a block of queries' list, each with a workgroup of its own, while there are fewer blocks than the card holds workgroups;
+// at least four tiles of 64 keys to a part, which is what joining the parts costs or so.
+int64_t attention_parts(int64_t n, int64_t top, const BlockShape& s)
+{
+    const int64_t entries = top == FB4_ALL_BLOCKS ? s.blocks_k : top;
+    const int64_t slots = s.block_q == 64 ? 1024 : 512;
+    if (n < 1 || n * 2 > slots) return 1;
+    return std::max<int64_t>(1, std::min(slots / n, entries * (s.block_k / 64) / 4));
+}
+
 }  // namespace
 
 extern "C" {
@@ -151,7 +161,8 @@ size_t fb4_block_attention_workspace(int64_t batch, int heads, int heads_k, int6
 {
     BlockShape s;
     if (check_blocks(batch, heads, heads_k, tokens_q, tokens_k, dim, block_q, block_k, &s) != FB4_OK || top < FB4_ALL_BLOCKS) return 0;
-    return 0;
+    const int64_t parts = attention_parts(batch * heads * s.blocks_q, top, s);
+    return parts > 1 ? (size_t)(parts * batch * heads * tokens_q * (dim + 2)) * sizeof(float) : 0;
 }
 
 int fb4_block_attention(const void* q, const void* k, const void* v, const int64_t* v_strides, int64_t batch, int heads, int heads_k, int64_t tokens_q,
@@ -176,20 +187,31 @@ int fb4_block_attention(const void* q, const void* k, const void* v, const int64
         return FB4_ERR_UNSUPPORTED;
     const int64_t n = batch * heads * s.blocks_q;
     if (n > kMaxWorkgroups || top > kMaxTokens) return FB4_ERR_UNSUPPORTED;
+    const int64_t parts = attention_parts(n, top, s);
     const AttentionShape a = {s.tokens_q, s.tokens_k, (uint32_t)top, s.heads, s.heads_k, (uint8_t)(block_q / 64), (uint8_t)(block_k / 64),
-                              (uint8_t)(dim / 8), 0, s.blocks_q, (uint32_t)n, scale};
-    const dim3 grid((unsigned)n);
-#define FB4_ATTENTION_LAUNCH(d, w) launch(block_attention_kernel<d, w>, grid, dim3(64 * w), 0, static_cast<hipStream_t>(stream), static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), static_cast<uint16_t*>(out), lse, blocks, lens, sv, so, a)
-#define FB4_ATTENTION_CASE(d)                              \
-    case d:                                                \
-        if (block_q == 64) FB4_ATTENTION_LAUNCH(d, 2);     \
-        else FB4_ATTENTION_LAUNCH(d, 4);                   \
+                              (uint16_t)parts, s.blocks_q, (uint32_t)(n * parts), scale};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const dim3 grid((unsigned)(n * parts));
+#define FB4_ATTENTION_LAUNCH(p, w, split) launch(block_attention_kernel<p, w, split>, grid, dim3(64 * w), 0, st, static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), static_cast<uint16_t*>(split ? workspace : out), lse, blocks, lens, sv, so, a)
+#define FB4_ATTENTION_CASE(p)                                              \
+    case p:                                                                \
+        if (block_q == 64 && parts > 1) FB4_ATTENTION_LAUNCH(p, 2, true);  \
+        else if (block_q == 64) FB4_ATTENTION_LAUNCH(p, 2, false);         \
+        else if (parts > 1) FB4_ATTENTION_LAUNCH(p, 4, true);              \
+        else FB4_ATTENTION_LAUNCH(p, 4, false);                            \
         break;
-    switch ((dim + 31) / 32) {
-        FB4_ATTENTION_CASE(1) FB4_ATTENTION_CASE(2) FB4_ATTENTION_CASE(3) FB4_ATTENTION_CASE(4)
+    switch (dim / 8) {
+        FB4_ATTENTION_CASE(1) FB4_ATTENTION_CASE(2) FB4_ATTENTION_CASE(3) FB4_ATTENTION_CASE(4) FB4_ATTENTION_CASE(5) FB4_ATTENTION_CASE(6)
+        FB4_ATTENTION_CASE(7) FB4_ATTENTION_CASE(8) FB4_ATTENTION_CASE(9) FB4_ATTENTION_CASE(10) FB4_ATTENTION_CASE(11) FB4_ATTENTION_CASE(12)
+        FB4_ATTENTION_CASE(13) FB4_ATTENTION_CASE(14) FB4_ATTENTION_CASE(15) FB4_ATTENTION_CASE(16)
     }
 #undef FB4_ATTENTION_CASE
 #undef FB4_ATTENTION_LAUNCH
+    if (parts > 1) {
+        const int64_t rows = batch * heads * tokens_q;   // (at most 512 blocks of 128)
+        launch(join_parts_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, static_cast<const float*>(workspace), lens, static_cast<uint16_t*>(out), lse,
+               so, (uint32_t)parts, (uint32_t)rows, s.tokens_q, (uint32_t)heads, (uint32_t)dim, scale);
+    }
     return hipGetLastError() == hipSuccess ? FB4_OK : FB4_ERR_HIP;
 }
 
