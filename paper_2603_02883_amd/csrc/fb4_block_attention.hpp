@@ -531,35 +531,51 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
 }
 
 // The parts of a row's list meet: accumulators and sums relative to the parts' own maxima.  Workspace: float [parts][rows][dim], then
-// {maximum, sum} [parts][rows].  A wavefront per row.
+// {maximum, sum} [parts][rows].  A workgroup per row: eight parts at a time, four channels to a thread, so that a row waits for few
+// reads one behind the other (48 rows x 21 parts x 128 channels 20.8 us with a wavefront that walks over the parts).
 __global__ __launch_bounds__(256) void join_parts_kernel(const float* workspace, const int32_t* lens, uint16_t* out, float* lse, TensorStrides so,
                                                          uint32_t parts, uint32_t n_rows, uint32_t tokens_q, uint32_t heads, uint32_t dim, float scale)
 {
-    const uint32_t lane = threadIdx.x & 63, at = blockIdx.x * 4u + (threadIdx.x >> 6);
-    if (at >= n_rows) return;
+    __shared__ float4 meet[8][32];
+    const uint32_t lane = threadIdx.x & 63, at = blockIdx.x, c = 4u * (threadIdx.x & 31u), sub = threadIdx.x >> 5;
     const uint32_t g = at / tokens_q, row = at - g * tokens_q, b = g / heads, h = g - b * heads;
     if (row >= length_of(lens, b, 0, tokens_q)) return;
-    const float2* state = reinterpret_cast<const float2*>(workspace + (size_t)parts * n_rows * dim);
-    float most = -__builtin_inff();
-    for (uint32_t p = 0; p < parts; ++p) most = fmaxf(most, state[(size_t)p * n_rows + at].x);
-    const float base = most == -__builtin_inff() ? 0.0f : most;
-    float sum = 0.0f, o[2] = {0.0f, 0.0f};
-    for (uint32_t p = 0; p < parts; ++p) {
-        const float2 st = state[(size_t)p * n_rows + at];
-        const float w = __builtin_amdgcn_exp2f((st.x - base) * (scale * 1.44269504088896340736f));
-        sum = fmaf(st.y, w, sum);
+    const float2* state = reinterpret_cast<const float2*>(workspace + (size_t)parts * n_rows * dim) + at;
+    const float factor = scale * 1.44269504088896340736f;
+    float most = -__builtin_inff(), sum = 0.0f;
+    for (uint32_t p = lane; p < parts; p += 64) most = fmaxf(most, state[(size_t)p * n_rows].x);
 #pragma unroll
-        for (uint32_t i = 0; i < 2; ++i) {
-            if (64u * i + lane < dim) o[i] = fmaf(workspace[((size_t)p * n_rows + at) * dim + 64u * i + lane], w, o[i]);
+    for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+    const float base = most == -__builtin_inff() ? 0.0f : most;
+    for (uint32_t p = lane; p < parts; p += 64) {
+        const float2 st = state[(size_t)p * n_rows];
+        sum = fmaf(st.y, __builtin_amdgcn_exp2f((st.x - base) * factor), sum);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (c < dim) {
+#pragma unroll 4
+        for (uint32_t p = sub; p < parts; p += 8) {
+            const float w = __builtin_amdgcn_exp2f((state[(size_t)p * n_rows].x - base) * factor);
+            const float4 x = *reinterpret_cast<const float4*>(workspace + ((size_t)p * n_rows + at) * dim + c);
+            o = make_float4(fmaf(x.x, w, o.x), fmaf(x.y, w, o.y), fmaf(x.z, w, o.z), fmaf(x.w, w, o.w));
         }
+    }
+    meet[sub][threadIdx.x & 31u] = o;
+    __syncthreads();
+    if (sub > 0) return;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+        const float4 x = meet[i][threadIdx.x];
+        o = make_float4(o.x + x.x, o.y + x.y, o.z + x.z, o.w + x.w);
     }
     const float inverse = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
     uint16_t* to = out + ((size_t)b * so.batch + (size_t)h * so.head + (size_t)row * so.token) * 8u;
-#pragma unroll
-    for (uint32_t i = 0; i < 2; ++i) {
-        if (64u * i + lane < dim) reinterpret_cast<__bf16*>(to)[64u * i + lane] = (__bf16)(o[i] * inverse);
-    }
-    if (lse && lane == 0) lse[at] = sum == 0.0f ? -__builtin_inff() : most * scale + 0.69314718055994530942f * __builtin_amdgcn_logf(sum);
+    const attn_bf16x2 lo = __builtin_convertvector((attn_f32x2{o.x * inverse, o.y * inverse}), attn_bf16x2);
+    const attn_bf16x2 hi = __builtin_convertvector((attn_f32x2{o.z * inverse, o.w * inverse}), attn_bf16x2);
+    if (c < dim) *reinterpret_cast<uint2*>(to + c) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+    if (lse && threadIdx.x == 0) lse[at] = sum == 0.0f ? -__builtin_inff() : most * scale + 0.69314718055994530942f * __builtin_amdgcn_logf(sum);
 }
 
 }  // namespace fb4

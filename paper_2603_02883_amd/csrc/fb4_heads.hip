@@ -209,7 +209,7 @@ int fb4_block_attention(const void* q, const void* k, const void* v, const int64
 #undef FB4_ATTENTION_LAUNCH
     if (parts > 1) {
         const int64_t rows = batch * heads * tokens_q;   // (at most 512 blocks of 128)
-        launch(join_parts_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, static_cast<const float*>(workspace), lens, static_cast<uint16_t*>(out), lse,
+        launch(join_parts_kernel, dim3((unsigned)rows), dim3(256), 0, st, static_cast<const float*>(workspace), lens, static_cast<uint16_t*>(out), lse,
                so, (uint32_t)parts, (uint32_t)rows, s.tokens_q, (uint32_t)heads, (uint32_t)dim, scale);
     }
     return hipGetLastError() == hipSuccess ? FB4_OK : FB4_ERR_HIP;
