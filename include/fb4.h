@@ -554,7 +554,8 @@ int fb4_select_key_blocks(const void* q, const void* k, int64_t batch, int heads
  * its weights rounded to bf16 for the second product, the output rounded once.
  *   q, k, heads, heads_k, dim, lens, block_q, block_k  as in fb4_select_key_blocks
  *   v       device, bf16 [batch][heads_k][tokens_k][dim] by v_strides: rows
- *           16-byte aligned, the channels contiguous
+ *           16-byte aligned, the channels contiguous, the token stride below 2^25
+ *           (FB4_ERR_UNSUPPORTED otherwise)
  *   blocks  device, int32 [batch][heads][ceil(tokens_q / block_q)][top]; in any
  *           order; an entry without a key (negative, or behind the sequence's last
  *           block) is skipped, one listed twice counts twice

@@ -287,21 +287,33 @@ struct TensorStrides {
     uint32_t batch, head, token;
 };
 
-// Keys between two barriers.  Two buffers of keys and values: with 128 channels a workgroup of two wavefronts would keep others off
+#define FB4_INLINE __attribute__((always_inline))   // (a lambda that is not inlined keeps what it captures in memory)
+
+// Keys between two barriers.  Two buffers of keys and of values: a workgroup of two wavefronts with long rows would keep others off
 // its compute unit with 64.
-constexpr int attention_keys(int pieces, int waves) { return waves == 2 && pieces > 8 ? 32 : 64; }
+constexpr int attention_keys(int pieces, int waves) { return waves == 2 && pieces > 9 ? 32 : 64; }
 
 // A workgroup of kWaves wavefronts takes one block of 32 * kWaves queries of one head; every wavefront holds 32 of them as B
-// operands and walks the listed blocks kKeys keys at a time.
+// operands and walks the listed blocks' keys in groups of 32.
+//
+// The walk overlaps: while the vector ALU turns group i's products into weights, the matrix cores form P V of group i - 1 and then
+// Q K of group i + 1, so that a wavefront alone keeps both busy (16 MFMAs of 32 cycles per group with 128 channels, about 70
+// instructions of 4).  Keys are therefore wanted a group early and values a group late, and their buffers change over at
+// different times: between the barriers before the last groups of tile t and of t + 1, the keys of t + 2 and the values of t + 1
+// (tiles of one group: of t) come in.
+//
 // kP: 16-byte pieces per row (dim / 8).  Keys and values go from memory straight into LDS (1 KiB per wavefront and load, lane i's 16
-// bytes at place i), the next tile's while this one's are used.  Those places are contiguous, so rows cannot be padded; instead
-// piece p of a row lies at p ^ f(row): for the keys f as in attention_scores_dma_kernel, which spreads the 16 rows that one pass of
-// an operand read takes over all 64 banks; for the values, of whose rows a pass takes four pieces of four successive ones, so
-// that these fall into different banks (16 pieces: 4 (r % 4), 8: 4 (r / 2 % 2); other lengths spread by themselves, or nearly).
-// With an odd kP the upper half of the last step of 16 channels lies past the row: its lanes read a zeroed piece.
-// The running maximum moves only when a power would pass 2^8: until then the accumulators need not be scaled, and the two
-// half-wavefronts, which hold different keys of the same query, need not meet.
-// kSplit: a part of the list; the accumulators, maximum and sum go to `out` as floats (see join_parts_kernel).
+// bytes at place i).  Those places are contiguous, so rows cannot be padded; instead piece p of a row lies at p ^ f(row): for the
+// keys f as in attention_scores_dma_kernel, which spreads the 16 rows that one pass of an operand read takes over all 64 banks; for
+// the values, of whose rows a pass takes four pieces of four successive ones, so that these fall into different banks (16 pieces:
+// 4 (r % 4), 8: 4 (r / 2 % 2); other lengths spread by themselves, or nearly).  With an odd kP the upper half of the last step of 16
+// channels lies past the row: its lanes read a zeroed piece.
+//
+// Weights are exp2(S c - m), c = scale log2 e, m a reference that moves only when a power would pass 2^8: until then the accumulators need
+// not be scaled, and the two half-wavefronts, which hold different keys of the same query, need not meet.  A fused multiply-add
+// takes m off the exact product, so m's own rounding is one factor in all weights and in their sum; beyond |m| = 2^20 that factor could
+// itself be no small number, and the wavefront goes on with exp2((S - max) c).
+// kSplit: a part of the list; the accumulators, reference and sum go to `out` as floats (see join_parts_kernel).
 template <int kP, int kWaves, bool kSplit>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2)))
 void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t* v, uint16_t* out, float* lse, const int32_t* blocks,
@@ -310,18 +322,20 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
     constexpr int kSteps = (kP + 1) / 2, kTiles = (kP + 3) / 4;   // of 16 channels; of 32
     constexpr int kKeys = attention_keys(kP, kWaves), kGroups = kKeys / 32;
     constexpr uint32_t kRowBytes = kP * 16, kBytes = kKeys * kRowBytes, kPositions = kKeys * kP, kLoads = (kPositions + 63) / 64;
+    constexpr int kMine = (kLoads + kWaves - 1) / kWaves;         // of a wavefront, at most
     constexpr uint32_t kG = kP % 16 == 0 ? 16 : kP % 8 == 0 ? 8 : kP % 4 == 0 ? 4 : kP % 2 == 0 ? 2 : 1;
-    // Two buffers, as two arrays: the compiler then sees that the loads into one do not touch the reads from the other.  Keys,
-    // values, 64 bytes that reads of unused channels may touch (zeros at their start).
-    __shared__ __align__(1024) uint8_t lds_a[2 * kBytes + 64];
-    __shared__ __align__(1024) uint8_t lds_b[2 * kBytes + 64];
+    // Each buffer an array of its own: the compiler then sees that the loads into one do not touch the reads from another.  (64 bytes
+    // more: zeros for the keys, what reads of unused channels may touch for the values)
+    __shared__ __align__(1024) uint8_t lds_k0[kBytes + 64], lds_k1[kBytes + 64], lds_v0[kBytes + 64], lds_v1[kBytes + 64];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t half = lane >> 5, col = lane & 31u;
     const uint32_t pos = xcd_local_position(blockIdx.x, s.n_workgroups);
-    const uint32_t item = kSplit ? pos / s.parts : pos, part = kSplit ? pos - item * s.parts : 0u;
-    const uint32_t g = item / s.blocks_q, block = item - g * s.blocks_q;   // g = batch * heads + head
-    const uint32_t b = g / s.heads, h = g - b * s.heads, hk = h / (s.heads / s.heads_k);
-    const uint32_t len_q = length_of(lens, b, 0, s.tokens_q), len_k = length_of(lens, b, 1, s.tokens_k);
+    // (divisions run in the vector ALU: the addresses made of their results stay in scalar registers so)
+    auto scalar = [](uint32_t x) FB4_INLINE { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
+    const uint32_t item = kSplit ? scalar(pos / s.parts) : pos, part = kSplit ? pos - item * s.parts : 0u;
+    const uint32_t g = scalar(item / s.blocks_q), block = item - g * s.blocks_q;   // g = batch * heads + head
+    const uint32_t b = scalar(g / s.heads), h = g - b * s.heads, hk = scalar(h / (s.heads / s.heads_k));
+    const uint32_t len_q = scalar(length_of(lens, b, 0, s.tokens_q)), len_k = scalar(length_of(lens, b, 1, s.tokens_k));
     const uint32_t first_q = block * s.block_q * 64u;
     if (first_q >= len_q) return;
     const uint32_t block_keys = s.block_k * 64u, blocks_k = (len_k + block_keys - 1) / block_keys;   // blocks with a key
@@ -329,7 +343,6 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
     const uint8_t* vg = reinterpret_cast<const uint8_t*>(v) + ((size_t)b * sv.batch + (size_t)hk * sv.head) * 16u;
     const uint32_t end_q = min(len_q, first_q + s.block_q * 64u);
     const uint32_t row = first_q + wave * 32u + col;                 // this lane's query
-    const bool works = first_q + wave * 32u < end_q;                 // (a wavefront without a query helps to load)
 
     // ---- the tiles: entries of the list, and of each the tiles with a key
     const bool all = s.top == kAllBlocks;
@@ -337,48 +350,67 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
     const uint32_t n_entries = all ? blocks_k : s.top;
     uint32_t entry = kSplit ? (uint32_t)((uint64_t)n_entries * part / s.parts) : 0u;
     const uint32_t last_entry = kSplit ? (uint32_t)((uint64_t)n_entries * (part + 1) / s.parts) : n_entries;
-    uint32_t key0 = 0, end = 0;   // the next tile's first key, the end of its block's keys
-    auto seek = [&]() {           // to the next entry with a key; false: there is none
-        for (; entry < last_entry; ++entry) {
-            const uint32_t which = all ? entry : (uint32_t)list[entry];
-            if (which < blocks_k) {   // (a negative one is not either)
-                key0 = __builtin_amdgcn_readfirstlane(which * block_keys);
-                end = min(key0 + block_keys, len_k);
-                ++entry;
-                return true;
+    struct Tile { uint32_t key, n; };   // first key, keys (0: no tile)
+    uint32_t cursor = 0, block_end = 0, held_from = entry;
+    int32_t held = 0;                   // a lane's entry of 64 (a read per entry would wait for the tiles' reads before it)
+    if (!all && entry < last_entry) held = list[min(entry + lane, last_entry - 1)];
+    auto next_tile = [&]() FB4_INLINE {
+        while (cursor >= block_end) {
+            if (entry >= last_entry) return Tile{0, 0};
+            if (!all && entry - held_from == 64) {
+                held_from = entry;
+                held = list[min(entry + lane, last_entry - 1)];
+            }
+            const uint32_t which = all ? entry : (uint32_t)__builtin_amdgcn_readlane(held, entry - held_from);
+            ++entry;
+            if (which < blocks_k) {     // (a negative one is not either)
+                cursor = which * block_keys;
+                block_end = min(cursor + block_keys, len_k);
             }
         }
-        return false;
+        const Tile t = {cursor, (uint32_t)min(block_end - cursor, (uint32_t)kKeys)};
+        cursor += kKeys;
+        return t;
     };
-    bool more = seek();
 
-    auto fetch = [&](uint8_t* buffer) {   // the tile at key0, and on to the next
-        const uint8_t* kt = kg + (size_t)key0 * kRowBytes;
-        const uint8_t* vt = vg + (size_t)key0 * sv.token * 16u;
-        const uint32_t valid = min(end - key0, (uint32_t)kKeys);
-        uint32_t l = lane;
-        asm volatile("" : "+v"(l));   // (opaque: else every load's offset is kept in a register of its own)
+    // ---- tiles from memory: this wavefront's loads wave, wave + kWaves, ..
+    auto key_place = [](uint32_t r) FB4_INLINE { return (r / (16u / kG)) & (kG - 1u); };                                    // f(row)
+    auto value_place = [](uint32_t r) FB4_INLINE { return kP == 16 ? 4u * (r & 3u) : kP == 8 ? 4u * ((r >> 1) & 1u) : 0u; };
+    uint32_t from_k[kMine], from_v[kMine];   // a lane's place in a tile, in bytes
 #pragma unroll
-        for (uint32_t i0 = 0; i0 < kLoads; i0 += kWaves) {
-            const uint32_t i = i0 + wave;
-            if (i0 + kWaves > kLoads && i >= kLoads) break;
-            const uint32_t j = 64u * i + l, r = j / kP, p = j - r * kP;
-            const uint32_t pk = p ^ ((r / (16u / kG)) & (kG - 1u)), pv = p ^ (kP == 16 ? 4u * (r & 3u) : kP == 8 ? 4u * ((r >> 1) & 1u) : 0u);
-            const uint32_t at = __builtin_amdgcn_readfirstlane(i * 1024u);
-            if (r < valid) {   // (a lane that takes no part leaves its 16 bytes alone)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(kt + r * kRowBytes + pk * 16u),
-                                                 (__attribute__((address_space(3))) void*)(buffer + at), 16, 0, 0);
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(vt + (size_t)r * sv.token * 16u + pv * 16u),
-                                                 (__attribute__((address_space(3))) void*)(buffer + kBytes + at), 16, 0, 0);
-            } else if (j < kPositions) {
-                // values behind the last key: zeros, which their weights of 0 leave zeros (the keys' scores are replaced)
-                *reinterpret_cast<uint4*>(buffer + kBytes + j * 16u) = make_uint4(0, 0, 0, 0);
+    for (int i = 0; i < kMine; ++i) {
+        const uint32_t j = 64u * (i * kWaves + wave) + lane, r = j / kP, p = j - r * kP;
+        from_k[i] = r * kRowBytes + ((p ^ key_place(r)) << 4);
+        from_v[i] = r * sv.token * 16u + ((p ^ value_place(r)) << 4);
+    }
+    auto copy = [&](const uint8_t* from, uint8_t* to) FB4_INLINE {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+    };
+    auto fetch = [&](const Tile& t, const uint8_t* base, const uint32_t* from, uint32_t row_bytes, uint8_t* buffer, bool values) FB4_INLINE {
+        if (t.n == (uint32_t)kKeys && kPositions % 64 == 0) {
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+                const uint32_t load = i * kWaves + wave;
+                if ((i + 1) * kWaves <= (int)kLoads || load < kLoads) copy(base + from[i], buffer + __builtin_amdgcn_readfirstlane(load * 1024u));
+            }
+        } else if (t.n) {
+#pragma unroll 1
+            for (uint32_t load = wave; load < kLoads; load += kWaves) {
+                const uint32_t j = 64u * load + lane, r = j / kP, p = j - r * kP;
+                if (r < t.n) {   // (a lane that takes no part leaves its 16 bytes alone)
+                    copy(base + r * row_bytes + ((p ^ (values ? value_place(r) : key_place(r))) << 4), buffer + __builtin_amdgcn_readfirstlane(load * 1024u));
+                } else if (values && j < kPositions) {
+                    // values behind the last key: zeros, which their weights of 0 leave zeros (the keys' products are replaced)
+                    *reinterpret_cast<uint4*>(buffer + j * 16u) = make_uint4(0, 0, 0, 0);
+                }
             }
         }
-        key0 += kKeys;
-        if (key0 >= end) more = seek();
     };
+    auto fetch_k = [&](const Tile& t, uint8_t* buffer) FB4_INLINE { fetch(t, kg + (size_t)t.key * kRowBytes, from_k, kRowBytes, buffer, false); };
+    auto fetch_v = [&](const Tile& t, uint8_t* buffer) FB4_INLINE { fetch(t, vg + (size_t)t.key * sv.token * 16u, from_v, sv.token * 16u, buffer, true); };
 
+    Tile now = next_tile();
+    fetch_k(now, lds_k0);
     // ---- this wavefront's queries as B operands
     mfma_bf16x8 qf[kSteps];
     {
@@ -390,52 +422,84 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
             qf[i] = __builtin_bit_cast(mfma_bf16x8, w);
         }
     }
-    const float factor = s.scale * 1.44269504088896340736f;   // to powers of two
-    mfma_f32x16 o[kTiles];
+    const float factor = s.scale * 1.44269504088896340736f;   // c
+    mfma_f32x16 o[kTiles], sc = {}, sd = {};   // accumulators; products of the groups at hand, in turn
+    mfma_bf16x8 p[2] = {};               // weights of the group before it, as operands
 #pragma unroll
     for (int d = 0; d < kTiles; ++d) o[d] = mfma_f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-    float most = -__builtin_inff(), sum = 0.0f;   // of this lane's query: what is taken off its products; sum over this lane's keys
+    // of this lane's query: the largest product that the reference is made of, the reference (-Inf: no product yet, then 0 is taken
+    // off), the sum over this lane's keys
+    float most = -__builtin_inff(), reference = -__builtin_inff(), off = 0.0f, sum = 0.0f;
+    bool large = false;                                  // (of the wavefront)
 
     // LDS offsets: the keys' operand, row lane % 32 of 32, piece 2 step + lane / 32; the values', 8 bytes of row (lane % 16) / 4
-    const uint32_t k_row = col * kRowBytes, k_swz = (col / (16u / kG)) & (kG - 1u);
+    const uint32_t k_row = col * kRowBytes, k_swz = key_place(col);
     const uint32_t v_r = 4u * half + (lane & 15u) / 4u;
-    const uint32_t v_swz = kP == 16 ? 4u * (v_r & 3u) : kP == 8 ? 4u * ((v_r >> 1) & 1u) : 0u;   // (8 and 16 rows further the same)
+    const uint32_t v_swz = value_place(v_r);   // (8 and 16 rows further the same)
     const uint32_t v_piece = 2u * ((lane >> 4) & 1u) + ((lane & 3u) >> 1), v_at = v_r * kRowBytes + 8u * (lane & 1u);
-
-    auto compute = [&](const uint8_t* buffer, uint32_t n) {   // n: keys of the tile
-        if (!works) return;
-        mfma_f32x16 sc[kGroups];
+    auto key_operand = [&](const uint8_t* keys, int group, int i) FB4_INLINE {
+        const uint32_t at = 32u * group * kRowBytes + k_row + (((2u * i + half) ^ k_swz) << 4);
+        return __builtin_bit_cast(mfma_bf16x8, *reinterpret_cast<const uint4*>(keys + ((kP % 2 && i == kSteps - 1 && half) ? kBytes : at)));
+    };
+    auto value_operand = [&](const uint8_t* values, int group, int i, int d) FB4_INLINE {
+        // lane t of 16 reads 8 bytes of row t / 4 and gets column t of the four rows.  (Channels past the row: what lies behind, in
+        // accumulators that nobody reads)
+        typedef __attribute__((address_space(3))) attn_s16x4* lds_s16x4;
+        const uint8_t* from = values + (32u * group + 16u * i) * kRowBytes + v_at + (((4u * d + v_piece) ^ v_swz) << 4);
+        const uint2 v0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(from)));
+        const uint2 v1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(from + 8u * kRowBytes)));
+        return __builtin_bit_cast(mfma_bf16x8, make_uint4(v0.x, v0.y, v1.x, v1.y));
+    };
+    // The instructions' order is the source's: a scheduling barrier behind every MFMA's slot, which holds what runs beside it.
+    constexpr int kProducts = 2 * kTiles;          // of P V per group
+    constexpr int kAhead = 4;                      // operands read ahead of their MFMA
+    // P V of the group whose weights are in p; `beside(x)`: what goes with product x
+    auto add_values = [&](const uint8_t* values, int group, auto beside) FB4_INLINE {
+        mfma_bf16x8 a[kProducts];
 #pragma unroll
-        for (int j = 0; j < kGroups; ++j) {
-            sc[j] = mfma_f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+        for (int x = 0; x < kProducts && x < kAhead; ++x) a[x] = value_operand(values, group, x / kTiles, x % kTiles);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                const uint32_t at = 32u * j * kRowBytes + k_row + (((2u * i + half) ^ k_swz) << 4);
-                const uint4 a = *reinterpret_cast<const uint4*>(buffer + ((kP % 2 && i == kSteps - 1 && half) ? 2u * kBytes : at));
-                sc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(mfma_bf16x8, a), qf[i], sc[j], 0, 0, 0);
+        for (int x = 0; x < kProducts; ++x) {
+            o[x % kTiles] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[x], p[x / kTiles], o[x % kTiles], 0, 0, 0);
+            if (x + kAhead < kProducts) a[x + kAhead] = value_operand(values, group, (x + kAhead) / kTiles, (x + kAhead) % kTiles);
+            beside(x);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // One step: weights of the group in `sc`, which are keys `first` .. of a tile of n; P V of the group before it, Q K of the one
+    // behind into `next`.
+    auto step = [&](mfma_f32x16& sc, mfma_f32x16& next, uint32_t first, uint32_t n, const uint8_t* values, int v_group, const uint8_t* keys,
+                    int k_group) FB4_INLINE {
+        if (first + 32u > n) {   // (a sequence's last tile)
+            uint32_t key = first + 4u * half;
+            asm volatile("" : "+v"(key));   // (opaque: else sixteen sums are kept for it all the time)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[i] = key + 8u * (i / 4) + i % 4 >= n ? -__builtin_inff() : sc[i];
+        }
+        mfma_bf16x8 a[kSteps];
+        float larger = -__builtin_inff();
+        add_values(values, v_group, [&](int x) FB4_INLINE {
+            // the first operands of Q K; the maximum, not before the products it is of are done
+            constexpr int kFirst = kProducts > 4 ? 2 : 0, kShare = 16 / (kProducts - kFirst), kEarly = kSteps < kAhead ? kSteps : kAhead;
+#pragma unroll
+            for (int i = 0; i < kEarly; ++i) {
+                if (x == (kProducts > kEarly - i ? kProducts - kEarly + i : 0)) a[i] = key_operand(keys, k_group, i);
             }
-        }
-        if (n < (uint32_t)kKeys) {   // (a sequence's last tile)
+            if (x >= kFirst) {
 #pragma unroll
-            for (int j = 0; j < kGroups; ++j) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    if (32u * j + 8u * (i / 4) + 4u * half + i % 4 >= n) sc[j][i] = -__builtin_inff();
-                }
+                for (int i = (x - kFirst) * kShare; i < (x == kProducts - 1 ? 16 : (x - kFirst + 1) * kShare); ++i) larger = fmaxf(larger, sc[i]);
             }
-        }
-        float larger = sc[0][0];
-#pragma unroll
-        for (int j = 0; j < kGroups; ++j) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) larger = fmaxf(larger, sc[j][i]);
-        }
-        if (__any((larger - most) * factor > 8.0f)) {
+        });
+        if (__any(fmaf(larger, factor, -reference) > 8.0f)) {
             larger = fmaxf(larger, most);
             larger = fmaxf(larger, __shfl_xor(larger, 32));
             // (of the difference: 1 where the maximum stays)
             const float shrink = most == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((most - larger) * factor);
             most = larger;
+            reference = larger * factor;
+            off = larger == -__builtin_inff() ? 0.0f : reference;
+            large = large || __any(fabsf(off) > 0x1p20f);
             sum *= shrink;
 #pragma unroll
             for (int d = 0; d < kTiles; ++d) {
@@ -443,58 +507,77 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
                 for (int i = 0; i < 16; ++i) o[d][i] *= shrink;
             }
         }
-        const float base = most == -__builtin_inff() ? 0.0f : most;   // (nothing but -Inf so far: the powers are to be 0)
-        float tile_sum = 0.0f;   // (one rounding of the row's sum per tile and not per key)
+        // In bf16 for the matrix cores, the sum from the unrounded weights: a rounding is half a bf16 step of a weight, as the output's
+        // own is of the result.  (The sum: one rounding of the row's per group and not per key)
+        float x = 0.0f, y = 0.0f;
+        uint32_t w[8];
+        auto products = [&](auto power) FB4_INLINE {
 #pragma unroll
-        for (int j = 0; j < kGroups; ++j) {
+            for (int i = 0; i < kSteps; ++i) {
+                if (i == 0) next = mfma_f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+                next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], qf[i], next, 0, 0, 0);
+                if (i + kAhead < kSteps) a[i + kAhead] = key_operand(keys, k_group, i + kAhead);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                // (of a difference: a fused product less the maximum's would keep that product's rounding, large for large scores)
-                sc[j][i] = __builtin_amdgcn_exp2f((sc[j][i] - base) * factor);
-                tile_sum += sc[j][i];
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                // P in bf16 for the matrix cores, the sum from the unrounded values: a rounding is half a bf16 step of a
-                // weight, as the output's own is of the result
-                uint32_t w[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    w[c] = __builtin_bit_cast(uint32_t, __builtin_convertvector((attn_f32x2{sc[j][8 * i + 2 * c], sc[j][8 * i + 2 * c + 1]}), attn_bf16x2));
-                const mfma_bf16x8 p = __builtin_bit_cast(mfma_bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-#pragma unroll
-                for (int d = 0; d < kTiles; ++d) {
-                    // lane t of 16 reads 8 bytes of row t / 4 and gets column t of the four rows.  (Channels past the row: what lies
-                    // behind, in accumulators that nobody reads)
-                    typedef __attribute__((address_space(3))) attn_s16x4* lds_s16x4;
-                    const uint8_t* from = buffer + kBytes + (32u * j + 16u * i) * kRowBytes + v_at + (((4u * d + v_piece) ^ v_swz) << 4);
-                    const uint2 v0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(from)));
-                    const uint2 v1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(from + 8u * kRowBytes)));
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(mfma_bf16x8, make_uint4(v0.x, v0.y, v1.x, v1.y)), p, o[d], 0, 0, 0);
+                for (int c = 8 * i / kSteps; c < 8 * (i + 1) / kSteps; ++c) {
+                    const float w0 = power(sc[2 * c]), w1 = power(sc[2 * c + 1]);
+                    x += w0;
+                    y += w1;
+                    w[c] = __builtin_bit_cast(uint32_t, __builtin_convertvector((attn_f32x2{w0, w1}), attn_bf16x2));
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
+        };
+        if (large) {
+            const float base = most == -__builtin_inff() ? 0.0f : most;
+            products([&](float z) FB4_INLINE { return __builtin_amdgcn_exp2f((z - base) * factor); });
+        } else {
+            products([&](float z) FB4_INLINE { return __builtin_amdgcn_exp2f(fmaf(z, factor, -off)); });
         }
-        sum += tile_sum;
+        sum += x + y;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) p[i] = __builtin_bit_cast(mfma_bf16x8, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
     };
-
-    if (kP % 2 && threadIdx.x < 8) reinterpret_cast<uint32_t*>((threadIdx.x & 4u ? lds_b : lds_a) + 2 * kBytes)[threadIdx.x & 3u] = 0;   // the zeroed pieces
-    uint32_t n_a = 0, n_b = 0;   // keys of the tiles in the buffers, 0: none
-    if (more) {
-        n_a = min(end - key0, (uint32_t)kKeys);
-        fetch(lds_a);
-    }
-    while (n_a) {
-        __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wavefront's part of the tile is in LDS
-        __syncthreads();                      // ... and everyone's; the other buffer is free
-        n_b = more ? min(end - key0, (uint32_t)kKeys) : 0u;
-        if (more) fetch(lds_b);
-        compute(lds_a, n_a);
-        if (!n_b) break;
-        __builtin_amdgcn_s_waitcnt(0x0F70);
-        __syncthreads();
-        n_a = more ? min(end - key0, (uint32_t)kKeys) : 0u;
-        if (more) fetch(lds_a);
-        compute(lds_b, n_b);
+    auto landed = [&]() FB4_INLINE {
+        __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wavefront's loads are in LDS
+        __syncthreads();                      // ... and everyone's; everyone is done with the buffers that come next
+    };
+    if (now.n) {
+        Tile then = next_tile();
+        // the zeroed pieces; values for the step before the first group, whose weights are 0
+        if (kP % 2 && threadIdx.x < 8) reinterpret_cast<uint32_t*>((threadIdx.x & 4u ? lds_k1 : lds_k0) + kBytes)[threadIdx.x & 3u] = 0;
+        for (uint32_t i = threadIdx.x; i < kBytes / 16 + 4; i += 64 * kWaves) *reinterpret_cast<uint4*>(lds_v1 + 16u * i) = make_uint4(0, 0, 0, 0);
+        landed();
+        fetch_k(then, lds_k1);
+        if (kGroups == 2) fetch_v(now, lds_v0);
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_operand(lds_k0, 0, i), qf[i], sc, 0, 0, 0);
+        // A tile; its keys and values in k_now and v_now, the next one's keys in k_then, the previous one's values in v_then, whose
+        // place the next one's take.  False: it was the last.
+        auto tile = [&](mfma_f32x16& s_now, mfma_f32x16& s_then, uint8_t* k_now, uint8_t* k_then, uint8_t* v_now, uint8_t* v_then) FB4_INLINE {
+            if (kGroups == 2) step(s_now, s_then, 0, now.n, v_then, 1, k_now, 1);
+            landed();
+            const Tile after = then.n ? next_tile() : Tile{0, 0};
+            fetch_k(after, k_now);
+            if (kGroups == 2) {
+                fetch_v(then, v_then);
+                step(s_then, s_now, 32, now.n, v_now, 0, k_then, 0);
+            } else {
+                fetch_v(now, v_now);
+                step(s_now, s_then, 0, now.n, v_then, 0, k_then, 0);
+            }
+            now = then;
+            then = after;
+            return now.n > 0;
+        };
+        const uint8_t* last_values;
+        for (;;) {
+            last_values = lds_v0;
+            if (!tile(sc, sd, lds_k0, lds_k1, lds_v0, lds_v1)) break;
+            last_values = lds_v1;
+            if (!tile(kGroups == 2 ? sc : sd, kGroups == 2 ? sd : sc, lds_k1, lds_k0, lds_v1, lds_v0)) break;
+        }
+        if (kGroups == 1) landed();
+        add_values(last_values, kGroups - 1, [](int) {});   // of the last group
     }
     sum += __shfl_xor(sum, 32);
     if (row >= end_q) return;
@@ -510,7 +593,7 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
                 if (c < kP * 8u) *reinterpret_cast<float4*>(to + c) = make_float4(o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]);
             }
         }
-        if (half == 0) *reinterpret_cast<float2*>(reinterpret_cast<float*>(out) + s.parts * n_rows * (kP * 8) + 2 * (part * n_rows + at_row)) = make_float2(most, sum);
+        if (half == 0) *reinterpret_cast<float2*>(reinterpret_cast<float*>(out) + s.parts * n_rows * (kP * 8) + 2 * (part * n_rows + at_row)) = make_float2(reference, sum);
         return;
     }
     const float inverse = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;   // (a NaN stays; no key: zeros)
@@ -527,21 +610,23 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
             if (c < kP * 8u) *reinterpret_cast<uint2*>(to + c) = make_uint2(w[0], w[1]);
         }
     }
-    if (lse && half == 0) lse[at_row] = sum == 0.0f ? -__builtin_inff() : most * s.scale + 0.69314718055994530942f * __builtin_amdgcn_logf(sum);
+    if (lse && half == 0) lse[at_row] = sum == 0.0f ? -__builtin_inff() : 0.69314718055994530942f * (off + __builtin_amdgcn_logf(sum));
 }
 
-// The parts of a row's list meet: accumulators and sums relative to the parts' own maxima.  Workspace: float [parts][rows][dim], then
-// {maximum, sum} [parts][rows].  A workgroup per row: eight parts at a time, four channels to a thread, so that a row waits for few
+#undef FB4_INLINE
+
+// The parts of a row's list meet: accumulators and sums relative to the parts' own references (powers of
+// two; -Inf: no key).  Workspace: float [parts][rows][dim], then
+// {reference, sum} [parts][rows].  A workgroup per row: eight parts at a time, four channels to a thread, so that a row waits for few
 // reads one behind the other (48 rows x 21 parts x 128 channels 20.8 us with a wavefront that walks over the parts).
 __global__ __launch_bounds__(256) void join_parts_kernel(const float* workspace, const int32_t* lens, uint16_t* out, float* lse, TensorStrides so,
-                                                         uint32_t parts, uint32_t n_rows, uint32_t tokens_q, uint32_t heads, uint32_t dim, float scale)
+                                                         uint32_t parts, uint32_t n_rows, uint32_t tokens_q, uint32_t heads, uint32_t dim)
 {
     __shared__ float4 meet[8][32];
     const uint32_t lane = threadIdx.x & 63, at = blockIdx.x, c = 4u * (threadIdx.x & 31u), sub = threadIdx.x >> 5;
     const uint32_t g = at / tokens_q, row = at - g * tokens_q, b = g / heads, h = g - b * heads;
     if (row >= length_of(lens, b, 0, tokens_q)) return;
     const float2* state = reinterpret_cast<const float2*>(workspace + (size_t)parts * n_rows * dim) + at;
-    const float factor = scale * 1.44269504088896340736f;
     float most = -__builtin_inff(), sum = 0.0f;
     for (uint32_t p = lane; p < parts; p += 64) most = fmaxf(most, state[(size_t)p * n_rows].x);
 #pragma unroll
@@ -549,7 +634,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float* workspace,
     const float base = most == -__builtin_inff() ? 0.0f : most;
     for (uint32_t p = lane; p < parts; p += 64) {
         const float2 st = state[(size_t)p * n_rows];
-        sum = fmaf(st.y, __builtin_amdgcn_exp2f((st.x - base) * factor), sum);
+        sum = fmaf(st.y, __builtin_amdgcn_exp2f(st.x - base), sum);
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
@@ -557,7 +642,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float* workspace,
     if (c < dim) {
 #pragma unroll 4
         for (uint32_t p = sub; p < parts; p += 8) {
-            const float w = __builtin_amdgcn_exp2f((state[(size_t)p * n_rows].x - base) * factor);
+            const float w = __builtin_amdgcn_exp2f(state[(size_t)p * n_rows].x - base);
             const float4 x = *reinterpret_cast<const float4*>(workspace + ((size_t)p * n_rows + at) * dim + c);
             o = make_float4(fmaf(x.x, w, o.x), fmaf(x.y, w, o.y), fmaf(x.z, w, o.z), fmaf(x.w, w, o.w));
         }
@@ -575,7 +660,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float* workspace,
     const attn_bf16x2 lo = __builtin_convertvector((attn_f32x2{o.x * inverse, o.y * inverse}), attn_bf16x2);
     const attn_bf16x2 hi = __builtin_convertvector((attn_f32x2{o.z * inverse, o.w * inverse}), attn_bf16x2);
     if (c < dim) *reinterpret_cast<uint2*>(to + c) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
-    if (lse && threadIdx.x == 0) lse[at] = sum == 0.0f ? -__builtin_inff() : most * scale + 0.69314718055994530942f * __builtin_amdgcn_logf(sum);
+    if (lse && threadIdx.x == 0) lse[at] = sum == 0.0f ? -__builtin_inff() : 0.69314718055994530942f * (base + __builtin_amdgcn_logf(sum));
 }
 
 }  // namespace fb4

@@ -180,6 +180,7 @@ int fb4_block_attention(const void* q, const void* k, const void* v, const int64
     TensorStrides sv = {0, 0, 0}, so;
     if (tokens_k > 0) {
         if (int rc = strides_of(v_strides, &sv)) return rc;
+        if (v_strides[2] >= 1 << 25) return FB4_ERR_UNSUPPORTED;   // (a tile's rows by 32-bit offsets)
     }
     if (int rc = strides_of(out_strides, &so)) return rc;
     if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) || !aligned(lens, 4) || !aligned(blocks, 4) || !aligned(lse, 4) ||
@@ -210,7 +211,7 @@ int fb4_block_attention(const void* q, const void* k, const void* v, const int64
     if (parts > 1) {
         const int64_t rows = batch * heads * tokens_q;   // (at most 512 blocks of 128)
         launch(join_parts_kernel, dim3((unsigned)rows), dim3(256), 0, st, static_cast<const float*>(workspace), lens, static_cast<uint16_t*>(out), lse,
-               so, (uint32_t)parts, (uint32_t)rows, s.tokens_q, (uint32_t)heads, (uint32_t)dim, scale);
+               so, (uint32_t)parts, (uint32_t)rows, s.tokens_q, (uint32_t)heads, (uint32_t)dim);
     }
     return hipGetLastError() == hipSuccess ? FB4_OK : FB4_ERR_HIP;
 }

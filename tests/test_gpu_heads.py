@@ -258,9 +258,9 @@ def attention_reference(q, k, v, blocks, scale, block_q, block_k, lens):
                 qs, ks, vs = q[b, h, i0:i1].double(), k[b, h // share].index_select(0, at).double(), v[b, h // share].index_select(0, at).double()
                 s = scale * (qs @ ks.T)
                 # A weight: its score's dim products and sums in fp32, the power (argument and result), one rounding to bf16.
-                # The sum of n positive weights: 32 of a tile of 64 keys per lane, then one addition per tile, each off by at most
-                # 2^-24 of the sum (the split parts of a long list take fewer and meet with one more each).
-                weight = (dim + 8) * 2.0 ** -23 * scale * (qs.abs() @ ks.abs().T).amax(-1, keepdim=True) + 2.0 ** -18 + (len(keys) / 64 + 64) * 2.0 ** -24
+                # The sum of n positive weights: 16 of a group of 32 keys per lane, then one addition per group, each off by at most
+                # 2^-24 of the sum: n / 32 + 16, and a few more where halves and parts meet.
+                weight = (dim + 8) * 2.0 ** -23 * scale * (qs.abs() @ ks.abs().T).amax(-1, keepdim=True) + 2.0 ** -18 + (len(keys) / 32 + 64) * 2.0 ** -24
                 total = torch.logsumexp(s, -1, keepdim=True)
                 p = torch.exp(s - total)
                 dead = total == -math.inf

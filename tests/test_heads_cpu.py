@@ -72,7 +72,7 @@ def test_attention_refusals():
         assert attention(**{**big, **bad}) == F.ERR_INVALID_ARG, bad
     for bad in (dict(dim=60), dict(dim=136), dict(bq=32), dict(bk=96), dict(bk=0), dict(q=P(AL + 8)), dict(k=P(AL + 8)), dict(v=P(AL + 8)),
                 dict(out=P(AL + 8)), dict(lens=P(AL + 2)), dict(blocks=P(AL + 1)), dict(lse=P(AL + 2)), dict(sv=strides(0, 64, 132)),
-                dict(so=strides(4, 64, 256)), dict(heads=70000, hk=1), dict(tq=2 ** 31), dict(batch=2 ** 24)):
+                dict(so=strides(4, 64, 256)), dict(sv=strides(0, 64, 2 ** 25)), dict(heads=70000, hk=1), dict(tq=2 ** 31), dict(batch=2 ** 24)):
         assert attention(**{**big, **bad}) == F.ERR_UNSUPPORTED, bad
     # a workspace that is too small, or none where there has to be one
     need = B.lib().fb4_block_attention_workspace(1, 1, 1, 1, 1 << 20, 64, -1, 64, 64)
