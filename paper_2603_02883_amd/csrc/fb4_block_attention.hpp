@@ -376,9 +376,12 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
     // ---- tiles from memory: this wavefront's loads wave, wave + kWaves, ..
     auto key_place = [](uint32_t r) FB4_INLINE { return (r / (16u / kG)) & (kG - 1u); };                                    // f(row)
     auto value_place = [](uint32_t r) FB4_INLINE { return kP == 16 ? 4u * (r & 3u) : kP == 8 ? 4u * ((r >> 1) & 1u) : 0u; };
-    uint32_t from_k[kMine], from_v[kMine];   // a lane's place in a tile, in bytes
+    // a lane's place in a tile, in bytes, for every load; for one, where the next is whole runs of 16 rows further (f is the same there)
+    constexpr bool kRegular = (64 * kWaves) % (16 * kP) == 0;
+    constexpr int kPlaces = kRegular ? 1 : kMine;
+    uint32_t from_k[kPlaces], from_v[kPlaces];
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
+    for (int i = 0; i < kPlaces; ++i) {
         const uint32_t j = 64u * (i * kWaves + wave) + lane, r = j / kP, p = j - r * kP;
         from_k[i] = r * kRowBytes + ((p ^ key_place(r)) << 4);
         from_v[i] = r * sv.token * 16u + ((p ^ value_place(r)) << 4);
@@ -391,7 +394,8 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
 #pragma unroll
             for (int i = 0; i < kMine; ++i) {
                 const uint32_t load = i * kWaves + wave;
-                if ((i + 1) * kWaves <= (int)kLoads || load < kLoads) copy(base + from[i], buffer + __builtin_amdgcn_readfirstlane(load * 1024u));
+                const uint8_t* at = kRegular ? base + (size_t)(i * (64 * kWaves / kP)) * row_bytes + from[0] : base + from[i % kPlaces];
+                if ((i + 1) * kWaves <= (int)kLoads || load < kLoads) copy(at, buffer + __builtin_amdgcn_readfirstlane(load * 1024u));
             }
         } else if (t.n) {
 #pragma unroll 1
@@ -409,8 +413,12 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
     auto fetch_k = [&](const Tile& t, uint8_t* buffer) FB4_INLINE { fetch(t, kg + (size_t)t.key * kRowBytes, from_k, kRowBytes, buffer, false); };
     auto fetch_v = [&](const Tile& t, uint8_t* buffer) FB4_INLINE { fetch(t, vg + (size_t)t.key * sv.token * 16u, from_v, sv.token * 16u, buffer, true); };
 
+    // (what the buffers hold is asked for at once: a short list's walk is little more than its first reads' wait)
     Tile now = next_tile();
     fetch_k(now, lds_k0);
+    Tile then = now.n ? next_tile() : Tile{0, 0};
+    fetch_k(then, lds_k1);
+    if (kGroups == 2) fetch_v(now, lds_v0);
     // ---- this wavefront's queries as B operands
     mfma_bf16x8 qf[kSteps];
     {
@@ -453,12 +461,14 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
     // The instructions' order is the source's: a scheduling barrier behind every MFMA's slot, which holds what runs beside it.
     constexpr int kProducts = 2 * kTiles;          // of P V per group
     constexpr int kAhead = 4;                      // operands read ahead of their MFMA
+    constexpr int kReady = kProducts < kAhead ? kProducts : kAhead;
+    mfma_bf16x8 ready[kReady];                     // the first operands of the next P V, read before its step
+    auto get_ready = [&](const uint8_t* values, int group, int x) FB4_INLINE { ready[x] = value_operand(values, group, x / kTiles, x % kTiles); };
     // P V of the group whose weights are in p; `beside(x)`: what goes with product x
     auto add_values = [&](const uint8_t* values, int group, auto beside) FB4_INLINE {
         mfma_bf16x8 a[kProducts];
 #pragma unroll
-        for (int x = 0; x < kProducts && x < kAhead; ++x) a[x] = value_operand(values, group, x / kTiles, x % kTiles);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int x = 0; x < kReady; ++x) a[x] = ready[x];
 #pragma unroll
         for (int x = 0; x < kProducts; ++x) {
             o[x % kTiles] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[x], p[x / kTiles], o[x % kTiles], 0, 0, 0);
@@ -470,7 +480,7 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
     // One step: weights of the group in `sc`, which are keys `first` .. of a tile of n; P V of the group before it, Q K of the one
     // behind into `next`.
     auto step = [&](mfma_f32x16& sc, mfma_f32x16& next, uint32_t first, uint32_t n, const uint8_t* values, int v_group, const uint8_t* keys,
-                    int k_group) FB4_INLINE {
+                    int k_group, auto later) FB4_INLINE {
         if (first + 32u > n) {   // (a sequence's last tile)
             uint32_t key = first + 4u * half;
             asm volatile("" : "+v"(key));   // (opaque: else sixteen sums are kept for it all the time)
@@ -484,7 +494,7 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
             constexpr int kFirst = kProducts > 4 ? 2 : 0, kShare = 16 / (kProducts - kFirst), kEarly = kSteps < kAhead ? kSteps : kAhead;
 #pragma unroll
             for (int i = 0; i < kEarly; ++i) {
-                if (x == (kProducts > kEarly - i ? kProducts - kEarly + i : 0)) a[i] = key_operand(keys, k_group, i);
+                if (x == (kProducts > kEarly + 1 - i ? kProducts - kEarly - 1 + i : 0)) a[i] = key_operand(keys, k_group, i);
             }
             if (x >= kFirst) {
 #pragma unroll
@@ -524,6 +534,10 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
                     y += w1;
                     w[c] = __builtin_bit_cast(uint32_t, __builtin_convertvector((attn_f32x2{w0, w1}), attn_bf16x2));
                 }
+#pragma unroll
+                for (int r = 0; r < kReady; ++r) {   // in the last slots, whose operands are read
+                    if (i == (kSteps > kReady ? kSteps - kReady + r : kSteps - 1)) later(r);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
@@ -542,41 +556,46 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
         __syncthreads();                      // ... and everyone's; everyone is done with the buffers that come next
     };
     if (now.n) {
-        Tile then = next_tile();
         // the zeroed pieces; values for the step before the first group, whose weights are 0
         if (kP % 2 && threadIdx.x < 8) reinterpret_cast<uint32_t*>((threadIdx.x & 4u ? lds_k1 : lds_k0) + kBytes)[threadIdx.x & 3u] = 0;
         for (uint32_t i = threadIdx.x; i < kBytes / 16 + 4; i += 64 * kWaves) *reinterpret_cast<uint4*>(lds_v1 + 16u * i) = make_uint4(0, 0, 0, 0);
         landed();
-        fetch_k(then, lds_k1);
-        if (kGroups == 2) fetch_v(now, lds_v0);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_operand(lds_k0, 0, i), qf[i], sc, 0, 0, 0);
         // A tile; its keys and values in k_now and v_now, the next one's keys in k_then, the previous one's values in v_then, whose
         // place the next one's take.  False: it was the last.
         auto tile = [&](mfma_f32x16& s_now, mfma_f32x16& s_then, uint8_t* k_now, uint8_t* k_then, uint8_t* v_now, uint8_t* v_then) FB4_INLINE {
-            if (kGroups == 2) step(s_now, s_then, 0, now.n, v_then, 1, k_now, 1);
+            if (kGroups == 2) step(s_now, s_then, 0, now.n, v_then, 1, k_now, 1, [](int) {});
             landed();
+#pragma unroll
+            for (int r = 0; r < kReady; ++r) get_ready(kGroups == 2 ? v_now : v_then, 0, r);
             const Tile after = then.n ? next_tile() : Tile{0, 0};
             fetch_k(after, k_now);
             if (kGroups == 2) {
                 fetch_v(then, v_then);
-                step(s_then, s_now, 32, now.n, v_now, 0, k_then, 0);
+                step(s_then, s_now, 32, now.n, v_now, 0, k_then, 0, [&](int r) FB4_INLINE { get_ready(v_now, 1, r); });
             } else {
                 fetch_v(now, v_now);
-                step(s_now, s_then, 0, now.n, v_then, 0, k_then, 0);
+                step(s_now, s_then, 0, now.n, v_then, 0, k_then, 0, [](int) {});
             }
             now = then;
             then = after;
             return now.n > 0;
         };
         const uint8_t* last_values;
+#pragma unroll
+        for (int r = 0; r < kReady; ++r) get_ready(lds_v1, kGroups - 1, r);
         for (;;) {
             last_values = lds_v0;
             if (!tile(sc, sd, lds_k0, lds_k1, lds_v0, lds_v1)) break;
             last_values = lds_v1;
             if (!tile(kGroups == 2 ? sc : sd, kGroups == 2 ? sd : sc, lds_k1, lds_k0, lds_v1, lds_v0)) break;
         }
-        if (kGroups == 1) landed();
+        if (kGroups == 1) {
+            landed();
+#pragma unroll
+            for (int r = 0; r < kReady; ++r) get_ready(last_values, 0, r);
+        }
         add_values(last_values, kGroups - 1, [](int) {});   // of the last group
     }
     sum += __shfl_xor(sum, 32);
