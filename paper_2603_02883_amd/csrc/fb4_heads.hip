@@ -85,25 +85,16 @@ int fb4_qk_norm_rope(const void* q, const int64_t* q_strides, const void* k, con
         return FB4_ERR_UNSUPPORTED;
     if (batch > (1 << 25) || tokens > (1 << 25) || batch * tokens > (1 << 25)) return FB4_ERR_UNSUPPORTED;   // (2^26 wavefronts to a launch)
     const int pieces = (int)(dim / 8);
-    int lanes = 1;
-    while (lanes < pieces) lanes *= 2;
-    const int rows = 64 / lanes, steps = (heads_q + rows - 1) / rows + (heads_k + rows - 1) / rows;
-    // A wavefront per token; several while there are few tokens.
-    const int64_t n = batch * tokens;
-    const int64_t chunks = std::min<int64_t>(std::min(steps, 255), std::max<int64_t>(1, 2048 / n));
-    RopeShape s = {(uint32_t)tokens, (uint32_t)n, (uint16_t)heads_q, (uint16_t)heads_k, eps, (uint8_t)pieces, {ends[0], ends[1], ends[2]},
-                   (uint8_t)n_axes, (uint8_t)pairs, (uint8_t)((norm ? kRopeNorm : 0) | (positions_shared ? kRopeShared : 0)), (uint8_t)chunks};
-    const dim3 grid((unsigned)((n * chunks + kRopeThreads / 64 - 1) / (kRopeThreads / 64)));
-#define FB4_ROPE_LAUNCH(pairing_, l) launch(qk_norm_rope_kernel<pairing_, l>, grid, dim3(kRopeThreads), 0, static_cast<hipStream_t>(stream), static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k), static_cast<uint16_t*>(q_out), static_cast<uint16_t*>(k_out), gamma_q, gamma_k, freqs, positions, sq, sk, s)
-#define FB4_ROPE_CASE(l)                                                          \
-    case l:                                                                       \
-        if (pairing == FB4_ROPE_ADJACENT) FB4_ROPE_LAUNCH(kRopeAdjacent, l);      \
-        else FB4_ROPE_LAUNCH(kRopeHalves, l);                                     \
-        break;
-    switch (lanes) {
-        FB4_ROPE_CASE(1) FB4_ROPE_CASE(2) FB4_ROPE_CASE(4) FB4_ROPE_CASE(8) FB4_ROPE_CASE(16) FB4_ROPE_CASE(32)
-    }
-#undef FB4_ROPE_CASE
+    // A wavefront per run of tokens; several, each with some of the heads, while there are few tokens.
+    const int64_t n = batch * tokens, rows = 64 / pieces, runs = (n + rows - 1) / rows;
+    const int64_t heads = heads_q + heads_k, most = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(heads, 255), 8192 / runs));
+    const int64_t each = (heads + most - 1) / most, chunks = (heads + each - 1) / each;
+    const RopeShape s = {(uint32_t)tokens, (uint32_t)n, (uint16_t)heads_q, (uint16_t)heads_k, eps, (uint8_t)pieces, {ends[0], ends[1], ends[2]},
+                         (uint8_t)n_axes, (uint8_t)pairs, (uint8_t)((norm ? kRopeNorm : 0) | (positions_shared ? kRopeShared : 0)), (uint8_t)chunks};
+    const dim3 grid((unsigned)((runs * chunks + kRopeThreads / 64 - 1) / (kRopeThreads / 64)));
+#define FB4_ROPE_LAUNCH(pairing_) launch(qk_norm_rope_kernel<pairing_>, grid, dim3(kRopeThreads), 0, static_cast<hipStream_t>(stream), static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k), static_cast<uint16_t*>(q_out), static_cast<uint16_t*>(k_out), gamma_q, gamma_k, freqs, positions, sq, sk, s)
+    if (pairing == FB4_ROPE_ADJACENT) FB4_ROPE_LAUNCH(kRopeAdjacent);
+    else FB4_ROPE_LAUNCH(kRopeHalves);
 #undef FB4_ROPE_LAUNCH
     return hipGetLastError() == hipSuccess ? FB4_OK : FB4_ERR_HIP;
 }
