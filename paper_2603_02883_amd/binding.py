@@ -139,6 +139,22 @@ def _tiles(grid_h, grid_w, tile_h, tile_w):
     return ((grid_h + tile_h - 1) // tile_h) * ((grid_w + tile_w - 1) // tile_w)
 
 
+def _require(ok, where, code=ERR_INVALID_ARG):
+    if not ok:
+        raise Fb4Error(code, where)
+
+
+def _on_device(where, device, *tensors):
+    """The kernels run on the current device, on its memory: anything else would be a foreign pointer there."""
+    for t, dtype in tensors:
+        _require(t is None or (t.is_cuda and t.device.index == device and t.dtype is dtype), where)
+
+
+def _strides(t):
+    """(batch, head, token) strides of a [batch][heads][tokens][dim] tensor (a single one's own stride says nothing)."""
+    return (ctypes.c_int64 * 3)(*[t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)])
+
+
 class CtypesCall:
     """The calls of csrc/fb4_pycall.c through ctypes, with the same arguments: the C module hands over here whatever it does not
     read itself (other types than its own, other shapes, errors), and where there is no module every call comes here."""
@@ -226,6 +242,81 @@ class CtypesCall:
         return _lib.fb4_seda_profile(h, _dp(meta), rows, nb, _dp(anchor_group), n_groups, _dp(counts), _dp(sub_formatbooks), s)
 
 
+class HeadsCall:
+    """The attention path's calls through ctypes, likewise.  They take strides and several types, so every tensor's place, type and
+    shape is checked; the C module hands over here whatever does not pass, to be refused."""
+
+    @staticmethod
+    def qk_norm_rope(q, k, positions, freqs, axis_pairs, gamma_q, gamma_k, eps, norm, pairing, q_out, k_out, device, s):
+        where = "fb4_qk_norm_rope"
+        batch, heads, tokens, dim = q.shape
+        _on_device(where, device, (q, torch.bfloat16), (k, torch.bfloat16), (positions, torch.int32), (freqs, torch.float64), (gamma_q, torch.float32),
+                   (gamma_k, torch.float32), (q_out, torch.bfloat16), (k_out, torch.bfloat16))
+        heads_k, n = 0 if k is None else k.shape[1], len(axis_pairs)
+        _require(k is None or k.shape == (batch, heads_k, tokens, dim), where)
+        if n:
+            _require(positions is not None and freqs is not None and positions.dim() == 3 and positions.shape[0] in (1, batch) and
+                     positions.shape[1:] == (tokens, n) and freqs.shape == (sum(axis_pairs),), where)
+        for t, h in ((q_out, heads), (k_out, heads_k)):
+            _require(t is None or t.shape == (batch, h, tokens, dim), where)
+        for t in (gamma_q, gamma_k):
+            _require(t is None or t.shape == (dim,), where)
+        for t in (positions, freqs, gamma_q, gamma_k, q_out, k_out):
+            _require(t is None or t.is_contiguous(), where, ERR_UNSUPPORTED)
+        for t in (q, k):
+            _require(t is None or dim == 1 or t.numel() == 0 or t.stride(3) == 1, where, ERR_UNSUPPORTED)
+        return _lib.fb4_qk_norm_rope(_dp(q), _strides(q), _dp(k), None if k is None else _strides(k), batch, tokens, heads, heads_k, dim,
+                                     1 if norm else 0, _dp(gamma_q), _dp(gamma_k), float(eps), _dp(positions) if n else None,
+                                     1 if n and positions.shape[0] == 1 else 0, _dp(freqs) if n else None, (ctypes.c_int32 * max(n, 1))(*axis_pairs), n,
+                                     int(pairing), _dp(q_out), _dp(k_out), s)
+
+    @staticmethod
+    def _sizes(where, q, k, lens, block_q, block_k):
+        """The sizes that the choice of blocks and the attention share, checked."""
+        batch, heads, tokens_q, dim = q.shape
+        _require(k.dim() == 4 and k.shape[0] == batch and k.shape[3] == dim and (lens is None or lens.shape == (batch, 2)) and block_q > 0 and block_k > 0, where)
+        for t in (q, k, lens):
+            _require(t is None or t.is_contiguous(), where, ERR_UNSUPPORTED)
+        return batch, heads, k.shape[1], tokens_q, k.shape[2], dim
+
+    @staticmethod
+    def select_key_blocks(q, k, top, block_q, block_k, lens, blocks, scores, workspace, device, s):
+        """(the bytes needed, where there is no workspace and has to be one; so the next one)"""
+        where = "fb4_select_key_blocks"
+        _on_device(where, device, (q, torch.bfloat16), (k, torch.bfloat16), (lens, torch.int32), (blocks, torch.int32), (scores, torch.float32),
+                   (workspace, torch.uint8))
+        batch, heads, heads_k, tokens_q, tokens_k, dim = HeadsCall._sizes(where, q, k, lens, block_q, block_k)
+        for t in (blocks, scores):
+            _require(t is None or (t.shape == (batch, heads, (tokens_q + block_q - 1) // block_q, top) and t.is_contiguous()), where)
+        size = _lib.fb4_select_key_blocks_workspace(batch, heads, heads_k, tokens_q, tokens_k, dim, block_q, block_k)
+        if workspace is None and size:
+            return size
+        return _lib.fb4_select_key_blocks(_dp(q), _dp(k), batch, heads, heads_k, tokens_q, tokens_k, dim, _dp(lens), block_q, block_k, top, _dp(blocks),
+                                          _dp(scores), _dp(workspace), 0 if workspace is None else workspace.numel(), s)
+
+    @staticmethod
+    def block_attention(q, k, v, blocks, scale, block_q, block_k, lens, out, lse, workspace, device, s):
+        where = "fb4_block_attention"
+        _on_device(where, device, (q, torch.bfloat16), (k, torch.bfloat16), (v, torch.bfloat16), (blocks, torch.int32), (lens, torch.int32),
+                   (out, torch.bfloat16), (lse, torch.float32), (workspace, torch.uint8))
+        batch, heads, heads_k, tokens_q, tokens_k, dim = HeadsCall._sizes(where, q, k, lens, block_q, block_k)
+        _require(v.shape == k.shape and out.shape == (batch, tokens_q, heads, dim) and (lse is None or lse.shape == (batch, heads, tokens_q)), where)
+        top = ALL_BLOCKS
+        if blocks is not None:
+            top = blocks.shape[-1]
+            _require(blocks.shape == (batch, heads, (tokens_q + block_q - 1) // block_q, top), where)
+        for t in (blocks, lse):
+            _require(t is None or t.is_contiguous(), where, ERR_UNSUPPORTED)
+        for t in (v, out):
+            _require(dim == 1 or t.numel() == 0 or t.stride(3) == 1, where, ERR_UNSUPPORTED)
+        size = _lib.fb4_block_attention_workspace(batch, heads, heads_k, tokens_q, tokens_k, dim, top, block_q, block_k)
+        if workspace is None and size:
+            return size
+        return _lib.fb4_block_attention(_dp(q), _dp(k), _dp(v), _strides(v), batch, heads, heads_k, tokens_q, tokens_k, dim, _dp(lens), _dp(blocks), top,
+                                        block_q, block_k, float(scale), _dp(out), _strides(out.transpose(1, 2)), _dp(lse), _dp(workspace),
+                                        0 if workspace is None else workspace.numel(), s)
+
+
 def _load_call():
     """The C module of this interpreter (by its path: a module of another one is not taken), built if it is missing and can be."""
     if not os.path.exists(_build.CALL):
@@ -239,15 +330,17 @@ def _load_call():
     loader = importlib.machinery.ExtensionFileLoader(name, _build.CALL)
     module = importlib.util.module_from_spec(importlib.util.spec_from_file_location(name, _build.CALL, loader=loader))
     loader.exec_module(module)
-    if not hasattr(module, "read_through"):   # built from an earlier source, without all of the calls
+    if not hasattr(module, "block_attention"):   # built from an earlier source, without all of the calls
         return CtypesCall
     module.bind(fb4_opts, ctypes.c_void_p, CtypesCall)
+    module.bind_heads(HeadsCall)
     # (a torch without the protocol has its tensors read by their methods)
     module.read_through(torch.Tensor, getattr(torch.Tensor, "__dlpack_c_exchange_api__", None))
     return module
 
 
 _call = _load_call()
+_heads_call = HeadsCall if _call is CtypesCall else _call
 
 
 def _stream(stream):
@@ -402,30 +495,8 @@ def fb4_seda_main_anchor_3d(scores, frames, grid_h, grid_w, tile_h=4, tile_w=4, 
     return anchors
 
 
-def _require(ok, where, code=ERR_INVALID_ARG):
-    if not ok:
-        raise Fb4Error(code, where)
-
-
-def _on_device(where, *tensors):
-    """The kernels run on the current device, on its memory: anything else would be a foreign pointer there."""
-    device = None
-    for t, dtype in tensors:
-        if t is not None:
-            if device is None:
-                device = torch.device("cuda", _get_device()) if t.is_cuda else None
-            _require(t.is_cuda and t.device == device and t.dtype is dtype, where)
-
-
-def _strides(t):
-    """(batch, head, token) strides of a [batch][heads][tokens][dim] tensor (a single one's own stride says nothing)."""
-    return (ctypes.c_int64 * 3)(*[t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)])
-
-
-def _workspace(given, size, device, stream):
+def _workspace(size, device, stream):
     """`size` bytes for the length of a call: memory of the stream that the call runs on, which later work there may reuse."""
-    if given is not None or size == 0:
-        return given
     if stream is None:
         return torch.empty(size, dtype=torch.uint8, device=device)
     with torch.cuda.stream(stream):
@@ -438,61 +509,34 @@ def fb4_qk_norm_rope(q, k, positions, freqs, axis_pairs, gamma_q=None, gamma_k=N
     k may be None.  positions: int32 cuda [batch or 1][tokens][axes]; freqs: float64 cuda [sum(axis_pairs)], radians per position;
     axis_pairs: pairs of channels per axis (empty: no rotation, positions and freqs None); gamma_q, gamma_k: float32 cuda [dim] or
     None; norm=False: rotation alone.  Returns contiguous (q_out, k_out) of the inputs' shapes."""
-    where = "fb4_qk_norm_rope"
-    batch, heads, tokens, dim = q.shape
-    _on_device(where, (q, torch.bfloat16), (k, torch.bfloat16), (positions, torch.int32), (freqs, torch.float64), (gamma_q, torch.float32),
-               (gamma_k, torch.float32), (q_out, torch.bfloat16), (k_out, torch.bfloat16))
-    heads_k = 0 if k is None else k.shape[1]
-    _require(k is None or (k.dim() == 4 and k.shape == (batch, heads_k, tokens, dim)), where)
-    n = len(axis_pairs)
-    if n:
-        _require(positions is not None and freqs is not None and positions.dim() == 3 and positions.shape[0] in (1, batch) and
-                 positions.shape[1:] == (tokens, n) and freqs.shape == (sum(axis_pairs),), where)
-    for t, h in ((q_out, heads), (k_out, heads_k)):
-        _require(t is None or t.shape == (batch, h, tokens, dim), where)
-    for t in (gamma_q, gamma_k):
-        _require(t is None or t.shape == (dim,), where)
-    for t in (positions, freqs, gamma_q, gamma_k, q_out, k_out):
-        _require(t is None or t.is_contiguous(), where, ERR_UNSUPPORTED)
-    for t in (q, k):
-        _require(t is None or dim == 1 or t.numel() == 0 or t.stride(3) == 1, where, ERR_UNSUPPORTED)
-    q_out = torch.empty((batch, heads, tokens, dim), dtype=q.dtype, device=q.device) if q_out is None else q_out
-    if k is not None and k_out is None:
-        k_out = torch.empty((batch, heads_k, tokens, dim), dtype=k.dtype, device=k.device)
-    _check(_lib.fb4_qk_norm_rope(_dp(q), _strides(q), _dp(k), None if k is None else _strides(k), batch, tokens, heads, heads_k, dim, 1 if norm else 0,
-                                 _dp(gamma_q), _dp(gamma_k), float(eps), _dp(positions), 1 if n and positions.shape[0] == 1 else 0, _dp(freqs),
-                                 (ctypes.c_int32 * max(n, 1))(*axis_pairs), n, int(pairing), _dp(q_out), None if k is None else _dp(k_out),
-                                 _stream(stream)), where)
-    return q_out, (None if k is None else k_out)
-
-
-def _heads(where, q, k, lens):
-    """The sizes that the choice of blocks and the attention share, checked."""
-    batch, heads, tokens_q, dim = q.shape
-    _require(k.dim() == 4 and k.shape[0] == batch and k.shape[3] == dim and (lens is None or lens.shape == (batch, 2)), where)
-    for t in (q, k, lens):
-        _require(t is None or t.is_contiguous(), where, ERR_UNSUPPORTED)
-    return batch, heads, k.shape[1], tokens_q, k.shape[2], dim
+    _require(q.is_cuda, "fb4_qk_norm_rope")
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    if k is None:
+        k_out = None
+    elif k_out is None:
+        k_out = torch.empty(k.shape, dtype=torch.bfloat16, device=k.device)
+    _check(_heads_call.qk_norm_rope(q, k, positions, freqs, tuple(axis_pairs), gamma_q, gamma_k, float(eps), bool(norm), int(pairing), q_out, k_out, _get_device(),
+                              _stream(stream)), "fb4_qk_norm_rope")
+    return q_out, k_out
 
 
 def fb4_select_key_blocks(q, k, top, block_q=128, block_k=128, lens=None, blocks=None, scores=None, want_scores=False, workspace=None, stream=None):
     """q: bf16 cuda [batch][heads][tokens_q][dim], k: [batch][heads_k][tokens_k][dim], contiguous; lens: int32 cuda [batch][2] (queries, keys)
     or None.  Returns int32 [batch][heads][query blocks][top], ascending, -1 behind (and the listed blocks' scores, float32, if asked)."""
-    where = "fb4_select_key_blocks"
-    _on_device(where, (q, torch.bfloat16), (k, torch.bfloat16), (lens, torch.int32), (blocks, torch.int32), (scores, torch.float32),
-               (workspace, torch.uint8))
-    batch, heads, heads_k, tokens_q, tokens_k, dim = _heads(where, q, k, lens)
-    _require(block_q > 0 and block_k > 0 and top >= 0, where)
-    shape = (batch, heads, (tokens_q + block_q - 1) // block_q, top)
-    for t in (blocks, scores):
-        _require(t is None or (t.shape == shape and t.is_contiguous()), where)
-    blocks = torch.empty(shape, dtype=torch.int32, device=q.device) if blocks is None else blocks
-    if want_scores and scores is None:
-        scores = torch.empty(shape, dtype=torch.float32, device=q.device)
-    size = _lib.fb4_select_key_blocks_workspace(batch, heads, heads_k, tokens_q, tokens_k, dim, block_q, block_k)
-    workspace = _workspace(workspace, size, q.device, stream)
-    _check(_lib.fb4_select_key_blocks(_dp(q), _dp(k), batch, heads, heads_k, tokens_q, tokens_k, dim, _dp(lens), block_q, block_k, top, _dp(blocks),
-                                      _dp(scores), _dp(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)), where)
+    _require(q.is_cuda, "fb4_select_key_blocks")
+    if blocks is None or (want_scores and scores is None):
+        _require(q.dim() == 4 and block_q > 0 and top >= 0, "fb4_select_key_blocks")
+        shape = (q.shape[0], q.shape[1], (q.shape[2] + block_q - 1) // block_q, top)
+        if blocks is None:
+            blocks = torch.empty(shape, dtype=torch.int32, device=q.device)
+        if want_scores and scores is None:
+            scores = torch.empty(shape, dtype=torch.float32, device=q.device)
+    s = _stream(stream)
+    rc = _heads_call.select_key_blocks(q, k, top, block_q, block_k, lens, blocks, scores, workspace, _get_device(), s)
+    if rc > 0:
+        rc = _heads_call.select_key_blocks(q, k, top, block_q, block_k, lens, blocks, scores, _workspace(rc, q.device, stream), _get_device(), s)
+    _check(rc, "fb4_select_key_blocks")
     return blocks if scores is None else (blocks, scores)
 
 
@@ -502,29 +546,22 @@ def fb4_block_attention(q, k, v, blocks=None, scale=None, block_q=128, block_k=1
     channels); blocks: int32 cuda [batch][heads][query blocks][n] or None for all keys; scale: dim ** -0.5 if None; lens: int32 cuda
     [batch][2] (queries, keys) or None.  Returns bf16 [batch][tokens_q][heads][dim] -- rows of fb4_quantize -- (and the logarithms of the
     sums, float32 [batch][heads][tokens_q], if asked).  Rows behind a sequence's last query are left as they were (zeros if not given)."""
-    where = "fb4_block_attention"
-    _on_device(where, (q, torch.bfloat16), (k, torch.bfloat16), (v, torch.bfloat16), (blocks, torch.int32), (lens, torch.int32),
-               (out, torch.bfloat16), (lse, torch.float32), (workspace, torch.uint8))
-    batch, heads, heads_k, tokens_q, tokens_k, dim = _heads(where, q, k, lens)
-    _require(block_q > 0 and block_k > 0 and v.shape == k.shape, where)
-    shape, top = (batch, tokens_q, heads, dim), ALL_BLOCKS
-    if blocks is not None:
-        top = blocks.shape[-1]
-        _require(blocks.shape == (batch, heads, (tokens_q + block_q - 1) // block_q, top), where)
-        _require(blocks.is_contiguous(), where, ERR_UNSUPPORTED)
-    _require((out is None or out.shape == shape) and (lse is None or lse.shape == (batch, heads, tokens_q)), where)
-    for t in (v, out):
-        _require(t is None or dim == 1 or t.numel() == 0 or t.stride(3) == 1, where, ERR_UNSUPPORTED)
-    _require(lse is None or lse.is_contiguous(), where, ERR_UNSUPPORTED)
-    empty = torch.empty if lens is None else torch.zeros
-    out = empty(shape, dtype=q.dtype, device=q.device) if out is None else out
-    if want_lse and lse is None:
-        lse = empty((batch, heads, tokens_q), dtype=torch.float32, device=q.device)
-    size = _lib.fb4_block_attention_workspace(batch, heads, heads_k, tokens_q, tokens_k, dim, top, block_q, block_k)
-    workspace = _workspace(workspace, size, q.device, stream)
-    _check(_lib.fb4_block_attention(_dp(q), _dp(k), _dp(v), _strides(v), batch, heads, heads_k, tokens_q, tokens_k, dim, _dp(lens), _dp(blocks), top,
-                                    block_q, block_k, float(dim ** -0.5 if scale is None else scale), _dp(out), _strides(out.transpose(1, 2)),
-                                    _dp(lse), _dp(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)), where)
+    _require(q.is_cuda, "fb4_block_attention")
+    if out is None or scale is None or (want_lse and lse is None):
+        batch, heads, tokens_q, dim = q.shape
+        empty = torch.empty if lens is None else torch.zeros
+        if out is None:
+            out = empty((batch, tokens_q, heads, dim), dtype=torch.bfloat16, device=q.device)
+        if want_lse and lse is None:
+            lse = empty((batch, heads, tokens_q), dtype=torch.float32, device=q.device)
+        if scale is None:
+            _require(dim > 0, "fb4_block_attention")
+            scale = dim ** -0.5
+    s = _stream(stream)
+    rc = _heads_call.block_attention(q, k, v, blocks, float(scale), block_q, block_k, lens, out, lse, workspace, _get_device(), s)
+    if rc > 0:
+        rc = _heads_call.block_attention(q, k, v, blocks, float(scale), block_q, block_k, lens, out, lse, _workspace(rc, q.device, stream), _get_device(), s)
+    _check(rc, "fb4_block_attention")
     return out if lse is None else (out, lse)
 
 

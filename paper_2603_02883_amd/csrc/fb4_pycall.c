@@ -197,7 +197,10 @@ enum { k_quantize, k_quantize_seda, k_quantize_decompose, k_dequantize, k_repack
 static const char* const call_names[kCalls] = {"quantize", "quantize_seda", "quantize_decompose", "dequantize", "repack_mxfp8",
                                                "layernorm_quantize", "gelu_quantize", "attention_scores",
                                                "select_salient_tokens", "seda_assign", "seda_main_anchor", "seda_profile"};
-static PyObject* through_ctypes[kCalls];
+// ... and the attention path's (bind_heads).
+enum { k_qk_norm_rope = kCalls, k_select_key_blocks, k_block_attention, kAll };
+static const char* const heads_names[kAll - kCalls] = {"qk_norm_rope", "select_key_blocks", "block_attention"};
+static PyObject* through_ctypes[kAll];
 
 static PyObject* elsewhere(int call, PyObject* const* a, Py_ssize_t n)
 {
@@ -372,6 +375,208 @@ static PyObject* py_seda_profile(ARGS)
     RETURN_CALL(fb4_seda_profile(h, m, d[0], d[1], ag, (int)g, counts, sub, s));
 }
 
+// The attention path.  Its calls take strides and several types, so everything is checked before a pointer is handed on: a tensor of the
+// wrong kind, shape or place goes by ctypes, where it is refused.
+
+// (weak: the module loads against a library without them too, and these calls go by ctypes then)
+extern __typeof__(fb4_qk_norm_rope) fb4_qk_norm_rope __attribute__((weak));
+extern __typeof__(fb4_select_key_blocks) fb4_select_key_blocks __attribute__((weak));
+extern __typeof__(fb4_select_key_blocks_workspace) fb4_select_key_blocks_workspace __attribute__((weak));
+extern __typeof__(fb4_block_attention) fb4_block_attention __attribute__((weak));
+extern __typeof__(fb4_block_attention_workspace) fb4_block_attention_workspace __attribute__((weak));
+
+typedef struct {
+    void* data;
+    int64_t size[4], stride[4];   // (a size of 1: stride 0)
+} view;
+enum { kInt = 0, kUint = 1, kFloat = 2, kBfloat = 4 };   // DLPack's type codes
+
+// A tensor of n dimensions of one type on GPU `device` (DLPack's types 2 and 10).
+static int viewed(PyObject* t, int n, int code, int bits, int64_t device, view* out)
+{
+    dl_tensor v;
+    if (!look(t, &v) || v.ndim != n || v.dtype.code != code || v.dtype.bits != bits || v.dtype.lanes != 1 ||
+        (v.device.type != 2 && v.device.type != 10) || v.device.id != device)
+        return -1;
+    for (int i = 0; i < n; ++i) {
+        out->size[i] = v.shape[i];
+        out->stride[i] = v.shape[i] > 1 ? v.strides[i] : 0;
+    }
+    out->data = data_of(&v);
+    return 0;
+}
+
+static int packed(const view* v, int n)   // contiguous
+{
+    int64_t next = 1;
+    for (int i = 0; i < n; ++i) {
+        if (v->size[i] == 0) return 1;
+    }
+    for (int i = n - 1; i >= 0; --i) {
+        if (v->size[i] > 1 && v->stride[i] != next) return 0;
+        next *= v->size[i];
+    }
+    return 1;
+}
+
+static int sizes_are(const view* v, int n, int64_t a, int64_t b, int64_t c, int64_t d)
+{
+    const int64_t want[4] = {a, b, c, d};
+    for (int i = 0; i < n; ++i) {
+        if (v->size[i] != want[i]) return 0;
+    }
+    return 1;
+}
+
+// ... of these sizes and contiguous; None: null if it may be missing.
+static int dense(PyObject* t, int missing, int n, int code, int bits, int64_t device, int64_t a, int64_t b, int64_t c, int64_t d, void** out)
+{
+    view v;
+    *out = NULL;
+    if (t == Py_None) return missing ? 0 : -1;
+    if (viewed(t, n, code, bits, device, &v) || !sizes_are(&v, n, a, b, c, d) || !packed(&v, n)) return -1;
+    *out = v.data;
+    return 0;
+}
+
+// [batch][heads][tokens][dim] with contiguous channels
+static int rows(PyObject* t, int64_t device, view* v)
+{
+    return viewed(t, 4, kBfloat, 16, device, v) || (v->size[3] > 1 && v->stride[3] != 1) ? -1 : 0;
+}
+
+// (q, k, positions, freqs, axis_pairs, gamma_q, gamma_k, eps, norm, pairing, q_out, k_out, device, stream)
+static PyObject* py_qk_norm_rope(ARGS)
+{
+    view q, k = {0}, p = {0};
+    void *freqs, *gq, *gk, *qo, *ko, *s;
+    int64_t device, pairing, pairs = 0, hk = 0;
+    int32_t axis_pairs[4];
+    if (!fb4_qk_norm_rope || n != 14 || integer(a[12], &device) || integer(a[9], &pairing) || address(a[13], &s) || !PyFloat_Check(a[7]) || !PyBool_Check(a[8]) ||
+        !PyTuple_Check(a[4]) || PyTuple_GET_SIZE(a[4]) > 4 || rows(a[0], device, &q))
+        return elsewhere(k_qk_norm_rope, a, n);
+    const int axes = (int)PyTuple_GET_SIZE(a[4]);
+    for (int i = 0; i < axes; ++i) {
+        int64_t x;
+        if (integer(PyTuple_GET_ITEM(a[4], i), &x) || x < 1 || x > 256) return elsewhere(k_qk_norm_rope, a, n);
+        axis_pairs[i] = (int32_t)x;
+        pairs += x;
+    }
+    const int64_t batch = q.size[0], tokens = q.size[2], dim = q.size[3];
+    if (a[1] != Py_None) {
+        if (rows(a[1], device, &k) || !sizes_are(&k, 4, batch, k.size[1], tokens, dim)) return elsewhere(k_qk_norm_rope, a, n);
+        hk = k.size[1];
+    }
+    if (axes && (viewed(a[2], 3, kInt, 32, device, &p) || (p.size[0] != 1 && p.size[0] != batch) || p.size[1] != tokens || p.size[2] != axes || !packed(&p, 3)))
+        return elsewhere(k_qk_norm_rope, a, n);
+    if (dense(a[3], !axes, 1, kFloat, 64, device, pairs, 0, 0, 0, &freqs) || dense(a[5], 1, 1, kFloat, 32, device, dim, 0, 0, 0, &gq) ||
+        dense(a[6], 1, 1, kFloat, 32, device, dim, 0, 0, 0, &gk) || dense(a[10], 0, 4, kBfloat, 16, device, batch, q.size[1], tokens, dim, &qo) ||
+        dense(a[11], a[1] == Py_None, 4, kBfloat, 16, device, batch, hk, tokens, dim, &ko))
+        return elsewhere(k_qk_norm_rope, a, n);
+    const float eps = (float)PyFloat_AS_DOUBLE(a[7]);
+    const int norm = a[8] == Py_True, shared = axes && p.size[0] == 1;
+    RETURN_CALL(fb4_qk_norm_rope(q.data, q.stride, k.data, k.stride, batch, tokens, (int)q.size[1], (int)hk, dim, norm, gq, gk, eps, p.data, shared, freqs,
+                                 axis_pairs, axes, (int)pairing, qo, ko, s));
+}
+
+// What the two below share: q, k, lens, the block sizes.  0, or -1 for ctypes.
+static int heads_of(PyObject* oq, PyObject* ok, PyObject* olens, PyObject* obq, PyObject* obk, int64_t device, view* q, view* k, void** lens, int64_t* bq,
+                    int64_t* bk)
+{
+    return rows(oq, device, q) || rows(ok, device, k) || !packed(q, 4) || !packed(k, 4) || k->size[0] != q->size[0] || k->size[3] != q->size[3] ||
+                   dense(olens, 1, 2, kInt, 32, device, q->size[0], 2, 0, 0, lens) || integer(obq, bq) || integer(obk, bk) || *bq < 1 || *bk < 1 ||
+                   q->size[1] > INT32_MAX || k->size[1] > INT32_MAX || *bq > INT32_MAX || *bk > INT32_MAX
+               ? -1 : 0;
+}
+
+// A workspace of uint8, or the bytes that are needed where there is none.
+static int workspace_of(PyObject* t, int64_t device, size_t needed, void** out, size_t* size)
+{
+    view v;
+    *out = NULL;
+    *size = 0;
+    if (t == Py_None) return needed == 0 ? 0 : 1;
+    if (viewed(t, 1, kUint, 8, device, &v) || !packed(&v, 1)) return -1;
+    *out = v.data;
+    *size = (size_t)v.size[0];
+    return 0;
+}
+
+// (q, k, top, block_q, block_k, lens, blocks, scores, workspace, device, stream)
+static PyObject* py_select_key_blocks(ARGS)
+{
+    view q, k;
+    void *lens, *blocks, *scores, *ws, *s;
+    size_t size;
+    int64_t device, top, bq, bk;
+    if (!fb4_select_key_blocks || n != 11 || integer(a[9], &device) || address(a[10], &s) || integer(a[2], &top) ||
+        heads_of(a[0], a[1], a[5], a[3], a[4], device, &q, &k, &lens, &bq, &bk) ||
+        dense(a[6], 0, 4, kInt, 32, device, q.size[0], q.size[1], (q.size[2] + bq - 1) / bq, top, &blocks) ||
+        dense(a[7], 1, 4, kFloat, 32, device, q.size[0], q.size[1], (q.size[2] + bq - 1) / bq, top, &scores))
+        return elsewhere(k_select_key_blocks, a, n);
+    const size_t needed = fb4_select_key_blocks_workspace(q.size[0], (int)q.size[1], (int)k.size[1], q.size[2], k.size[2], q.size[3], (int)bq, (int)bk);
+    const int rc_ws = workspace_of(a[8], device, needed, &ws, &size);
+    if (rc_ws < 0) return elsewhere(k_select_key_blocks, a, n);
+    if (rc_ws > 0) return PyLong_FromSize_t(needed);
+    RETURN_CALL(fb4_select_key_blocks(q.data, k.data, q.size[0], (int)q.size[1], (int)k.size[1], q.size[2], k.size[2], q.size[3], lens, (int)bq, (int)bk, top,
+                                      blocks, scores, ws, size, s));
+}
+
+// (q, k, v, blocks, scale, block_q, block_k, lens, out, lse, workspace, device, stream)
+static PyObject* py_block_attention(ARGS)
+{
+    view q, k, v, b = {0}, o;
+    void *lens, *lse, *ws, *s;
+    size_t size;
+    int64_t device, bq, bk;
+    if (!fb4_block_attention || n != 13 || integer(a[11], &device) || address(a[12], &s) || !PyFloat_Check(a[4]) ||
+        heads_of(a[0], a[1], a[7], a[5], a[6], device, &q, &k, &lens, &bq, &bk) || rows(a[2], device, &v) ||
+        !sizes_are(&v, 4, k.size[0], k.size[1], k.size[2], k.size[3]) || rows(a[8], device, &o) ||
+        !sizes_are(&o, 4, q.size[0], q.size[2], q.size[1], q.size[3]) ||
+        dense(a[9], 1, 3, kFloat, 32, device, q.size[0], q.size[1], q.size[2], 0, &lse))
+        return elsewhere(k_block_attention, a, n);
+    int64_t top = FB4_ALL_BLOCKS;
+    if (a[3] != Py_None) {
+        if (viewed(a[3], 4, kInt, 32, device, &b) || !sizes_are(&b, 4, q.size[0], q.size[1], (q.size[2] + bq - 1) / bq, b.size[3]) || !packed(&b, 4))
+            return elsewhere(k_block_attention, a, n);
+        top = b.size[3];
+    }
+    const size_t needed = fb4_block_attention_workspace(q.size[0], (int)q.size[1], (int)k.size[1], q.size[2], k.size[2], q.size[3], top, (int)bq, (int)bk);
+    const int rc_ws = workspace_of(a[10], device, needed, &ws, &size);
+    if (rc_ws < 0) return elsewhere(k_block_attention, a, n);
+    if (rc_ws > 0) return PyLong_FromSize_t(needed);
+    const float scale = (float)PyFloat_AS_DOUBLE(a[4]);
+    const int64_t so[3] = {o.stride[0], o.stride[2], o.stride[1]};   // (out is [batch][tokens][heads][dim])
+    RETURN_CALL(fb4_block_attention(q.data, k.data, v.data, v.stride, q.size[0], (int)q.size[1], (int)k.size[1], q.size[2], k.size[2], q.size[3], lens, b.data,
+                                    top, (int)bq, (int)bk, scale, o.data, so, lse, ws, size, s));
+}
+
+// The named attributes of `from` into `to`, all or (-1) none.
+static int take_calls(PyObject* from, const char* const* names, int n, PyObject** to)
+{
+    PyObject* found[kAll];
+    for (int i = 0; i < n; ++i) {
+        found[i] = PyObject_GetAttrString(from, names[i]);
+        if (!found[i]) {
+            while (i > 0) Py_DECREF(found[--i]);
+            return -1;
+        }
+    }
+    for (int i = 0; i < n; ++i) Py_XSETREF(to[i], found[i]);
+    return 0;
+}
+
+// (object with the attention path's calls through ctypes)
+static PyObject* py_bind_heads(ARGS)
+{
+    if (n != 1) {
+        PyErr_SetString(PyExc_TypeError, "bind_heads(calls through ctypes)");
+        return NULL;
+    }
+    if (take_calls(a[0], heads_names, kAll - kCalls, through_ctypes + kCalls)) return NULL;
+    Py_RETURN_NONE;
+}
+
 // (fb4_opts, c_void_p, object with the same calls through ctypes)
 static PyObject* py_bind(ARGS)
 {
@@ -379,15 +584,7 @@ static PyObject* py_bind(ARGS)
         PyErr_SetString(PyExc_TypeError, "bind(options type, handle type, calls through ctypes)");
         return NULL;
     }
-    PyObject* found[kCalls];
-    for (int i = 0; i < kCalls; ++i) {
-        found[i] = PyObject_GetAttrString(a[2], call_names[i]);
-        if (!found[i]) {
-            while (i > 0) Py_DECREF(found[--i]);
-            return NULL;
-        }
-    }
-    for (int i = 0; i < kCalls; ++i) Py_XSETREF(through_ctypes[i], found[i]);
+    if (take_calls(a[2], call_names, kCalls, through_ctypes)) return NULL;
     Py_INCREF(a[0]);
     Py_XSETREF(options_type, (PyTypeObject*)a[0]);
     Py_INCREF(a[1]);
@@ -412,7 +609,8 @@ static PyObject* py_read_through(ARGS)
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD(quantize), METHOD(quantize_seda), METHOD(quantize_decompose), METHOD(dequantize), METHOD(repack_mxfp8),
                                 METHOD(layernorm_quantize), METHOD(gelu_quantize), METHOD(attention_scores), METHOD(select_salient_tokens),
-                                METHOD(seda_assign), METHOD(seda_main_anchor), METHOD(seda_profile), METHOD(bind),
+                                METHOD(seda_assign), METHOD(seda_main_anchor), METHOD(seda_profile), METHOD(qk_norm_rope),
+                                METHOD(select_key_blocks), METHOD(block_attention), METHOD(bind), METHOD(bind_heads),
                                 METHOD(read_through), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fb4call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
