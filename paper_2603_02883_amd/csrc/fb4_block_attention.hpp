@@ -99,8 +99,10 @@ __device__ __forceinline__ uint64_t order_of(double x)
 
 typedef double select_f64x2 __attribute__((ext_vector_type(2)));
 typedef double select_f64x4 __attribute__((ext_vector_type(4)));
-constexpr int kSelectThreads = 512;
-constexpr uint32_t kSelectRows = 16;   // blocks of queries to a workgroup
+// Blocks of queries to a workgroup, in sixteens (the rows of an MFMA): two where their scores fill LDS, which halves what is read of
+// the keys' means -- from L2, at 9 TB/s, which one each was bound by.
+constexpr int select_sets(int values) { return values == 16 ? 2 : 1; }
+constexpr int select_threads(int values) { return 512 * select_sets(values); }
 
 // A workgroup takes 16 blocks of queries of one head: their scores with all the head's blocks of keys by 16x16x4 MFMAs in double,
 // then the largest `top` of every row.  The channels of a product may come in any order as long as both operands have the same:
@@ -111,11 +113,12 @@ constexpr uint32_t kSelectRows = 16;   // blocks of queries to a workgroup
 // D16: channels / 16, rounded up; kValues: scores of a row per lane.
 // Measured: 24 heads x 1024 x 1024 blocks x 128 channels 424 us with doubles in LDS and a search bit by bit on four wavefronts.
 template <int D16, int kValues>
-__global__ __launch_bounds__(kSelectThreads) __attribute__((amdgpu_waves_per_eu(kValues > 16 ? 2 : 4)))
+__global__ __launch_bounds__(select_threads(kValues)) __attribute__((amdgpu_waves_per_eu(kValues > 16 ? 2 : 4)))
 void select_blocks_kernel(const double* means, const int32_t* lens, int32_t* chosen, float* scores, uint32_t top, uint32_t n_q, uint32_t dim,
                           uint32_t row_tiles, uint32_t n_workgroups, BlockShape s)
 {
-    constexpr uint32_t kWaves = kSelectThreads / 64, kRowDoubles = 16 * D16, kPieces = kRowDoubles / 2;
+    constexpr int kSets = select_sets(kValues);
+    constexpr uint32_t kThreads = select_threads(kValues), kWaves = kThreads / 64, kSelectRows = 16 * kSets, kRowDoubles = 16 * D16, kPieces = kRowDoubles / 2;
     __shared__ __align__(16) uint32_t order[kSelectRows][64 * kValues];
     __shared__ __align__(16) double queries[kSelectRows * kRowDoubles];   // 16-byte piece p of row r at p ^ (r % 8)
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -127,7 +130,7 @@ void select_blocks_kernel(const double* means, const int32_t* lens, int32_t* cho
     const uint32_t rows = min(s.blocks_q - block0, kSelectRows);
     const double* mq = means + ((size_t)g * s.blocks_q + block0) * dim;
     const double* mk = means + ((size_t)n_q + (size_t)gk * s.blocks_k) * dim;
-    for (uint32_t i = threadIdx.x; i < kSelectRows * kPieces; i += kSelectThreads) {
+    for (uint32_t i = threadIdx.x; i < kSelectRows * kPieces; i += kThreads) {
         const uint32_t r = i / kPieces, p = i - r * kPieces;
         select_f64x2 w = {0.0, 0.0};
         if (r < rows && 2u * p < dim) w = *reinterpret_cast<const select_f64x2*>(mq + (size_t)r * dim + 2u * p);
@@ -139,8 +142,8 @@ void select_blocks_kernel(const double* means, const int32_t* lens, int32_t* cho
     for (uint32_t t = wave; 16u * t < n; t += kWaves) {
         const double* row = mk + (size_t)(16u * t + r) * dim;
         const bool there = 16u * t + r < n;
-        select_f64x4 acc = {0, 0, 0, 0};
-        constexpr int kChunks = D16 > 6 ? (D16 + 1) / 2 : D16;   // read at a time (128 registers hold no 8)
+        select_f64x4 acc[kSets] = {};
+        constexpr int kChunks = D16 > 4 ? (D16 + 1) / 2 : D16;   // read at a time (128 registers hold no 8)
 #pragma unroll 1
         for (int c0 = 0; c0 < D16; c0 += kChunks) {
             select_f64x2 keys[2 * kChunks];
@@ -154,14 +157,19 @@ void select_blocks_kernel(const double* means, const int32_t* lens, int32_t* cho
             for (int i = 0; i < 2 * kChunks; ++i) {
                 if (D16 % kChunks && c0 + i / 2 >= D16) break;
                 const uint32_t p = 8u * (c0 + i / 2) + k4 / 2u + i % 2;
-                const select_f64x2 a = *reinterpret_cast<const select_f64x2*>(queries + r * kRowDoubles + 2u * (p ^ (r & 7u)));
-                acc = __builtin_amdgcn_mfma_f64_16x16x4f64(a[0], keys[i][0], acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f64_16x16x4f64(a[1], keys[i][1], acc, 0, 0, 0);
+#pragma unroll
+                for (int u = 0; u < kSets; ++u) {
+                    const select_f64x2 a = *reinterpret_cast<const select_f64x2*>(queries + (16u * u + r) * kRowDoubles + 2u * (p ^ (r & 7u)));
+                    acc[u] = __builtin_amdgcn_mfma_f64_16x16x4f64(a[0], keys[i][0], acc[u], 0, 0, 0);
+                    acc[u] = __builtin_amdgcn_mfma_f64_16x16x4f64(a[1], keys[i][1], acc[u], 0, 0, 0);
+                }
             }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)   // accumulator i: row lane / 16 + 4 i, column lane % 16
-            order[(lane >> 4) + 4u * i][16u * t + r] = there ? order_of((float)acc[i]) : 0;
+        for (int i = 0; i < 4; ++i) {   // accumulator i: row lane / 16 + 4 i, column lane % 16
+#pragma unroll
+            for (int u = 0; u < kSets; ++u) order[16u * u + (lane >> 4) + 4u * i][16u * t + r] = there ? order_of((float)acc[u][i]) : 0;
+        }
     }
     __syncthreads();
     // ---- the largest of every row

@@ -128,14 +128,15 @@ int fb4_select_key_blocks(const void* q, const void* k, int64_t batch, int heads
     else if (pieces > 4) FB4_MEANS(8);
     else FB4_MEANS(4);
 #undef FB4_MEANS
-    const uint32_t row_tiles = (s.blocks_q + kSelectRows - 1) / kSelectRows;
+    const int values = s.blocks_k <= 128 ? 2 : s.blocks_k <= 512 ? 8 : s.blocks_k <= 1024 ? 16 : 32;
+    const uint32_t rows = 16 * select_sets(values), row_tiles = (s.blocks_q + rows - 1) / rows;
     const dim3 sgrid((unsigned)(batch * heads * row_tiles));
-#define FB4_SELECT_LAUNCH(d, v) launch(select_blocks_kernel<d, v>, sgrid, dim3(kSelectThreads), 0, st, means, lens, blocks, scores, (uint32_t)top, (uint32_t)n_q, (uint32_t)dim, row_tiles, sgrid.x, s)
+#define FB4_SELECT_LAUNCH(d, v) launch(select_blocks_kernel<d, v>, sgrid, dim3(select_threads(v)), 0, st, means, lens, blocks, scores, (uint32_t)top, (uint32_t)n_q, (uint32_t)dim, row_tiles, sgrid.x, s)
 #define FB4_SELECT_CASE(d)                                       \
     case d:                                                      \
-        if (s.blocks_k <= 128) FB4_SELECT_LAUNCH(d, 2);          \
-        else if (s.blocks_k <= 512) FB4_SELECT_LAUNCH(d, 8);     \
-        else if (s.blocks_k <= 1024) FB4_SELECT_LAUNCH(d, 16);   \
+        if (values == 2) FB4_SELECT_LAUNCH(d, 2);                \
+        else if (values == 8) FB4_SELECT_LAUNCH(d, 8);           \
+        else if (values == 16) FB4_SELECT_LAUNCH(d, 16);         \
         else FB4_SELECT_LAUNCH(d, 32);                           \
         break;
     switch ((dim + 15) / 16) {
