@@ -280,6 +280,7 @@ constexpr uint32_t kAllBlocks = 0xFFFFFFFFu;   // no list (FB4_ALL_BLOCKS in 32 
 
 typedef float attn_f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 attn_bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t attn_u32x4 __attribute__((ext_vector_type(4)));
 typedef short attn_s16x4 __attribute__((ext_vector_type(4)));
 
 struct AttentionShape {
@@ -607,9 +608,9 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
         add_values(last_values, kGroups - 1, [](int) {});   // of the last group
     }
     sum += __shfl_xor(sum, 32);
-    if (row >= end_q) return;
     const size_t at_row = (size_t)g * s.tokens_q + row;
     if (kSplit) {
+        if (row >= end_q) return;
         const size_t n_rows = (size_t)(s.n_workgroups / s.parts / s.blocks_q) * s.tokens_q;
         float* to = reinterpret_cast<float*>(out) + (part * n_rows + at_row) * (kP * 8);
 #pragma unroll
@@ -624,20 +625,34 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
         return;
     }
     const float inverse = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;   // (a NaN stays; no key: zeros)
-    uint16_t* to = out + ((size_t)b * so.batch + (size_t)h * so.head + (size_t)row * so.token) * 8u;
+    if (lse && half == 0 && row < end_q) lse[at_row] = sum == 0.0f ? -__builtin_inff() : 0.69314718055994530942f * (off + __builtin_amdgcn_logf(sum));
+    // Rows through LDS, 16 bytes to a lane: from the accumulators a store is 32 rows' 16 bytes each (17 x 16 x 1350 x 72: 11 of 100 us).
+    // Every wavefront has a buffer of its own, once all are done with the tiles.
+    __syncthreads();
+    uint8_t* mine = wave == 0 ? lds_k0 : wave == 1 ? lds_k1 : wave == 2 ? lds_v0 : lds_v1;
 #pragma unroll
     for (int d = 0; d < kTiles; ++d) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t c = 32u * d + 8u * i + 4u * half;
             uint32_t w[2];
 #pragma unroll
             for (int x = 0; x < 2; ++x)
                 w[x] = __builtin_bit_cast(uint32_t, __builtin_convertvector((attn_f32x2{o[d][4 * i + 2 * x] * inverse, o[d][4 * i + 2 * x + 1] * inverse}), attn_bf16x2));
-            if (c < kP * 8u) *reinterpret_cast<uint2*>(to + c) = make_uint2(w[0], w[1]);
+            // channels 32 d + 8 i + 4 half ..: half of piece 4 d + i
+            if (4 * d + i < kP) *reinterpret_cast<uint2*>(mine + col * kRowBytes + (((4u * d + i) ^ k_swz) << 4) + 8u * half) = make_uint2(w[0], w[1]);
         }
     }
-    if (lse && half == 0) lse[at_row] = sum == 0.0f ? -__builtin_inff() : 0.69314718055994530942f * (off + __builtin_amdgcn_logf(sum));
+    __builtin_amdgcn_wave_barrier();
+    uint16_t* to = out + ((size_t)b * so.batch + (size_t)h * so.head) * 8u;
+#pragma unroll
+    for (int i = 0; i < (kP + 1) / 2; ++i) {
+        const uint32_t j = 64u * i + lane, r = j / kP, p16 = j - r * kP, at = first_q + wave * 32u + r;
+        if (r >= 32u || at >= end_q) break;
+        const attn_u32x4 w = *reinterpret_cast<const attn_u32x4*>(mine + r * kRowBytes + ((p16 ^ key_place(r)) << 4));
+        attn_u32x4* place = reinterpret_cast<attn_u32x4*>(to + ((size_t)at * so.token + p16) * 8u);
+        if (kP % 8 == 0) __builtin_nontemporal_store(w, place);   // (whole lines; 72 channels' parts of lines are better kept: 99.6 / 102.8 us)
+        else *place = w;
+    }
 }
 
 #undef FB4_INLINE
