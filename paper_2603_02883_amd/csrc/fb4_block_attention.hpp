@@ -335,7 +335,8 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
     constexpr uint32_t kG = kP % 16 == 0 ? 16 : kP % 8 == 0 ? 8 : kP % 4 == 0 ? 4 : kP % 2 == 0 ? 2 : 1;
     // Each buffer an array of its own: the compiler then sees that the loads into one do not touch the reads from another.  (64 bytes
     // more: zeros for the keys, what reads of unused channels may touch for the values)
-    __shared__ __align__(1024) uint8_t lds_k0[kBytes + 64], lds_k1[kBytes + 64], lds_v0[kBytes + 64], lds_v1[kBytes + 64];
+    constexpr uint32_t kPadK = kP % 2 ? 64 : 0, kPadV = kP % 4 ? 64 : 0;
+    __shared__ __align__(1024) uint8_t lds_k0[kBytes + kPadK], lds_k1[kBytes + kPadK], lds_v0[kBytes + kPadV], lds_v1[kBytes + kPadV];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t half = lane >> 5, col = lane & 31u;
     const uint32_t pos = xcd_local_position(blockIdx.x, s.n_workgroups);
@@ -454,15 +455,20 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
     const uint32_t v_r = 4u * half + (lane & 15u) / 4u;
     const uint32_t v_swz = value_place(v_r);   // (8 and 16 rows further the same)
     const uint32_t v_piece = 2u * ((lane >> 4) & 1u) + ((lane & 3u) >> 1), v_at = v_r * kRowBytes + 8u * (lane & 1u);
+    uint32_t k_at[kSteps], v_place[kTiles];   // (whole, so that a buffer and a group are constants in the reads)
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) k_at[i] = k_row + (((2u * i + half) ^ k_swz) << 4);
+#pragma unroll
+    for (int d = 0; d < kTiles; ++d) v_place[d] = v_at + (((4u * d + v_piece) ^ v_swz) << 4);
     auto key_operand = [&](const uint8_t* keys, int group, int i) FB4_INLINE {
-        const uint32_t at = 32u * group * kRowBytes + k_row + (((2u * i + half) ^ k_swz) << 4);
+        const uint32_t at = k_at[i] + 32u * group * kRowBytes;
         return __builtin_bit_cast(mfma_bf16x8, *reinterpret_cast<const uint4*>(keys + ((kP % 2 && i == kSteps - 1 && half) ? kBytes : at)));
     };
     auto value_operand = [&](const uint8_t* values, int group, int i, int d) FB4_INLINE {
         // lane t of 16 reads 8 bytes of row t / 4 and gets column t of the four rows.  (Channels past the row: what lies behind, in
         // accumulators that nobody reads)
         typedef __attribute__((address_space(3))) attn_s16x4* lds_s16x4;
-        const uint8_t* from = values + (32u * group + 16u * i) * kRowBytes + v_at + (((4u * d + v_piece) ^ v_swz) << 4);
+        const uint8_t* from = values + v_place[d] + (32u * group + 16u * i) * kRowBytes;
         const uint2 v0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(from)));
         const uint2 v1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(from + 8u * kRowBytes)));
         return __builtin_bit_cast(mfma_bf16x8, make_uint4(v0.x, v0.y, v1.x, v1.y));
@@ -567,14 +573,14 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
     if (now.n) {
         // the zeroed pieces; values for the step before the first group, whose weights are 0
         if (kP % 2 && threadIdx.x < 8) reinterpret_cast<uint32_t*>((threadIdx.x & 4u ? lds_k1 : lds_k0) + kBytes)[threadIdx.x & 3u] = 0;
-        for (uint32_t i = threadIdx.x; i < kBytes / 16 + 4; i += 64 * kWaves) *reinterpret_cast<uint4*>(lds_v1 + 16u * i) = make_uint4(0, 0, 0, 0);
+        for (uint32_t i = threadIdx.x; i < (kBytes + kPadV) / 16; i += 64 * kWaves) *reinterpret_cast<uint4*>(lds_v1 + 16u * i) = make_uint4(0, 0, 0, 0);
         landed();
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_operand(lds_k0, 0, i), qf[i], sc, 0, 0, 0);
-        // A tile; its keys and values in k_now and v_now, the next one's keys in k_then, the previous one's values in v_then, whose
-        // place the next one's take.  False: it was the last.
+        // A tile from its last group on, and the next one's first; its keys and values in k_now and v_now, the next one's keys in k_then,
+        // the previous one's values in v_then, whose place the next one's take.  False: it was the last.  (From a wait on, so that
+        // nothing is in flight where the loop comes round: the compiler knows less there and would wait at the first read)
         auto tile = [&](mfma_f32x16& s_now, mfma_f32x16& s_then, uint8_t* k_now, uint8_t* k_then, uint8_t* v_now, uint8_t* v_then) FB4_INLINE {
-            if (kGroups == 2) step(s_now, s_then, 0, now.n, v_then, 1, k_now, 1, [](int) {});
             landed();
 #pragma unroll
             for (int r = 0; r < kReady; ++r) get_ready(kGroups == 2 ? v_now : v_then, 0, r);
@@ -589,11 +595,14 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
             }
             now = then;
             then = after;
-            return now.n > 0;
+            if (now.n == 0) return false;
+            if (kGroups == 2) step(s_now, s_then, 0, now.n, v_now, 1, k_then, 1, [](int) {});
+            return true;
         };
         const uint8_t* last_values;
 #pragma unroll
         for (int r = 0; r < kReady; ++r) get_ready(lds_v1, kGroups - 1, r);
+        if (kGroups == 2) step(sc, sd, 0, now.n, lds_v1, 1, lds_k0, 1, [](int) {});
         for (;;) {
             last_values = lds_v0;
             if (!tile(sc, sd, lds_k0, lds_k1, lds_v0, lds_v1)) break;
@@ -657,52 +666,63 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
 
 #undef FB4_INLINE
 
-// The parts of a row's list meet: accumulators and sums relative to the parts' own references (powers of
-// two; -Inf: no key).  Workspace: float [parts][rows][dim], then
-// {reference, sum} [parts][rows].  A workgroup per row: eight parts at a time, four channels to a thread, so that a row waits for few
-// reads one behind the other (48 rows x 21 parts x 128 channels 20.8 us with a wavefront that walks over the parts).
+// The parts of a row's list meet: accumulators and sums relative to the parts' own references (powers of two; -Inf: no key).
+// Workspace: float [parts][rows][dim], then {reference, sum} [parts][rows].  32 lanes, four channels each, take a row's parts one after
+// the other, four reads ahead, eight rows to a workgroup; of many parts (kMany) a workgroup's eight sets of lanes take every eighth
+// and meet in LDS, so that a row waits for few reads one behind the other (48 rows x 21 parts x 128 channels 20.8 us with one walk
+// over the parts, 4.1 so; 25600 rows x 2 parts x 72 channels 27 us so).
+template <bool kMany>
 __global__ __launch_bounds__(256) void join_parts_kernel(const float* workspace, const int32_t* lens, uint16_t* out, float* lse, TensorStrides so,
                                                          uint32_t parts, uint32_t n_rows, uint32_t tokens_q, uint32_t heads, uint32_t dim)
 {
-    __shared__ float4 meet[8][32];
-    const uint32_t lane = threadIdx.x & 63, at = blockIdx.x, c = 4u * (threadIdx.x & 31u), sub = threadIdx.x >> 5;
+    __shared__ float4 meet[kMany ? 8 : 1][32];
+    const uint32_t l = threadIdx.x & 31u, set = threadIdx.x >> 5, c = 4u * l;
+    const uint32_t at = kMany ? blockIdx.x : min(blockIdx.x * 8u + set, n_rows - 1u);   // (a set past the last row does its work again)
+    const uint32_t first = kMany ? set : 0u, step = kMany ? 8u : 1u;
     const uint32_t g = at / tokens_q, row = at - g * tokens_q, b = g / heads, h = g - b * heads;
-    if (row >= length_of(lens, b, 0, tokens_q)) return;
+    const bool live = row < length_of(lens, b, 0, tokens_q);
     const float2* state = reinterpret_cast<const float2*>(workspace + (size_t)parts * n_rows * dim) + at;
     float most = -__builtin_inff(), sum = 0.0f;
-    for (uint32_t p = lane; p < parts; p += 64) most = fmaxf(most, state[(size_t)p * n_rows].x);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
-    const float base = most == -__builtin_inff() ? 0.0f : most;
-    for (uint32_t p = lane; p < parts; p += 64) {
-        const float2 st = state[(size_t)p * n_rows];
-        sum = fmaf(st.y, __builtin_amdgcn_exp2f(st.x - base), sum);
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (live) {   // (a row that no part wrote is not read)
+        for (uint32_t p = l; p < parts; p += 32) most = fmaxf(most, state[(size_t)p * n_rows].x);
     }
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (c < dim) {
+    for (int d = 1; d < 32; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+    const float base = most == -__builtin_inff() ? 0.0f : most;
+    if (live) {
+        for (uint32_t p = l; p < parts; p += 32) {
+            const float2 st = state[(size_t)p * n_rows];
+            sum = fmaf(st.y, __builtin_amdgcn_exp2f(st.x - base), sum);
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) sum += __shfl_xor(sum, d);
+    if (live && c < dim) {
 #pragma unroll 4
-        for (uint32_t p = sub; p < parts; p += 8) {
+        for (uint32_t p = first; p < parts; p += step) {
             const float w = __builtin_amdgcn_exp2f(state[(size_t)p * n_rows].x - base);
             const float4 x = *reinterpret_cast<const float4*>(workspace + ((size_t)p * n_rows + at) * dim + c);
             o = make_float4(fmaf(x.x, w, o.x), fmaf(x.y, w, o.y), fmaf(x.z, w, o.z), fmaf(x.w, w, o.w));
         }
     }
-    meet[sub][threadIdx.x & 31u] = o;
-    __syncthreads();
-    if (sub > 0) return;
+    if (kMany) {
+        meet[set][l] = o;
+        __syncthreads();
+        if (set > 0) return;
 #pragma unroll
-    for (int i = 1; i < 8; ++i) {
-        const float4 x = meet[i][threadIdx.x];
-        o = make_float4(o.x + x.x, o.y + x.y, o.z + x.z, o.w + x.w);
+        for (int i = 1; i < 8; ++i) {
+            const float4 x = meet[i][l];
+            o = make_float4(o.x + x.x, o.y + x.y, o.z + x.z, o.w + x.w);
+        }
     }
+    if (!live) return;
     const float inverse = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
     uint16_t* to = out + ((size_t)b * so.batch + (size_t)h * so.head + (size_t)row * so.token) * 8u;
     const attn_bf16x2 lo = __builtin_convertvector((attn_f32x2{o.x * inverse, o.y * inverse}), attn_bf16x2);
     const attn_bf16x2 hi = __builtin_convertvector((attn_f32x2{o.z * inverse, o.w * inverse}), attn_bf16x2);
     if (c < dim) *reinterpret_cast<uint2*>(to + c) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
-    if (lse && threadIdx.x == 0) lse[at] = sum == 0.0f ? -__builtin_inff() : 0.69314718055994530942f * (base + __builtin_amdgcn_logf(sum));
+    if (lse && l == 0) lse[at] = sum == 0.0f ? -__builtin_inff() : 0.69314718055994530942f * (base + __builtin_amdgcn_logf(sum));
 }
 
 }  // namespace fb4
