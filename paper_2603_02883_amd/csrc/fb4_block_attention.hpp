@@ -400,12 +400,12 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
     };
     auto fetch = [&](const Tile& t, const uint8_t* base, const uint32_t* from, uint32_t row_bytes, uint8_t* buffer, bool values) FB4_INLINE {
-        if (t.n == (uint32_t)kKeys && kPositions % 64 == 0) {
+        if (t.n == (uint32_t)kKeys) {
 #pragma unroll
             for (int i = 0; i < kMine; ++i) {
                 const uint32_t load = i * kWaves + wave;
                 const uint8_t* at = kRegular ? base + (size_t)(i * (64 * kWaves / kP)) * row_bytes + from[0] : base + from[i % kPlaces];
-                if ((i + 1) * kWaves <= (int)kLoads || load < kLoads) copy(at, buffer + __builtin_amdgcn_readfirstlane(load * 1024u));
+                if ((i + 1) * kWaves * 64 <= (int)kPositions || 64u * load + lane < kPositions) copy(at, buffer + __builtin_amdgcn_readfirstlane(load * 1024u));
             }
         } else if (t.n) {
 #pragma unroll 1

@@ -41,7 +41,7 @@ int check_blocks(int64_t batch, int heads, int heads_k, int64_t tokens_q, int64_
 // keys (about 1 us).  A compute unit with two pairs of wavefronts takes 0.7 of its rounds one after the other, three 2.1, four 2.8; a
 // workgroup's start and end cost about a tile, the join two and 2 ps per row, part and channel.  At most four pairs of wavefronts
 // for each of 256 compute units.  Over 98 calls of 8 to 400 blocks and 2 to 256 tiles the choice is 1.8 % slower than the best of 1 to 64
-// parts in the mean (512 / n parts wherever n <= 256: 6.6 %).  8 single queries of 128 channels, 256 tiles: 64 parts 18.8 us, one 350;
+// parts in the mean, over 72 of other shapes 3.6 % (512 / n parts wherever n <= 256: 6.6 % over the first).  8 single queries of 128 channels, 256 tiles: 64 parts 18.8 us, one 350;
 // 200 blocks of 64 queries of 72 channels: 64 tiles three parts 56.0 us, one 75.6; 8 tiles one part 13.5 us, two 17.3.
 int64_t attention_parts(int64_t n, int64_t rows, int64_t dim, int64_t top, const BlockShape& s)
 {
