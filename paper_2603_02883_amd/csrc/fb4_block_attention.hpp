@@ -111,7 +111,9 @@ constexpr int select_threads(int values) { return 512 * select_sets(values); }
 // products.  Rounding keeps the order but for what becomes equal, so the fp32 values decide unless the border falls between
 // equal ones; those blocks' scores are then formed again in double.
 // D16: channels / 16, rounded up; kValues: scores of a row per lane.
-// Measured: 24 heads x 1024 x 1024 blocks x 128 channels 424 us with doubles in LDS and a search bit by bit on four wavefronts.
+// Measured, means included (24 heads x 1024 x 1024 blocks x 128 channels): 353 us, of which the means' kernel 148 at 5.5 TB/s; 424
+// with doubles in LDS and a search bit by bit on four wavefronts.  The MFMAs alone are 82 us; the rest is reads of the keys' means from
+// L2 and the search.
 template <int D16, int kValues>
 __global__ __launch_bounds__(select_threads(kValues)) __attribute__((amdgpu_waves_per_eu(kValues > 16 ? 2 : 4)))
 void select_blocks_kernel(const double* means, const int32_t* lens, int32_t* chosen, float* scores, uint32_t top, uint32_t n_q, uint32_t dim,
@@ -429,10 +431,10 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
     Tile then = now.n ? next_tile() : Tile{0, 0};
     fetch_k(then, lds_k1);
     if (kGroups == 2) fetch_v(now, lds_v0);
-    // ---- this wavefront's queries as B operands
+    // ---- this wavefront's queries as B operands (past the last one that one: a padded row's values touch no other's rounding)
     mfma_bf16x8 qf[kSteps];
     {
-        const uint16_t* from = q + ((size_t)g * s.tokens_q + min(row, s.tokens_q - 1u)) * (kP * 8);
+        const uint16_t* from = q + ((size_t)g * s.tokens_q + min(row, end_q - 1u)) * (kP * 8);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             uint4 w = make_uint4(0, 0, 0, 0);

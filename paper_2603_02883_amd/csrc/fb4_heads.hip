@@ -215,8 +215,8 @@ int fb4_block_attention(const void* q, const void* k, const void* v, const int64
 #undef FB4_ATTENTION_CASE
 #undef FB4_ATTENTION_LAUNCH
     if (parts > 1) {
-        const int64_t rows = batch * heads * tokens_q;   // (at most 512 blocks)
-        const bool many = parts > 8 && rows <= 4096;
+        const int64_t rows = batch * heads * tokens_q;   // (at most 512 blocks; of more than eight parts 113)
+        const bool many = parts > 8;
         launch(many ? join_parts_kernel<true> : join_parts_kernel<false>, dim3((unsigned)(many ? rows : (rows + 7) / 8)), dim3(256), 0, st,
                static_cast<const float*>(workspace), lens, static_cast<uint16_t*>(out), lse, so, (uint32_t)parts, (uint32_t)rows, s.tokens_q, (uint32_t)heads,
                (uint32_t)dim);

@@ -452,6 +452,119 @@ def test_two_streams_and_graphs(F):
         assert all(torch.equal(g, got[-1]) for g in got) and all(torch.equal(x, lists[-1]) for x in lists)
 
 
+@pytest.mark.parametrize("dim", [40, 64, 72, 104, 128])
+def test_padding_leaves_no_trace(F, dim):
+    """Rows behind a sequence's end change no bit of the others, not even by the rounding of what a wavefront shares."""
+    lens = torch.tensor([[70, 200], [129, 65], [1, 333]], dtype=torch.int32, device="cuda")
+    got = []
+    for fill in (0.0, 3e30, math.inf, math.nan):
+        q, k, v = rand(3, 2, 150, dim, seed=100), rand(3, 2, 333, dim, seed=101), rand(3, 2, 333, dim, seed=102)
+        for i, (a, b) in enumerate(lens.tolist()):
+            q[i, :, a:], k[i, :, b:], v[i, :, b:] = fill, fill, fill
+        for bq, bk in ((64, 64), (128, 128)):
+            blocks, scores = F.fb4_select_key_blocks(q, k, 2, bq, bk, lens, want_scores=True)
+            got.append((blocks, scores.nan_to_num(-1.0), *F.fb4_block_attention(q, k, v, blocks, None, bq, bk, lens, want_lse=True),
+                        F.fb4_block_attention(q, k, v, None, None, bq, bk, lens)))
+    for i in range(2, len(got)):
+        assert all(torch.equal(a, b) for a, b in zip(got[i], got[i % 2])), i
+
+
+@pytest.mark.parametrize("block_q", [64, 128])
+@pytest.mark.parametrize("dim", [40, 72, 104, 128])
+def test_shared_lists(F, dim, block_q):
+    """Lists long enough for several workgroups each: ragged sequences, entries without a key in some parts or all."""
+    lens = torch.tensor([[200, 4000], [77, 2049], [1, 64], [200, 0]], dtype=torch.int32, device="cuda")
+    q, k, v = rand(4, 2, 200, dim, seed=110), rand(4, 1, 4000, dim, seed=111), rand(4, 1, 4000, dim, seed=112)
+    blocks = -(-200 // block_q)
+    assert F.binding._lib.fb4_block_attention_workspace(4, 2, 1, 200, 4000, dim, F.binding.ALL_BLOCKS, block_q, 64) > 0
+    check_attention(F, q, k, v, None, None, block_q, 64, lens)
+    lists = some_blocks((4, 2, blocks, 40), 63, 7)
+    lists[0, 0, 0, :25] = -1
+    lists[0, 1, 0, 5:] = -1
+    lists[1, 0] = -1
+    assert F.binding._lib.fb4_block_attention_workspace(4, 2, 1, 200, 4000, dim, 40, block_q, 64) > 0
+    check_attention(F, q, k, v, lists, None, block_q, 64, lens)
+
+
+def test_parts_of_many_rows(F):
+    """On both sides of the eight parts from which a row's join is a workgroup's."""
+    for tokens, dim, more in ((2368, 8, True), (2368, 64, False)):
+        q, k, v = rand(1, 2, tokens, dim, seed=120), rand(1, 2, 640, dim, seed=121), rand(1, 2, 640, dim, seed=122)
+        g = torch.Generator()
+        g.manual_seed(dim)
+        lists = torch.randint(-1, 10, (1, 2, tokens // 64, 40), generator=g).int().cuda()
+        size = F.binding._lib.fb4_block_attention_workspace(1, 2, 2, tokens, 640, dim, 40, 64, 64)
+        assert size > 0 and (size > 8 * 2 * tokens * (dim + 2) * 4) == more
+        check_attention(F, q, k, v, lists)
+
+
+def test_given_workspaces(F):
+    q, k, v = rand(1, 2, 1, 64, seed=130), rand(1, 2, 5000, 64, seed=131), rand(1, 2, 5000, 64, seed=132)
+    lib = F.binding._lib
+    size = lib.fb4_block_attention_workspace(1, 2, 2, 1, 5000, 64, F.binding.ALL_BLOCKS, 64, 64)
+    held = torch.full((size + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+    got = F.fb4_block_attention(q, k, v, None, None, 64, 64, workspace=held[:size])
+    assert torch.equal(got, F.fb4_block_attention(q, k, v, None, None, 64, 64)) and (held[size:] == 0xA5).all()
+    with pytest.raises(F.Fb4Error):
+        F.fb4_block_attention(q, k, v, None, None, 64, 64, workspace=held[:size - 1])
+    with pytest.raises(F.Fb4Error):
+        F.fb4_block_attention(q, k, v, None, None, 64, 64, workspace=held[8:])
+    size = lib.fb4_select_key_blocks_workspace(1, 2, 2, 1, 5000, 64, 64, 64)
+    held = torch.full((size + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+    lists = F.fb4_select_key_blocks(q, k, 5, 64, 64, workspace=held[:size])
+    assert torch.equal(lists, F.fb4_select_key_blocks(q, k, 5, 64, 64)) and (held[size:] == 0xA5).all()
+    with pytest.raises(F.Fb4Error):
+        F.fb4_select_key_blocks(q, k, 5, 64, 64, workspace=held[:size - 1])
+
+
+def test_both_bindings_answer_alike(F):
+    """The calls through the C module and through ctypes: the same results, the same refusals."""
+    B = F.binding
+    if B._heads_call is B.HeadsCall:
+        pytest.skip("no C module")
+    qkv = rand(2, 130, 6, 64, seed=140).permute(0, 2, 1, 3)
+    q, k, v = qkv[:, :2].contiguous(), qkv[:, 2:4].contiguous(), qkv[:, 4:]
+    lens = torch.tensor([[130, 100], [70, 130]], dtype=torch.int32, device="cuda")
+    pos = torch.arange(130, device="cuda", dtype=torch.int32).view(1, 130, 1)
+    freqs = 50.0 ** (-torch.arange(32, device="cuda", dtype=torch.float64) / 32)
+    calls = [lambda: F.fb4_qk_norm_rope(qkv[:, :2], qkv[:, 2:4], pos, freqs, (32,)), lambda: F.fb4_qk_norm_rope(q, None, None, None, ()),
+             lambda: F.fb4_qk_norm_rope(q, k, pos, freqs, (8, 24)), lambda: F.fb4_qk_norm_rope(q, k.float(), pos, freqs, (32,)),
+             lambda: F.fb4_qk_norm_rope(q, k, pos.long(), freqs, (32,)), lambda: F.fb4_qk_norm_rope(q, k, pos, freqs[:31], (32,)),
+             lambda: F.fb4_qk_norm_rope(q, k, pos, freqs, (32,), gamma_q=freqs.float()), lambda: F.fb4_qk_norm_rope(q, k, pos, freqs, (32,), pairing=2),
+             lambda: F.fb4_qk_norm_rope(q.transpose(2, 3), None, None, None, ()), lambda: F.fb4_qk_norm_rope(q, k, pos, freqs, (32,), eps=-1.0)]
+    for bq, bk in ((64, 64), (128, 64)):
+        lists = F.fb4_select_key_blocks(q, k, 2, bq, bk, lens)
+        calls += [lambda bq=bq, bk=bk: F.fb4_select_key_blocks(q, k, 2, bq, bk, lens, want_scores=True),
+                  lambda bq=bq, bk=bk, x=lists: F.fb4_block_attention(q, k, v, x, None, bq, bk, lens, want_lse=True),
+                  lambda bq=bq, bk=bk: F.fb4_block_attention(q, k, v, None, 0.3, bq, bk)]
+    calls += [lambda: F.fb4_select_key_blocks(q, k, 2, 32, 64), lambda: F.fb4_select_key_blocks(qkv[:, :2], k, 2, 64, 64),
+              lambda: F.fb4_select_key_blocks(q, k, 2, 64, 64, lens[:1]), lambda: F.fb4_select_key_blocks(q, k[:1], 2, 64, 64),
+              lambda: F.fb4_select_key_blocks(q, k, 2, 64, 64, lens.long()), lambda: F.fb4_select_key_blocks(q, k, -1, 64, 64),
+              lambda: F.fb4_block_attention(q, k, v[:, :, :129], None, 1.0, 64, 64), lambda: F.fb4_block_attention(q, k, v.transpose(2, 3), None, 1.0, 64, 64),
+              lambda: F.fb4_block_attention(q, k, v, lists.long(), 1.0, 128, 64), lambda: F.fb4_block_attention(q, k, v, lists, 1.0, 64, 64),
+              lambda: F.fb4_block_attention(q, k, v, None, 0.0, 64, 64), lambda: F.fb4_block_attention(q, k, v, None, math.nan, 64, 64),
+              lambda: F.fb4_block_attention(q, k, v, None, 1.0, 64, 96), lambda: F.fb4_block_attention(q, k[:, :1], v, None, 1.0, 64, 64)]
+
+    def answer(call):
+        try:
+            got = call()
+        except F.Fb4Error as e:
+            return str(e)
+        return [x.nan_to_num(-1.0) if x.is_floating_point() else x for x in (got if isinstance(got, tuple) else (got,)) if x is not None]
+    first = [answer(c) for c in calls]
+    module = B._heads_call
+    B._heads_call = B.HeadsCall
+    try:
+        second = [answer(c) for c in calls]
+    finally:
+        B._heads_call = module
+    refused = 0
+    for i, (a, b) in enumerate(zip(first, second)):
+        refused += isinstance(a, str)
+        assert a == b if isinstance(a, str) else all(torch.equal(x, y) for x, y in zip(a, b)), i
+    assert refused == 8 + 6 + 8   # of the three calls, in the order above
+
+
 def test_from_the_projection_to_the_quantizer(F):
     """As a layer uses them: norm and rotation out of the packed projection, salient tokens and key blocks from the same q and k,
     attention over the chosen blocks, its rows through the quantizer."""
