@@ -105,7 +105,7 @@ int fb4_qk_norm_rope(const void* q, const int64_t* q_strides, const void* k, con
     const int64_t each = (heads + most - 1) / most, chunks = (heads + each - 1) / each;
     const RopeShape s = {(uint32_t)tokens, (uint32_t)n, (uint16_t)heads_q, (uint16_t)heads_k, eps, (uint8_t)pieces, {ends[0], ends[1], ends[2]},
                          (uint8_t)n_axes, (uint8_t)pairs, (uint8_t)((norm ? kRopeNorm : 0) | (positions_shared ? kRopeShared : 0)), (uint8_t)chunks};
-    const dim3 grid((unsigned)((runs * chunks + kRopeThreads / 64 - 1) / (kRopeThreads / 64)));
+    const dim3 grid((unsigned)((runs + kRopeThreads / 64 - 1) / (kRopeThreads / 64) * chunks));
 #define FB4_ROPE_LAUNCH(pairing_) launch(qk_norm_rope_kernel<pairing_>, grid, dim3(kRopeThreads), 0, static_cast<hipStream_t>(stream), static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k), static_cast<uint16_t*>(q_out), static_cast<uint16_t*>(k_out), gamma_q, gamma_k, freqs, positions, sq, sk, s)
     if (pairing == FB4_ROPE_ADJACENT) FB4_ROPE_LAUNCH(kRopeAdjacent);
     else FB4_ROPE_LAUNCH(kRopeHalves);

@@ -2,10 +2,15 @@
 //
 // A row is one head of one token: `dim` channels, 16 bytes of which a lane holds; rows stay in registers from the read to
 // the write, so every element is read once and written once.  A wavefront takes as many successive tokens as rows fit its 64
-// lanes (7 of 72 channels, 4 of 128), forms every lane's angles once and goes through the heads with them, four heads' reads
-// ahead of their use.  Tokens side by side, not heads: a head's successive tokens lie side by side in the output, and lines that
-// two wavefronts write in part cost more than lines that they read in part (16 heads of 72 channels of 17 frames, permuted input:
-// 87 us with a token's heads side by side on 9 of 16 lanes).
+// lanes (7 of 72 channels, 4 of 128), forms every lane's angles once and goes through the heads with them, eight heads' reads
+// ahead of their use; a workgroup's wavefronts take successive runs of tokens, and an XCD's workgroups too.  Tokens side by side, not
+// heads: a head's successive tokens lie side by side in the output, and lines that two wavefronts write in part cost more than
+// lines that they read in part (16 heads of 72 channels of 17 frames, permuted input: 87 us with a token's heads side by side on 9 of
+// 16 lanes).
+// Bound by the memory stream.  Measured, queries and keys of 128 channels: 16 x 1024 tokens, 24 + 24 heads of a packed projection
+// 83.7 us (4.8 TB/s, what a copy reaches); 65536 tokens, 24 + 8 heads 195 us (5.5 TB/s; 229 with neighbouring workgroups on different
+// XCDs and four heads ahead); the permuted input above 61.5 us (3.4 TB/s: a row of 144 bytes lies in two lines or three, in channels 36
+// apart, of which others read the rest).
 //   t = positions[a] * freqs[p] in double, brought to (-1/2, 1/2] revolutions there (a far position times a frequency
 //   needs more than fp32's 24 bits), then the hardware's sine and cosine of revolutions (1.2e-7 off at most, measured over
 //   2^18 arguments: a thirtieth of a percent of a bf16 step).
@@ -13,6 +18,8 @@
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include "fb4_mfma.hpp"
 
 namespace fb4 {
 
@@ -42,7 +49,7 @@ typedef uint32_t rope_u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t rope_u32x2 __attribute__((ext_vector_type(2)));
 typedef float rope_f32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kRopeAhead = 4;   // heads whose rows are read before the first of them is used
+constexpr int kRopeAhead = 8;   // heads whose rows are read before the first of them is used
 
 template <int kPairing>
 __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(const uint16_t* q, const uint16_t* k, uint16_t* q_out, uint16_t* k_out,
@@ -50,9 +57,11 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(const uint16
                                                                     const int32_t* positions, RopeStrides sq, RopeStrides sk, RopeShape s)
 {
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t unit = blockIdx.x * (kRopeThreads / 64) + wave;
-    const uint32_t run = __builtin_amdgcn_readfirstlane(unit / s.chunks), chunk = unit - run * s.chunks;
     const uint32_t pieces = s.pieces, rows = 64u / pieces, sub = lane / pieces, l = lane - sub * pieces;
+    constexpr uint32_t kTeam = kRopeThreads / 64;   // successive runs of tokens to a workgroup
+    const uint32_t teams = ((s.n_tokens + rows - 1u) / rows + kTeam - 1u) / kTeam;
+    const uint32_t pos = xcd_local_position(blockIdx.x, teams * s.chunks);
+    const uint32_t team = __builtin_amdgcn_readfirstlane(pos / s.chunks), chunk = pos - team * s.chunks, run = team * kTeam + wave;
     const uint32_t t = run * rows + sub;
     if (run * rows >= s.n_tokens) return;
     const bool live = sub < rows && t < s.n_tokens;
