@@ -35,7 +35,8 @@
  *   - A call made while another device than the handle's is current returns
  *     FB4_ERR_INVALID_ARG.  The entry points without a handle
  *     (fb4_attention_scores, fb4_select_salient_tokens, fb4_seda_assign,
- *     fb4_seda_main_anchor, fb4_seda_main_anchor_3d, fb4_probe_mfma_rate) run on
+ *     fb4_seda_main_anchor, fb4_seda_main_anchor_3d, fb4_qk_norm_rope,
+ *     fb4_select_key_blocks, fb4_block_attention, fb4_probe_mfma_rate) run on
  *     the current device.
  *   - The producer-fused entry points (fb4_layernorm_quantize,
  *     fb4_gelu_quantize) read x as plain IEEE bf16 and hand the quantizer the
