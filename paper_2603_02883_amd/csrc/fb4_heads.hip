@@ -40,9 +40,10 @@ int check_blocks(int64_t batch, int heads, int heads_k, int64_t tokens_q, int64_
 // Parts of a block of queries' list, each with a workgroup of its own: the number with the least cost, in times of one tile of 64
 // keys (about 1 us).  A compute unit with two pairs of wavefronts takes 0.7 of its rounds one after the other, three 2.1, four 2.8; a
 // workgroup's start and end cost about a tile, the join two and 2 ps per row, part and channel.  At most four pairs of wavefronts
-// for each of 256 compute units.  Over 98 calls of 8 to 400 blocks and 2 to 256 tiles the choice is 1.8 % slower than the best of 1 to 64
-// parts in the mean, over 72 of other shapes 3.6 % (512 / n parts wherever n <= 256: 6.6 % over the first).  8 single queries of 128 channels, 256 tiles: 64 parts 18.8 us, one 350;
-// 200 blocks of 64 queries of 72 channels: 64 tiles three parts 56.0 us, one 75.6; 8 tiles one part 13.5 us, two 17.3.
+// for each of 256 compute units.  Over 98 calls of 8 to 400 blocks and 2 to 256 tiles the choice is 1.8 % slower than the best of 1 to
+// 64 parts in the mean, over 72 of other shapes 3.6 % (512 / n parts wherever n <= 256: 6.6 % over the first).  8 single queries of 128
+// channels, 256 tiles: 64 parts 18.8 us, one 350; 200 blocks of 64 queries of 72 channels: 64 tiles three parts 56.0 us, one 75.6; 8 tiles
+// one part 13.5 us, two 17.3.
 int64_t attention_parts(int64_t n, int64_t rows, int64_t dim, int64_t top, const BlockShape& s)
 {
     const int64_t entries = top == FB4_ALL_BLOCKS ? s.blocks_k : top, tiles = s.block_k / 64, pairs = s.block_q / 64;
@@ -99,7 +100,8 @@ int fb4_qk_norm_rope(const void* q, const int64_t* q_strides, const void* k, con
         return FB4_ERR_UNSUPPORTED;
     if (batch > (1 << 25) || tokens > (1 << 25) || batch * tokens > (1 << 25)) return FB4_ERR_UNSUPPORTED;   // (2^26 wavefronts to a launch)
     const int pieces = (int)(dim / 8);
-    // A wavefront per run of tokens; several, each with some of the heads, while there are few tokens.
+    // A wavefront per run of tokens; several, each with some of the heads, while there are few tokens: up to 8192 wavefronts (16384: the
+    // permuted input of fb4_rope.hpp 58.5 us and not 61, the packed one 87 and not 83; 4096: 66 and 82).
     const int64_t n = batch * tokens, rows = 64 / pieces, runs = (n + rows - 1) / rows;
     const int64_t heads = heads_q + heads_k, most = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(heads, 255), 8192 / runs));
     const int64_t each = (heads + most - 1) / most, chunks = (heads + each - 1) / each;
