@@ -325,7 +325,7 @@ constexpr int attention_keys(int pieces, int waves) { return waves == 2 && piece
 // takes m off the exact product, so m's own rounding is one factor in all weights and in their sum; beyond |m| = 2^20 that factor could
 // itself be no small number, and the wavefront goes on with exp2((S - max) c).
 // kSplit: a part of the list; the accumulators, reference and sum go to `out` as floats (see join_parts_kernel).
-// Measured (channels; listed keys): 24 heads x 16384 queries x 2048 of 128: 434-452 us, 0.91-0.95 PFLOP/s, held by the power limit (on zeros
+// Measured (channels; listed keys): 24 heads x 16384 queries x 2048 of 128: 434-463 us by card, 0.89-0.95 PFLOP/s, held by the power limit (on zeros
 // 340) and the loads into LDS (a fifth); 65536 queries, random lists: 1870 us, 11 GB from beyond the L2s; 272 x 1350 queries x 448 of 72:
 // 97 us, a third of it first reads and output; 48 single queries x 8192 of 128: 42 us, 4.7 TB/s.
 template <int kP, int kWaves, bool kSplit>
