@@ -495,6 +495,18 @@ def fb4_seda_main_anchor_3d(scores, frames, grid_h, grid_w, tile_h=4, tile_w=4, 
     return anchors
 
 
+def _output(shape, dtype, device, stream, zeros=False):
+    """An output of a call on `stream`, made there: its fill, and whatever used the memory before, then come before the kernels.  The
+    caller's stream, where results are used, holds the memory too."""
+    make = torch.zeros if zeros else torch.empty
+    if stream is None:
+        return make(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = make(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 def _workspace(size, device, stream):
     """`size` bytes for the length of a call: memory of the stream that the call runs on, which later work there may reuse."""
     if stream is None:
@@ -511,11 +523,11 @@ def fb4_qk_norm_rope(q, k, positions, freqs, axis_pairs, gamma_q=None, gamma_k=N
     None; norm=False: rotation alone.  Returns contiguous (q_out, k_out) of the inputs' shapes."""
     _require(q.is_cuda, "fb4_qk_norm_rope")
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+        q_out = _output(q.shape, torch.bfloat16, q.device, stream)
     if k is None:
         k_out = None
     elif k_out is None:
-        k_out = torch.empty(k.shape, dtype=torch.bfloat16, device=k.device)
+        k_out = _output(k.shape, torch.bfloat16, q.device, stream)
     _check(_heads_call.qk_norm_rope(q, k, positions, freqs, tuple(axis_pairs), gamma_q, gamma_k, float(eps), bool(norm), int(pairing), q_out, k_out, _get_device(),
                               _stream(stream)), "fb4_qk_norm_rope")
     return q_out, k_out
@@ -529,9 +541,9 @@ def fb4_select_key_blocks(q, k, top, block_q=128, block_k=128, lens=None, blocks
         _require(q.dim() == 4 and block_q > 0 and top >= 0, "fb4_select_key_blocks")
         shape = (q.shape[0], q.shape[1], (q.shape[2] + block_q - 1) // block_q, top)
         if blocks is None:
-            blocks = torch.empty(shape, dtype=torch.int32, device=q.device)
+            blocks = _output(shape, torch.int32, q.device, stream)
         if want_scores and scores is None:
-            scores = torch.empty(shape, dtype=torch.float32, device=q.device)
+            scores = _output(shape, torch.float32, q.device, stream)
     s = _stream(stream)
     rc = _heads_call.select_key_blocks(q, k, top, block_q, block_k, lens, blocks, scores, workspace, _get_device(), s)
     if rc > 0:
@@ -549,11 +561,10 @@ def fb4_block_attention(q, k, v, blocks=None, scale=None, block_q=128, block_k=1
     _require(q.is_cuda, "fb4_block_attention")
     if out is None or scale is None or (want_lse and lse is None):
         batch, heads, tokens_q, dim = q.shape
-        empty = torch.empty if lens is None else torch.zeros
         if out is None:
-            out = empty((batch, tokens_q, heads, dim), dtype=torch.bfloat16, device=q.device)
+            out = _output((batch, tokens_q, heads, dim), torch.bfloat16, q.device, stream, zeros=lens is not None)
         if want_lse and lse is None:
-            lse = empty((batch, heads, tokens_q), dtype=torch.float32, device=q.device)
+            lse = _output((batch, heads, tokens_q), torch.float32, q.device, stream, zeros=lens is not None)
         if scale is None:
             _require(dim > 0, "fb4_block_attention")
             scale = dim ** -0.5

@@ -595,3 +595,31 @@ def test_from_the_projection_to_the_quantizer(F):
     codes_ref, meta_ref = O.quantize(DEFAULT_FORMATBOOK, synth.bf16_bits(rows))
     assert np.array_equal(codes.cpu().numpy(), codes_ref) and np.array_equal(meta.cpu().numpy().view(np.uint16), meta_ref)
     luts.free()
+
+
+def test_outputs_of_another_stream_while_the_current_one_is_busy(F):
+    """Outputs that the call makes itself, on a stream that waits for nothing: what the current one still has to do does not reach them."""
+    q, k, v = rand(2, 4, 300, 64, seed=150), rand(2, 2, 500, 64, seed=151), rand(2, 2, 500, 64, seed=152)
+    lens = torch.tensor([[300, 450], [77, 500]], dtype=torch.int32, device="cuda")
+    pos = torch.arange(300, device="cuda", dtype=torch.int32).view(1, 300, 1)
+    freqs = 50.0 ** (-torch.arange(32, device="cuda", dtype=torch.float64) / 32)
+    calls = [lambda **a: F.fb4_block_attention(q, k, v, None, None, 64, 64, lens, want_lse=True, **a),
+             lambda **a: F.fb4_block_attention(q, k, v, None, None, 128, 128, want_lse=True, **a),
+             lambda **a: F.fb4_select_key_blocks(q, k, 3, 64, 64, lens, want_scores=True, **a),
+             lambda **a: F.fb4_qk_norm_rope(q, q, pos, freqs, (32,), **a)]
+    side, x = torch.cuda.Stream(), torch.randn(4096, 4096, device="cuda")
+    for call in calls:
+        ref = call()
+        torch.cuda.synchronize()
+        for _ in range(20):   # (some 30 ms)
+            x @ x
+        got = call(stream=side)
+        side.synchronize()
+        seen = [g.cpu() for g in got]      # behind the current stream's work, which is done with then
+        torch.cuda.synchronize()
+        for a, b, c in zip(got, ref, seen):
+            a, b, c = (t.nan_to_num(-1.0) if t.is_floating_point() else t for t in (a, b, c))
+            assert torch.equal(a, b) and torch.equal(a.cpu(), c)
+    out = F.fb4_block_attention(q, k, v, None, None, 64, 64, lens, stream=side)
+    side.synchronize()
+    assert (out[1, 77:] == 0).all()

@@ -95,3 +95,60 @@ def test_binding_hands_on_no_host_tensors_and_no_other_types():
 
 def test_empty_calls_need_no_pointers_in_the_binding_either():
     assert F.strerror(F.OK) and B.lib().fb4_block_attention_workspace(0, 1, 1, 0, 0, 8, 0, 64, 64) == 0
+
+
+class OnGpu:
+    """As much of a GPU tensor as the binding looks at before it hands it on."""
+    is_cuda, device = True, "cuda:0"
+
+    def __init__(self, *shape):
+        self.shape = shape
+
+    def dim(self):
+        return len(self.shape)
+
+
+def test_outputs_are_made_on_the_stream_that_the_call_runs_on(monkeypatch):
+    """A fill, and whatever used the memory before, come before the kernels only on the kernels' own stream; the caller's may be far
+    behind."""
+    import contextlib
+    from types import SimpleNamespace
+    now, made, handed = ["callers"], [], []
+
+    @contextlib.contextmanager
+    def on(stream):
+        now.append(stream.name)
+        yield
+        now.pop()
+
+    def maker(kind):
+        def make(shape, dtype, device):
+            t = OnGpu(*(shape if isinstance(shape, tuple) else (shape,)))
+            t.made, t.kept_for = (kind, now[-1]), []
+            t.record_stream = t.kept_for.append
+            made.append(t)
+            return t
+        return make
+
+    def call(*args):
+        handed.append(args)
+        return F.OK
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: now[-1])
+    monkeypatch.setattr(torch, "empty", maker("empty"))
+    monkeypatch.setattr(torch, "zeros", maker("zeros"))
+    monkeypatch.setattr(B, "_heads_call", SimpleNamespace(qk_norm_rope=call, select_key_blocks=call, block_attention=call))
+    monkeypatch.setattr(B, "_get_device", lambda: 0)
+    monkeypatch.setattr(B, "_raw_stream", lambda device: 7)
+    side = SimpleNamespace(name="side", cuda_stream=99)
+    q, k, lens = OnGpu(2, 4, 100, 64), OnGpu(2, 2, 300, 64), OnGpu(2, 2)
+    calls = [lambda s: F.fb4_qk_norm_rope(q, k, None, None, (), stream=s), lambda s: F.fb4_select_key_blocks(q, k, 2, want_scores=True, stream=s),
+             lambda s: F.fb4_block_attention(q, k, k, want_lse=True, stream=s), lambda s: F.fb4_block_attention(q, k, k, lens=lens, want_lse=True, stream=s)]
+    for kind, one in zip(("empty", "empty", "empty", "zeros"), calls):
+        for stream, name, handle in ((side, "side", 99), (None, "callers", 7)):
+            made.clear()
+            outs = one(stream)
+            assert len(made) == 2 and all(a is b for a, b in zip(outs, made)) and handed[-1][-1] == handle
+            assert all(t.made == (kind, name) for t in made), [t.made for t in made]
+            # (the memory comes back only when the caller's stream, where the results are used, is done with it too)
+            assert all(t.kept_for == ([] if stream is None else ["callers"]) for t in made)
