@@ -322,8 +322,9 @@ constexpr int attention_keys(int pieces, int waves) { return waves == 2 && piece
 //
 // Weights are exp2(S c - m), c = scale log2 e, m a reference that moves only when a power would pass 2^8: until then the accumulators need
 // not be scaled, and the two half-wavefronts, which hold different keys of the same query, need not meet.  A fused multiply-add
-// takes m off the exact product, so m's own rounding is one factor in all weights and in their sum; beyond |m| = 2^20 that factor could
-// itself be no small number, and the wavefront goes on with exp2((S - max) c).
+// takes m off the exact product, so m's own rounding is one factor in all weights and in their sum, and when m moves they are scaled by the
+// power of the rounded values' difference; beyond |m| = 2^20 that factor could itself be no small number, and the wavefront goes on with
+// exp2((S - max) c).
 // kSplit: a part of the list; the accumulators, reference and sum go to `out` as floats (see join_parts_kernel).
 // Measured (channels; listed keys): 24 heads x 16384 queries x 2048 of 128: 434-463 us by card, 0.89-0.95 PFLOP/s, held by the power limit (on zeros
 // 340) and the loads into LDS (a fifth); 65536 queries, random lists: 1870 us, 11 GB from beyond the L2s; 272 x 1350 queries x 448 of 72:
@@ -522,14 +523,18 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
             }
         });
         if (__any(fmaf(larger, factor, -reference) > 8.0f)) {
+#pragma clang fp contract(off)   // (a rounded product is meant)
             larger = fmaxf(larger, most);
             larger = fmaxf(larger, __shfl_xor(larger, 32));
-            // (of the difference: 1 where the maximum stays)
-            const float shrink = most == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((most - larger) * factor);
+            const float product = larger * factor, fresh = larger == -__builtin_inff() ? 0.0f : product;
+            const bool was_large = large;
+            large = large || __any(fabsf(fresh) > 0x1p20f);
+            // from what the weights so far are relative to: the rounded product, or (large) the exact one
+            const float moved = was_large ? (most - larger) * factor : large ? fmaf(-larger, factor, off) : off - fresh;
+            const float shrink = most == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(moved);
             most = larger;
-            reference = larger * factor;
-            off = larger == -__builtin_inff() ? 0.0f : reference;
-            large = large || __any(fabsf(off) > 0x1p20f);
+            reference = product;
+            off = fresh;
             sum *= shrink;
 #pragma unroll
             for (int d = 0; d < kTiles; ++d) {

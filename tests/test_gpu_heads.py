@@ -623,3 +623,71 @@ def test_outputs_of_another_stream_while_the_current_one_is_busy(F):
     out = F.fb4_block_attention(q, k, v, None, None, 64, 64, lens, stream=side)
     side.synchronize()
     assert (out[1, 77:] == 0).all()
+
+
+# Scores that are exact in fp32, of any size: what a weight is off by does not grow with them.
+def exact_scores(first, second, key_first, key_second, v, scale):
+    """Query i's score of key j is first * key_first[j] + second[i] * key_second[j].  (the scores; the call's first arguments)"""
+    q, k = torch.zeros(1, 1, len(second), 64, dtype=torch.float64), torch.zeros(1, 1, len(key_first), 64, dtype=torch.float64)
+    q[0, 0, :, 0], q[0, 0, :, 1] = first, torch.as_tensor(second, dtype=torch.float64)
+    k[0, 0, :, 0], k[0, 0, :, 1] = torch.as_tensor(key_first, dtype=torch.float64), torch.as_tensor(key_second, dtype=torch.float64)
+    s = q[0, 0] @ k[0, 0].T
+    assert all(torch.equal(x, x.bfloat16().double()) for x in (q, k)) and torch.equal(s, s.float().double()) and scale == float(np.float32(scale))
+    return s, q.bfloat16().cuda(), k.bfloat16().cuda(), v, scale
+
+
+def check_exact_scores(F, s, q, k, v, scale, block_q=64, parts=False):
+    """parts: the list is shared by several workgroups (not where there are as many as 1024 heads)."""
+    if not parts:
+        q = q.expand(1, 1024, -1, -1).contiguous()
+    size = F.binding._lib.fb4_block_attention_workspace(1, q.shape[1], 1, q.shape[2], k.shape[2], 64, F.binding.ALL_BLOCKS, block_q, 64)
+    assert (size > 0) == parts
+    out, lse = F.fb4_block_attention(q, k, v, None, scale, block_q, 64, want_lse=True)
+    assert agree(out, out[:, :, :1], 0) and agree(lse, lse[:, :1], 0)
+    s, v64 = s.cuda() * scale, v[0, 0].double()
+    total = torch.logsumexp(s, -1, keepdim=True)
+    p = torch.softmax(s, -1)
+    # A weight: the power's argument, of which 2^-22 is lost (above 2^-40 of the largest it is below 40), and its result; one
+    # rounding to bf16.  The sum as in attention_reference.
+    weight = 40 * 2.0 ** -22 + 2.0 ** -18 + (s.shape[1] / 32 + 64) * 2.0 ** -24
+    bound = (p @ v64.abs()) * (BF16 + 2 * weight) + BF16 * (p @ v64).abs() * (1 + BF16) + TINY + 2.0 ** -40 * v64.abs().sum(0)
+    right = agree(out[0, :, 0].double(), p @ v64, bound), agree(lse[0, 0].double(), total[:, 0], weight + 2.0 ** -21 * total[:, 0].abs())
+    assert right == (True, True), ((out[0, :, 0].double() - p @ v64).abs() / bound).max()
+
+
+def old_and_new_values(keys, new, seed):
+    v = rand(1, 1, keys, 64, seed=seed)
+    v[0, 0, :, 0], v[0, 0, new, 0] = 1, -1
+    return v
+
+
+LARGE_SCORES = [(2048, 2832, 0.125), (-2048, 2832, 0.125), (2048, 2048, 0.17), (1024, 1416, 0.125), (64, 96, 0.125)]   # log2 of a weight up to 2^20
+LARGER_SCORES = [(2048, 6144, 0.125), (2048, 6112, 0.125), (-2048, 6112, 0.125), (2048, 8160, 0.5)]                   # beyond
+
+
+@pytest.mark.parametrize("block_q", [64, 128])
+@pytest.mark.parametrize("first,key,scale", LARGE_SCORES + LARGER_SCORES)
+def test_large_scores_with_a_moving_maximum(F, first, key, scale, block_q):
+    """Some of a row's weights are taken before its maximum moves and some after: both count relative to one reference."""
+    scale = float(np.float32(scale))
+    least = int(8 / (scale * 1.4427)) + 1
+    second = list(range(least, least + 36))                      # what the late keys' scores have more
+    for keys in (65, 300, 449):
+        for late in ([keys - 1], [70 % keys, keys - 1], list(range(33, 64))):
+            more = torch.zeros(keys)
+            more[late] = 1
+            check_exact_scores(F, *exact_scores(first, second, [key] * keys, more, old_and_new_values(keys, late, keys), scale), block_q)
+
+
+@pytest.mark.parametrize("keys", [300, 2000])
+def test_scores_on_both_sides_of_two_to_the_twentieth(F, keys):
+    """A row's weights are formed one way up to 2^20 and another beyond: a row that begins below and ends above."""
+    for sign in (1, -1):
+        for below in (4.0, 20.0):
+            scale = float(np.float32((2.0 ** 20 - sign * below) / (2.0 ** 22 * math.log2(math.e))))   # 0.1733: 1/4 per unit of a score
+            more = torch.zeros(keys)
+            more[keys // 2:] = 1
+            more[-1] = 2
+            v = old_and_new_values(keys, list(range(keys // 2, keys)), 9)
+            second = [4, 8, 20, 30, 33, 36, 40, 44, 50, 60]
+            check_exact_scores(F, *exact_scores(2048 * sign, second, [2048] * keys, more, v, scale), parts=keys > 300)
