@@ -279,6 +279,7 @@ void select_blocks_kernel(const double* means, const int32_t* lens, int32_t* cho
 
 // ------------------------------------------------------------------------------------------------ attention
 constexpr uint32_t kAllBlocks = 0xFFFFFFFFu;   // no list (FB4_ALL_BLOCKS in 32 bits)
+constexpr float kLog2E = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 typedef float attn_f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 attn_bf16x2 __attribute__((ext_vector_type(2)));
@@ -325,7 +326,7 @@ constexpr int attention_keys(int pieces, int waves) { return waves == 2 && piece
 // takes m off the exact product, so m's own rounding is one factor in all weights and in their sum, and when m moves they are scaled by the
 // power of the rounded values' difference; beyond |m| = 2^20 that factor could itself be no small number, and the wavefront goes on with
 // exp2((S - max) c).
-// kSplit: a part of the list; the accumulators, reference and sum go to `out` as floats (see join_parts_kernel).
+// kSplit: a part of the list; the accumulators, maximum and sum go to `out` as floats (see join_parts_kernel).
 // Measured (channels; listed keys): 24 heads x 16384 queries x 2048 of 128: 434-463 us by card, 0.89-0.95 PFLOP/s, held by the power limit (on zeros
 // 340) and the loads into LDS (a fifth); 65536 queries, random lists: 1870 us, 11 GB from beyond the L2s; 272 x 1350 queries x 448 of 72:
 // 97 us, a third of it first reads and output; 48 single queries x 8192 of 128: 42 us, 4.7 TB/s.
@@ -446,7 +447,7 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
             qf[i] = __builtin_bit_cast(mfma_bf16x8, w);
         }
     }
-    const float factor = s.scale * 1.44269504088896340736f;   // c
+    const float factor = s.scale * kLog2E;   // c
     mfma_f32x16 o[kTiles], sc = {}, sd = {};   // accumulators; products of the groups at hand, in turn
     mfma_bf16x8 p[2] = {};               // weights of the group before it, as operands
 #pragma unroll
@@ -629,6 +630,14 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
     sum += __shfl_xor(sum, 32);
     const size_t at_row = (size_t)g * s.tokens_q + row;
     if (kSplit) {
+        // relative to the exact product of maximum and factor, whose difference from another part's is then one of maxima
+        const float exact = large || most == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(fmaf(-most, factor, off));
+        sum *= exact;
+#pragma unroll
+        for (int d = 0; d < kTiles; ++d) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] *= exact;
+        }
         if (row >= end_q) return;
         const size_t n_rows = (size_t)(s.n_workgroups / s.parts / s.blocks_q) * s.tokens_q;
         float* to = reinterpret_cast<float*>(out) + (part * n_rows + at_row) * (kP * 8);
@@ -640,11 +649,11 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
                 if (c < kP * 8u) *reinterpret_cast<float4*>(to + c) = make_float4(o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]);
             }
         }
-        if (half == 0) *reinterpret_cast<float2*>(reinterpret_cast<float*>(out) + s.parts * n_rows * (kP * 8) + 2 * (part * n_rows + at_row)) = make_float2(reference, sum);
+        if (half == 0) *reinterpret_cast<float2*>(reinterpret_cast<float*>(out) + s.parts * n_rows * (kP * 8) + 2 * (part * n_rows + at_row)) = make_float2(most, sum);
         return;
     }
     const float inverse = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;   // (a NaN stays; no key: zeros)
-    if (lse && half == 0 && row < end_q) lse[at_row] = sum == 0.0f ? -__builtin_inff() : 0.69314718055994530942f * (off + __builtin_amdgcn_logf(sum));
+    if (lse && half == 0 && row < end_q) lse[at_row] = sum == 0.0f ? -__builtin_inff() : kLn2 * (off + __builtin_amdgcn_logf(sum));
     // Rows through LDS, 16 bytes to a lane: from the accumulators a store is 32 rows' 16 bytes each (17 x 16 x 1350 x 72: 11 of 100 us).
     // Every wavefront has a buffer of its own, once all are done with the tiles.
     __syncthreads();
@@ -676,14 +685,15 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
 
 #undef FB4_INLINE
 
-// The parts of a row's list meet: accumulators and sums relative to the parts' own references (powers of two; -Inf: no key).
-// Workspace: float [parts][rows][dim], then {reference, sum} [parts][rows].  32 lanes, four channels each, take a row's parts one after
+// The parts of a row's list meet: accumulators and sums relative to the parts' own maxima (-Inf: no key), a part's weight
+// exp2((its maximum - the largest) c): of a difference, which is small where the weight is not, however large both are.
+// Workspace: float [parts][rows][dim], then {maximum, sum} [parts][rows].  32 lanes, four channels each, take a row's parts one after
 // the other, four reads ahead, eight rows to a workgroup; of many parts (kMany) a workgroup's eight sets of lanes take every eighth
 // and meet in LDS, so that a row waits for few reads one behind the other (48 rows x 21 parts x 128 channels 20.8 us with one walk
 // over the parts, 4.1 so; 25600 rows x 2 parts x 72 channels 27 us so).
 template <bool kMany>
 __global__ __launch_bounds__(256) void join_parts_kernel(const float* workspace, const int32_t* lens, uint16_t* out, float* lse, TensorStrides so,
-                                                         uint32_t parts, uint32_t n_rows, uint32_t tokens_q, uint32_t heads, uint32_t dim)
+                                                         uint32_t parts, uint32_t n_rows, uint32_t tokens_q, uint32_t heads, uint32_t dim, float scale)
 {
     __shared__ float4 meet[kMany ? 8 : 1][32];
     const uint32_t l = threadIdx.x & 31u, set = threadIdx.x >> 5, c = 4u * l;
@@ -699,11 +709,11 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float* workspace,
     }
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
-    const float base = most == -__builtin_inff() ? 0.0f : most;
+    const float base = most == -__builtin_inff() ? 0.0f : most, factor = scale * kLog2E;
     if (live) {
         for (uint32_t p = l; p < parts; p += 32) {
             const float2 st = state[(size_t)p * n_rows];
-            sum = fmaf(st.y, __builtin_amdgcn_exp2f(st.x - base), sum);
+            sum = fmaf(st.y, __builtin_amdgcn_exp2f((st.x - base) * factor), sum);
         }
     }
 #pragma unroll
@@ -711,7 +721,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float* workspace,
     if (live && c < dim) {
 #pragma unroll 4
         for (uint32_t p = first; p < parts; p += step) {
-            const float w = __builtin_amdgcn_exp2f(state[(size_t)p * n_rows].x - base);
+            const float w = __builtin_amdgcn_exp2f((state[(size_t)p * n_rows].x - base) * factor);
             const float4 x = *reinterpret_cast<const float4*>(workspace + ((size_t)p * n_rows + at) * dim + c);
             o = make_float4(fmaf(x.x, w, o.x), fmaf(x.y, w, o.y), fmaf(x.z, w, o.z), fmaf(x.w, w, o.w));
         }
@@ -732,7 +742,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float* workspace,
     const attn_bf16x2 lo = __builtin_convertvector((attn_f32x2{o.x * inverse, o.y * inverse}), attn_bf16x2);
     const attn_bf16x2 hi = __builtin_convertvector((attn_f32x2{o.z * inverse, o.w * inverse}), attn_bf16x2);
     if (c < dim) *reinterpret_cast<uint2*>(to + c) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
-    if (lse && l == 0) lse[at] = sum == 0.0f ? -__builtin_inff() : 0.69314718055994530942f * (base + __builtin_amdgcn_logf(sum));
+    if (lse && l == 0) lse[at] = sum == 0.0f ? -__builtin_inff() : fmaf(base, scale, kLn2 * __builtin_amdgcn_logf(sum));
 }
 
 }  // namespace fb4

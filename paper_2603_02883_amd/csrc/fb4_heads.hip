@@ -221,7 +221,7 @@ int fb4_block_attention(const void* q, const void* k, const void* v, const int64
         const bool many = parts > 8;
         launch(many ? join_parts_kernel<true> : join_parts_kernel<false>, dim3((unsigned)(many ? rows : (rows + 7) / 8)), dim3(256), 0, st,
                static_cast<const float*>(workspace), lens, static_cast<uint16_t*>(out), lse, so, (uint32_t)parts, (uint32_t)rows, s.tokens_q, (uint32_t)heads,
-               (uint32_t)dim);
+               (uint32_t)dim, scale);
     }
     return hipGetLastError() == hipSuccess ? FB4_OK : FB4_ERR_HIP;
 }

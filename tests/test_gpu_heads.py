@@ -691,3 +691,14 @@ def test_scores_on_both_sides_of_two_to_the_twentieth(F, keys):
             v = old_and_new_values(keys, list(range(keys // 2, keys)), 9)
             second = [4, 8, 20, 30, 33, 36, 40, 44, 50, 60]
             check_exact_scores(F, *exact_scores(2048 * sign, second, [2048] * keys, more, v, scale), parts=keys > 300)
+
+
+@pytest.mark.parametrize("first,key,scale", LARGE_SCORES + LARGER_SCORES)
+def test_large_scores_in_parts(F, first, key, scale):
+    """Parts of a list with maxima of their own: joined relative to one."""
+    scale = float(np.float32(scale))
+    second, keys = list(range(1, 40)), 2000
+    for late in ([keys - 1], [100], list(range(640, 700)) + [1500]):
+        more = torch.zeros(keys)
+        more[late] = 1
+        check_exact_scores(F, *exact_scores(first, second, [key] * keys, more, old_and_new_values(keys, late, 7), scale), parts=True)
