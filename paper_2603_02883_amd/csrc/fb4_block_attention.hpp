@@ -452,8 +452,8 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
     mfma_bf16x8 p[2] = {};               // weights of the group before it, as operands
 #pragma unroll
     for (int d = 0; d < kTiles; ++d) o[d] = mfma_f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-    // of this lane's query: the largest product that the reference is made of, the reference (-Inf: no product yet, then 0 is taken
-    // off), the sum over this lane's keys
+    // of this lane's query: the largest product that the reference is made of, the reference (-Inf: no product yet), what is taken off
+    // (the rounded product; 0 where there is none), the sum over this lane's keys
     float most = -__builtin_inff(), reference = -__builtin_inff(), off = 0.0f, sum = 0.0f;
     bool large = false;                                  // (of the wavefront)
 
@@ -534,7 +534,8 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
             const float moved = was_large ? (most - larger) * factor : large ? fmaf(-larger, factor, off) : off - fresh;
             const float shrink = most == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(moved);
             most = larger;
-            reference = product;
+            // (large: the rounding is no small part of 8, so the next move comes that much sooner, or, past fp32, with every group)
+            reference = !large ? product : fabsf(product) < __builtin_inff() ? fmaf(-fabsf(product), 0x1p-22f, product) : -__builtin_inff();
             off = fresh;
             sum *= shrink;
 #pragma unroll
@@ -653,7 +654,10 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
         return;
     }
     const float inverse = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;   // (a NaN stays; no key: zeros)
-    if (lse && half == 0 && row < end_q) lse[at_row] = sum == 0.0f ? -__builtin_inff() : kLn2 * (off + __builtin_amdgcn_logf(sum));
+    if (lse && half == 0 && row < end_q) {
+        const float log_sum = __builtin_amdgcn_logf(sum);
+        lse[at_row] = sum == 0.0f ? -__builtin_inff() : large ? fmaf(most, s.scale, kLn2 * log_sum) : kLn2 * (off + log_sum);
+    }
     // Rows through LDS, 16 bytes to a lane: from the accumulators a store is 32 rows' 16 bytes each (17 x 16 x 1350 x 72: 11 of 100 us).
     // Every wavefront has a buffer of its own, once all are done with the tiles.
     __syncthreads();

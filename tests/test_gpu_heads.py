@@ -702,3 +702,35 @@ def test_large_scores_in_parts(F, first, key, scale):
         more = torch.zeros(keys)
         more[late] = 1
         check_exact_scores(F, *exact_scores(first, second, [key] * keys, more, old_and_new_values(keys, late, 7), scale), parts=True)
+
+
+def test_far_scores_that_are_neighbours(F):
+    """Scores so far out that a step of theirs is more than a weight's range, whose products with the scale round to one number: the
+    larger one takes all the weight."""
+    rng, found = np.random.default_rng(5), 0
+    low, high = 255 * 2.0 ** 16, 2.0 ** 16                           # scores about 2^33, 512 apart
+    for scale in np.linspace(0.25, 0.27, 400).astype(np.float32) / np.float32(math.log2(math.e)):
+        factor = np.float32(scale * np.float32(math.log2(math.e)))
+        for j in rng.integers(0, 200, 4):
+            a, b = np.float32(255 * 2.0 ** 25 + 512 * int(j)), np.float32(255 * 2.0 ** 25 + 512 * int(j + 1))
+            if float(b) * float(factor) - float(a * factor) > 8 or found >= 12:
+                continue
+            found += 1
+            more = torch.full((200,), float(j))
+            more[150:] = float(j + 1)
+            v = old_and_new_values(200, list(range(150, 200)), 11)
+            check_exact_scores(F, *exact_scores(2.0 ** 16, [512.0] * 5, [255 * 2.0 ** 9] * 200, more, v, float(scale)))
+    assert found == 12
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("keys", [200, 3000])
+def test_scores_at_the_end_of_fp32(F, keys, sign):
+    """Finite scores whose products with log2 e are not."""
+    for order in (1, -1):
+        k = torch.full((keys,), 1.5 * 2.0 ** 64)
+        k[keys // 2:] = 1.75 * 2.0 ** 64
+        if order < 0:
+            k = k.flip(0)
+        v = old_and_new_values(keys, list(range(keys // 2, keys)), 12)
+        check_exact_scores(F, *exact_scores(sign * 2.0 ** 63, [1.0] * 3, k, [0.0] * keys, v, 1.0), parts=keys > 200)
