@@ -572,8 +572,9 @@ int fb4_select_key_blocks(const void* q, const void* k, int64_t batch, int heads
  *   workspace  as in fb4_select_key_blocks, by fb4_block_attention_workspace; may be
  *           NULL where that is 0
  * A query without a key, or all of whose scores are -Inf, gives zeros and lse =
- * -Inf; rows behind a sequence's last query keep what they held, in out and
- * in lse.  A row's sums are formed in an order that depends on the sizes in the call
+ * -Inf; a score of +Inf gives NaN and lse = +Inf, a score that is NaN gives NaN in
+ * both; rows behind a sequence's last query keep what they held, in out and in
+ * lse.  A row's sums are formed in an order that depends on the sizes in the call
  * (the same call always gives the same results).
  */
 #define FB4_ALL_BLOCKS (-1)

@@ -526,7 +526,8 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
         if (__any(fmaf(larger, factor, -reference) > 8.0f)) {
 #pragma clang fp contract(off)   // (a rounded product is meant)
             larger = fmaxf(larger, most);
-            larger = fmaxf(larger, __shfl_xor(larger, 32));
+            // (finite, so that a score of +Inf has an infinite weight and sum: no number in the output, +Inf in lse)
+            larger = fminf(fmaxf(larger, __shfl_xor(larger, 32)), 0x1.fffffep127f);
             const float product = larger * factor, fresh = larger == -__builtin_inff() ? 0.0f : product;
             const bool was_large = large;
             large = large || __any(fabsf(fresh) > 0x1p20f);

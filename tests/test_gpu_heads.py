@@ -734,3 +734,25 @@ def test_scores_at_the_end_of_fp32(F, keys, sign):
             k = k.flip(0)
         v = old_and_new_values(keys, list(range(keys // 2, keys)), 12)
         check_exact_scores(F, *exact_scores(sign * 2.0 ** 63, [1.0] * 3, k, [0.0] * keys, v, 1.0), parts=keys > 200)
+
+
+@pytest.mark.parametrize("keys", [1, 40, 300, 3000])
+def test_infinite_scores(F, keys):
+    """A key whose score is +Inf: no number for the row's output, +Inf for its lse; a NaN beside it is a NaN; other rows as ever."""
+    q, k, v = rand(1, 1, 40, 64, seed=160), rand(1, 1, keys, 64, seed=161), rand(1, 1, keys, 64, seed=162)
+    q[..., 0], k[..., 0] = 0, 0
+    ref, ref_lse = F.fb4_block_attention(q, k, v, None, None, 64, 64, want_lse=True)
+    for at in {0, keys // 2, keys - 1}:
+        far = k.clone()
+        far[0, 0, at, 0] = 3e38
+        row = q.clone()
+        row[0, 0, 7, 0], row[0, 0, 33, 0], row[0, 0, 34, 0] = 3e38, -3e38, 3e38
+        row[0, 0, 34, 5] = math.nan
+        out, lse = F.fb4_block_attention(row, far, v, None, None, 64, 64, want_lse=True)
+        others = torch.ones(40, dtype=torch.bool, device="cuda")
+        others[[7, 33, 34]] = False
+        assert out[0, 7].isnan().all() and lse[0, 0, 7] == math.inf
+        assert out[0, 34].isnan().all() and lse[0, 0, 34].isnan()
+        assert not out[0, 33].isnan().any() and ((lse[0, 0, 33] == -math.inf) == (keys == 1)) and not lse[0, 0, 33].isnan()
+        assert agree(out[0, others].double(), ref[0, others].double(), 2 * BF16 * (ref[0, others].double().abs() + 1.0))
+        assert agree(lse[0, 0, others].double(), ref_lse[0, 0, others].double(), 2.0 ** -18 + 2.0 ** -20 * ref_lse[0, 0, others].double().abs())
