@@ -675,7 +675,9 @@ void block_attention_kernel(const uint16_t* q, const uint16_t* k, const uint16_t
             if (4 * d + i < kP) *reinterpret_cast<uint2*>(mine + col * kRowBytes + (((4u * d + i) ^ k_swz) << 4) + 8u * half) = make_uint2(w[0], w[1]);
         }
     }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");   // (other lanes read them)
     __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     uint16_t* to = out + ((size_t)b * so.batch + (size_t)h * so.head) * 8u;
 #pragma unroll
     for (int i = 0; i < (kP + 1) / 2; ++i) {

@@ -52,3 +52,10 @@ def test_kernel_arguments_fit_a_launch():
         count = m.group(1)
         sizes.append(int.from_bytes(count[1:], "big") if len(count) > 1 else count[0])
     assert len(sizes) == len(spills()) > 300 and max(sizes) <= 112
+
+
+def test_attention_rows_that_lanes_exchange_are_fenced():
+    """Rows that one lane writes to LDS and another of its wavefront reads: a barrier of the wavefront alone orders no memory."""
+    text = open(os.path.join(CSRC, "fb4_block_attention.hpp")).read()
+    fenced = re.findall(r'fence\(__ATOMIC_RELEASE, "wavefront"\);[^\n]*\n\s*__builtin_amdgcn_wave_barrier\(\);\s*__builtin_amdgcn_fence\(__ATOMIC_ACQUIRE, "wavefront"\);', text)
+    assert len(fenced) == text.count("wave_barrier()") > 0
