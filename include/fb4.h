@@ -532,7 +532,10 @@ int fb4_qk_norm_rope(const void* q, const int64_t* q_strides, const void* k, con
  *   lens    device, int32 [batch][2]: queries and keys of each sequence of a
  *           padded batch, clamped to 0 .. tokens; NULL = all.  What lies behind is not read
  *   block_q, block_k  64 or 128 (FB4_ERR_UNSUPPORTED otherwise); at most 2048
- *           blocks of keys (FB4_ERR_UNSUPPORTED beyond)
+ *           blocks of keys, fewer than 2^24 blocks of queries and keys in all
+ *           sequences and heads, and batch * heads * ceil(blocks of queries / 16)
+ *           below 2^23 -- with 513 to 1024 blocks of keys batch * heads *
+ *           ceil(blocks of queries / 32) below 2^22 (FB4_ERR_UNSUPPORTED beyond)
  *   blocks  device, int32 [batch][heads][ceil(tokens_q / block_q)][top]: the chosen
  *           blocks, ascending, then -1 (fewer than top blocks with a key; a block without a
  *           query has none) -- the `blocks` argument of fb4_block_attention
@@ -553,7 +556,9 @@ int fb4_select_key_blocks(const void* q, const void* k, int64_t batch, int heads
  *   out[i] = sum_j P[i][j] V[j], P[i] = softmax of scale * Q[i] . K[j]
  * Products on the matrix cores with fp32 accumulation, the softmax in one pass in fp32,
  * its weights rounded to bf16 for the second product, the output rounded once.
- *   q, k, heads, heads_k, dim, lens, block_q, block_k  as in fb4_select_key_blocks
+ *   q, k, heads, heads_k, dim, lens, block_q, block_k  as in fb4_select_key_blocks,
+ *           with any number of keys; fewer than 2^24 blocks of queries in all
+ *           (FB4_ERR_UNSUPPORTED beyond)
  *   v       device, bf16 [batch][heads_k][tokens_k][dim] by v_strides: rows
  *           16-byte aligned, the channels contiguous, the token stride below 2^25
  *           (FB4_ERR_UNSUPPORTED otherwise)

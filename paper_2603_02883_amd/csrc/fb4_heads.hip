@@ -12,7 +12,8 @@ using namespace fb4;
 namespace {
 
 constexpr int64_t kMaxTokens = 0x7FFFFFFF;
-constexpr int64_t kMaxWorkgroups = (1 << 24) - 1;   // a launch takes fewer than 2^32 threads, 256 per workgroup
+constexpr int64_t kMaxThreads = 0xFFFFFFFFll;       // of a launch
+constexpr int64_t kMaxWorkgroups = (1 << 24) - 1;   // ... of 256 threads each
 
 // (batch, head, token) strides in elements to units of 8: what the kernels count in.
 template <typename T>
@@ -134,7 +135,10 @@ int fb4_select_key_blocks(const void* q, const void* k, int64_t batch, int heads
     if (workspace_bytes < fb4_select_key_blocks_workspace(batch, heads, heads_k, tokens_q, tokens_k, dim, block_q, block_k)) return FB4_ERR_INVALID_ARG;
     const int64_t n_q = batch * heads * s.blocks_q, n_k = batch * heads_k * s.blocks_k;
     if (!aligned(q, 16) || !aligned(k, 16) || !aligned(lens, 4) || !aligned(blocks, 4) || !aligned(scores, 4) || !aligned(workspace, 16)) return FB4_ERR_UNSUPPORTED;
-    if (s.blocks_k > kSelectMaxBlocks || n_q + n_k > kMaxWorkgroups || top > kMaxTokens) return FB4_ERR_UNSUPPORTED;
+    const int values = s.blocks_k <= 128 ? 2 : s.blocks_k <= 512 ? 8 : s.blocks_k <= 1024 ? 16 : 32;
+    const uint32_t rows = 16 * select_sets(values), row_tiles = (s.blocks_q + rows - 1) / rows;
+    if (s.blocks_k > kSelectMaxBlocks || n_q + n_k > kMaxWorkgroups || batch * heads * row_tiles * select_threads(values) > kMaxThreads || top > kMaxTokens)
+        return FB4_ERR_UNSUPPORTED;
     hipStream_t st = static_cast<hipStream_t>(stream);
     double* means = static_cast<double*>(workspace);
     const uint32_t pieces = (uint32_t)(dim / 8);
@@ -144,8 +148,6 @@ int fb4_select_key_blocks(const void* q, const void* k, int64_t batch, int heads
     else if (pieces > 4) FB4_MEANS(8);
     else FB4_MEANS(4);
 #undef FB4_MEANS
-    const int values = s.blocks_k <= 128 ? 2 : s.blocks_k <= 512 ? 8 : s.blocks_k <= 1024 ? 16 : 32;
-    const uint32_t rows = 16 * select_sets(values), row_tiles = (s.blocks_q + rows - 1) / rows;
     const dim3 sgrid((unsigned)(batch * heads * row_tiles));
 #define FB4_SELECT_LAUNCH(d, v) launch(select_blocks_kernel<d, v>, sgrid, dim3(select_threads(v)), 0, st, means, lens, blocks, scores, (uint32_t)top, (uint32_t)n_q, (uint32_t)dim, row_tiles, sgrid.x, s)
 #define FB4_SELECT_CASE(d)                                       \

@@ -152,3 +152,16 @@ def test_outputs_are_made_on_the_stream_that_the_call_runs_on(monkeypatch):
             assert all(t.made == (kind, name) for t in made), [t.made for t in made]
             # (the memory comes back only when the caller's stream, where the results are used, is done with it too)
             assert all(t.kept_for == ([] if stream is None else ["callers"]) for t in made)
+
+
+def test_select_refuses_launches_of_more_than_32_bits_of_threads():
+    """Both kernels' launches have to fit before the first runs: the choice takes 512 threads per 16 blocks of queries of a head, 1024
+    per 32 with 513 to 1024 blocks of keys."""
+    big = dict(ws=P(AL), size=1 << 50, dim=8, bk=64)
+    many = dict(heads=60000, hk=1, tq=1, **big)
+    for bad in (dict(batch=140, tk=1), dict(batch=150, tk=1), dict(batch=70, tk=64 * 513), dict(batch=70, tk=64 * 1024)):
+        assert select(**{**many, **bad}) == F.ERR_UNSUPPORTED, bad
+    # what fits comes as far as the device
+    if not torch.cuda.is_available():
+        for good in (dict(batch=139, tk=1), dict(batch=69, tk=64 * 1024), dict(batch=70, tk=64 * 512), dict(batch=100, tk=64 * 1025)):
+            assert select(**{**many, **good}) == F.ERR_HIP, good
