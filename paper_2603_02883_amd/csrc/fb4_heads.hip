@@ -35,6 +35,8 @@ int check_blocks(int64_t batch, int heads, int heads_k, int64_t tokens_q, int64_
     if (heads > 65535 || dim % 8 || dim > 128 || tokens_q > kMaxTokens || tokens_k > kMaxTokens || batch > kMaxTokens) return FB4_ERR_UNSUPPORTED;
     *s = BlockShape{(uint32_t)tokens_q, (uint32_t)tokens_k, (uint16_t)heads, (uint16_t)heads_k, (uint16_t)block_q, (uint16_t)block_k,
                     (uint32_t)((tokens_q + block_q - 1) / block_q), (uint32_t)((tokens_k + block_k - 1) / block_k)};
+    // (2^41 blocks are more than any memory holds; below that no product of sizes passes 64 bits)
+    if ((double)batch * heads * s->blocks_q > 0x1p40 || (double)batch * heads_k * s->blocks_k > 0x1p40) return FB4_ERR_UNSUPPORTED;
     return FB4_OK;
 }
 

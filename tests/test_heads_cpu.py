@@ -165,3 +165,15 @@ def test_select_refuses_launches_of_more_than_32_bits_of_threads():
     if not torch.cuda.is_available():
         for good in (dict(batch=139, tk=1), dict(batch=69, tk=64 * 1024), dict(batch=70, tk=64 * 512), dict(batch=100, tk=64 * 1025)):
             assert select(**{**many, **good}) == F.ERR_HIP, good
+
+
+def test_sizes_whose_products_pass_64_bits_are_refused():
+    """Each size in its own range, their product a small number modulo 2^64: what a check of the wrapped product would let through."""
+    lib = B.lib()
+    for batch, heads, tq in ((2 ** 30, 2 ** 15, 2 ** 25), (2 ** 31 - 1, 2 ** 15, 2 ** 31 - 64), (2 ** 27, 2 ** 15, 2 ** 22 * 64), (2 ** 30, 2 ** 15, 2 ** 25 + 64)):
+        sizes = dict(batch=batch, heads=heads, hk=1, tq=tq, tk=0, dim=64, bq=64, bk=64)
+        assert select(**sizes, ws=P(AL), size=2 ** 64 - 1) == F.ERR_UNSUPPORTED, sizes
+        assert attention(**sizes, ws=P(AL), size=2 ** 64 - 1) == F.ERR_UNSUPPORTED, sizes
+        assert lib.fb4_select_key_blocks_workspace(batch, heads, 1, tq, 0, 64, 64, 64) == 0
+        assert lib.fb4_block_attention_workspace(batch, heads, 1, tq, 0, 64, 2, 64, 64) == 0
+    assert select(batch=2 ** 31 - 1, heads=1, hk=1, tq=1, tk=2 ** 31 - 1, bk=64, ws=P(AL), size=2 ** 64 - 1) == F.ERR_UNSUPPORTED
