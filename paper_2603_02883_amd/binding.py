@@ -30,6 +30,7 @@ FLAG_TWO_STAGE = 1
 ROPE_ADJACENT = 0
 ROPE_HALVES = 1
 ALL_BLOCKS = -1
+INT_MAX = 2 ** 31 - 1   # (ctypes cuts off what is larger)
 DTYPE_BF16 = 0
 DTYPE_F32 = 1
 
@@ -254,6 +255,8 @@ class HeadsCall:
                    (gamma_k, torch.float32), (q_out, torch.bfloat16), (k_out, torch.bfloat16))
         heads_k, n = 0 if k is None else k.shape[1], len(axis_pairs)
         _require(k is None or k.shape == (batch, heads_k, tokens, dim), where)
+        _require(pairing in (ROPE_ADJACENT, ROPE_HALVES) and all(0 < p <= dim for p in axis_pairs), where)
+        _require(max(heads, heads_k) <= INT_MAX, where, ERR_UNSUPPORTED)
         if n:
             _require(positions is not None and freqs is not None and positions.dim() == 3 and positions.shape[0] in (1, batch) and
                      positions.shape[1:] == (tokens, n) and freqs.shape == (sum(axis_pairs),), where)
@@ -275,6 +278,7 @@ class HeadsCall:
         """The sizes that the choice of blocks and the attention share, checked."""
         batch, heads, tokens_q, dim = q.shape
         _require(k.dim() == 4 and k.shape[0] == batch and k.shape[3] == dim and (lens is None or lens.shape == (batch, 2)) and block_q > 0 and block_k > 0, where)
+        _require(max(heads, k.shape[1], block_q, block_k) <= INT_MAX, where, ERR_UNSUPPORTED)
         for t in (q, k, lens):
             _require(t is None or t.is_contiguous(), where, ERR_UNSUPPORTED)
         return batch, heads, k.shape[1], tokens_q, k.shape[2], dim

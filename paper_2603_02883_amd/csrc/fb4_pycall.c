@@ -391,6 +391,15 @@ typedef struct {
 } view;
 enum { kInt = 0, kUint = 1, kFloat = 2, kBfloat = 4 };   // DLPack's type codes
 
+// ... none that 64 bits do not hold, where the number is one of the call's sizes.
+static int whole(PyObject* o, int64_t* out)
+{
+    int past = 0;
+    if (!PyLong_Check(o)) return -1;
+    *out = PyLong_AsLongLongAndOverflow(o, &past);
+    return past ? -1 : 0;
+}
+
 // A tensor of n dimensions of one type on GPU `device` (DLPack's types 2 and 10).
 static int viewed(PyObject* t, int n, int code, int bits, int64_t device, view* out)
 {
@@ -452,19 +461,19 @@ static PyObject* py_qk_norm_rope(ARGS)
     void *freqs, *gq, *gk, *qo, *ko, *s;
     int64_t device, pairing, pairs = 0, hk = 0;
     int32_t axis_pairs[4];
-    if (!fb4_qk_norm_rope || n != 14 || integer(a[12], &device) || integer(a[9], &pairing) || address(a[13], &s) || !PyFloat_Check(a[7]) || !PyBool_Check(a[8]) ||
-        !PyTuple_Check(a[4]) || PyTuple_GET_SIZE(a[4]) > 4 || rows(a[0], device, &q))
+    if (!fb4_qk_norm_rope || n != 14 || integer(a[12], &device) || whole(a[9], &pairing) || (pairing != FB4_ROPE_ADJACENT && pairing != FB4_ROPE_HALVES) ||
+        address(a[13], &s) || !PyFloat_Check(a[7]) || !PyBool_Check(a[8]) || !PyTuple_Check(a[4]) || PyTuple_GET_SIZE(a[4]) > 4 || rows(a[0], device, &q) || q.size[1] > INT32_MAX)
         return elsewhere(k_qk_norm_rope, a, n);
     const int axes = (int)PyTuple_GET_SIZE(a[4]);
     for (int i = 0; i < axes; ++i) {
         int64_t x;
-        if (integer(PyTuple_GET_ITEM(a[4], i), &x) || x < 1 || x > 256) return elsewhere(k_qk_norm_rope, a, n);
+        if (whole(PyTuple_GET_ITEM(a[4], i), &x) || x < 1 || x > 256) return elsewhere(k_qk_norm_rope, a, n);
         axis_pairs[i] = (int32_t)x;
         pairs += x;
     }
     const int64_t batch = q.size[0], tokens = q.size[2], dim = q.size[3];
     if (a[1] != Py_None) {
-        if (rows(a[1], device, &k) || !sizes_are(&k, 4, batch, k.size[1], tokens, dim)) return elsewhere(k_qk_norm_rope, a, n);
+        if (rows(a[1], device, &k) || !sizes_are(&k, 4, batch, k.size[1], tokens, dim) || k.size[1] > INT32_MAX) return elsewhere(k_qk_norm_rope, a, n);
         hk = k.size[1];
     }
     if (axes && (viewed(a[2], 3, kInt, 32, device, &p) || (p.size[0] != 1 && p.size[0] != batch) || p.size[1] != tokens || p.size[2] != axes || !packed(&p, 3)))
@@ -484,7 +493,7 @@ static int heads_of(PyObject* oq, PyObject* ok, PyObject* olens, PyObject* obq, 
                     int64_t* bk)
 {
     return rows(oq, device, q) || rows(ok, device, k) || !packed(q, 4) || !packed(k, 4) || k->size[0] != q->size[0] || k->size[3] != q->size[3] ||
-                   dense(olens, 1, 2, kInt, 32, device, q->size[0], 2, 0, 0, lens) || integer(obq, bq) || integer(obk, bk) || *bq < 1 || *bk < 1 ||
+                   dense(olens, 1, 2, kInt, 32, device, q->size[0], 2, 0, 0, lens) || whole(obq, bq) || whole(obk, bk) || *bq < 1 || *bk < 1 ||
                    q->size[1] > INT32_MAX || k->size[1] > INT32_MAX || *bq > INT32_MAX || *bk > INT32_MAX
                ? -1 : 0;
 }
@@ -509,7 +518,7 @@ static PyObject* py_select_key_blocks(ARGS)
     void *lens, *blocks, *scores, *ws, *s;
     size_t size;
     int64_t device, top, bq, bk;
-    if (!fb4_select_key_blocks || n != 11 || integer(a[9], &device) || address(a[10], &s) || integer(a[2], &top) ||
+    if (!fb4_select_key_blocks || n != 11 || integer(a[9], &device) || address(a[10], &s) || whole(a[2], &top) ||
         heads_of(a[0], a[1], a[5], a[3], a[4], device, &q, &k, &lens, &bq, &bk) ||
         dense(a[6], 0, 4, kInt, 32, device, q.size[0], q.size[1], (q.size[2] + bq - 1) / bq, top, &blocks) ||
         dense(a[7], 1, 4, kFloat, 32, device, q.size[0], q.size[1], (q.size[2] + bq - 1) / bq, top, &scores))

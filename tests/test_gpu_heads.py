@@ -756,3 +756,25 @@ def test_infinite_scores(F, keys):
         assert not out[0, 33].isnan().any() and ((lse[0, 0, 33] == -math.inf) == (keys == 1)) and not lse[0, 0, 33].isnan()
         assert agree(out[0, others].double(), ref[0, others].double(), 2 * BF16 * (ref[0, others].double().abs() + 1.0))
         assert agree(lse[0, 0, others].double(), ref_lse[0, 0, others].double(), 2.0 ** -18 + 2.0 ** -20 * ref_lse[0, 0, others].double().abs())
+
+
+def test_numbers_that_c_would_cut_off(F):
+    """By either way into the library: 2^32 + 64 is not 64, 2^64 + 2 not 2."""
+    B = F.binding
+    q, k, v = rand(1, 2, 100, 64, seed=170), rand(1, 2, 200, 64, seed=171), rand(1, 2, 200, 64, seed=172)
+    pos, freqs = torch.zeros(1, 100, 1, device="cuda", dtype=torch.int32), torch.ones(8, device="cuda", dtype=torch.float64)
+    lists, far = torch.zeros(1, 2, 1, 2, device="cuda", dtype=torch.int32), 2 ** 32
+    calls = [lambda: F.fb4_select_key_blocks(q, k, 2, far + 64, 64), lambda: F.fb4_select_key_blocks(q, k, 2, 64, far + 64),
+             lambda: F.fb4_select_key_blocks(q, k, 2, far + 64, 64, blocks=lists), lambda: F.fb4_select_key_blocks(q, k, 2 ** 64 + 2, 128, 64, blocks=lists),
+             lambda: F.fb4_block_attention(q, k, v, lists, None, far + 128, 64), lambda: F.fb4_block_attention(q, k, v, None, None, 64, far + 64),
+             lambda: F.fb4_qk_norm_rope(q, q, pos, freqs, (far + 8,)), lambda: F.fb4_qk_norm_rope(q, q, pos, freqs, (8,), pairing=far),
+             lambda: F.fb4_qk_norm_rope(q, q, pos, freqs, (8,), pairing=2 ** 64 + 1)]
+    module = B._heads_call
+    try:
+        for B._heads_call in {module, B.HeadsCall}:
+            for i, call in enumerate(calls):
+                with pytest.raises(F.Fb4Error):
+                    call()
+                    raise AssertionError(i)
+    finally:
+        B._heads_call = module

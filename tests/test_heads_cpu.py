@@ -177,3 +177,60 @@ def test_sizes_whose_products_pass_64_bits_are_refused():
         assert lib.fb4_select_key_blocks_workspace(batch, heads, 1, tq, 0, 64, 64, 64) == 0
         assert lib.fb4_block_attention_workspace(batch, heads, 1, tq, 0, 64, 2, 64, 64) == 0
     assert select(batch=2 ** 31 - 1, heads=1, hk=1, tq=1, tk=2 ** 31 - 1, bk=64, ws=P(AL), size=2 ** 64 - 1) == F.ERR_UNSUPPORTED
+
+
+class Laid(OnGpu):
+    """... and as much as the calls through ctypes look at: a contiguous tensor of no memory."""
+
+    def __init__(self, dtype, *shape):
+        self.dtype, self.shape, self.device = dtype, torch.Size(shape), torch.device("cuda", 0)
+
+    def is_contiguous(self):
+        return True
+
+    def numel(self):
+        return self.shape.numel()
+
+    def stride(self, i):
+        return self.shape[i + 1:].numel()
+
+    def data_ptr(self):
+        return AL
+
+    def transpose(self, a, b):
+        return self
+
+
+def test_numbers_that_c_would_cut_off_are_refused(monkeypatch):
+    """A block size of 2^32 + 64 is 64 to C, for which the list has too few rows."""
+    class Library:
+        fb4_select_key_blocks_workspace = fb4_block_attention_workspace = staticmethod(lambda *a: 0)
+        fb4_strerror = staticmethod(lambda code: b"refused")
+
+        def __getattr__(self, name):
+            def call(*a):
+                handed.append(name)
+                return F.OK
+            return call
+    handed = []
+    monkeypatch.setattr(B, "_lib", Library())
+    bf, i32, far = torch.bfloat16, torch.int32, 2 ** 32
+    q, k, ws = Laid(bf, 1, 2, 100, 64), Laid(bf, 1, 2, 100, 64), Laid(torch.uint8, 4096)
+
+    def choose(bq=64, bk=64):
+        return B.HeadsCall.select_key_blocks(q, k, 3, bq, bk, None, Laid(i32, 1, 2, -(-100 // bq), 3), None, ws, 0, None)
+
+    def attend(bq=64, bk=64):
+        return B.HeadsCall.block_attention(q, k, k, Laid(i32, 1, 2, -(-100 // bq), 3), 1.0, bq, bk, None, Laid(bf, 1, 100, 2, 64), None, ws, 0, None)
+
+    def turn(pairs=(8, 8), pairing=0, q=q, k=k):
+        return B.HeadsCall.qk_norm_rope(q, k, Laid(i32, 1, 100, len(pairs)), Laid(torch.float64, sum(pairs)), pairs, None, None, 1e-6, True, pairing,
+                                        q, k, 0, None)
+    assert choose() == attend() == turn() == F.OK and len(handed) == 3
+    wide, seq = Laid(bf, 1, far + 2, 100, 64), Laid(bf, 1, 2, 100, 64)
+    for call in (lambda: choose(far + 64), lambda: choose(64, far + 64), lambda: attend(far + 128), lambda: attend(64, far + 64),
+                 lambda: turn((far + 8,)), lambda: turn((far + 4, 4 - far)), lambda: turn(pairing=far), lambda: turn(pairing=far + 1), lambda: turn(q=wide),
+                 lambda: turn(q=seq, k=wide)):
+        with pytest.raises(F.Fb4Error):
+            call()
+    assert len(handed) == 3
