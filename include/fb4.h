@@ -567,7 +567,8 @@ int fb4_select_key_blocks(const void* q, const void* k, int64_t batch, int heads
  *           block) is skipped, one listed twice counts twice
  *   top     entries of a list, at least 0; FB4_ALL_BLOCKS: all keys, blocks NULL (FB4_ERR_INVALID_ARG
  *           if it is not, or if it is NULL with entries)
- *   scale   > 0 and finite (FB4_ERR_INVALID_ARG otherwise)
+ *   scale   > 0 and finite (FB4_ERR_INVALID_ARG otherwise), at most 2^127
+ *           (FB4_ERR_UNSUPPORTED beyond)
  *   out     device, bf16 [batch][heads][tokens_q][dim] by out_strides, rows
  *           16-byte aligned, none overlapping another or an input: with
  *           [batch][tokens][heads][dim] the rows that fb4_quantize takes

@@ -184,6 +184,7 @@ int fb4_block_attention(const void* q, const void* k, const void* v, const int64
     BlockShape s;
     if (int rc = check_blocks(batch, heads, heads_k, tokens_q, tokens_k, dim, block_q, block_k, &s)) return rc;
     if (top < FB4_ALL_BLOCKS || !(scale > 0.0f) || !std::isfinite(scale)) return FB4_ERR_INVALID_ARG;
+    if (scale > 0x1p127f) return FB4_ERR_UNSUPPORTED;   // (times log2 e: no number)
     if (top == FB4_ALL_BLOCKS ? blocks != nullptr : top > 0 && !blocks) return FB4_ERR_INVALID_ARG;
     if (batch == 0 || tokens_q == 0) return FB4_OK;
     if (!q || !out || !out_strides || (tokens_k > 0 && (!k || !v || !v_strides))) return FB4_ERR_INVALID_ARG;

@@ -234,3 +234,10 @@ def test_numbers_that_c_would_cut_off_are_refused(monkeypatch):
         with pytest.raises(F.Fb4Error):
             call()
     assert len(handed) == 3
+
+
+def test_scales_whose_product_with_log2_e_leaves_fp32_are_refused():
+    assert attention(ws=P(AL), size=1 << 40, scale=3e38) == F.ERR_UNSUPPORTED
+    assert attention(ws=P(AL), size=1 << 40, scale=2.0 ** 127 * 1.0001) == F.ERR_UNSUPPORTED
+    if not torch.cuda.is_available():   # (as far as the device)
+        assert attention(ws=P(AL), size=1 << 40, scale=2.0 ** 127) == F.ERR_HIP
