@@ -508,7 +508,9 @@ int fb4_seda_main_anchor_3d(const float* scores, int64_t frames, int heads, int 
  *               dim (FB4_ERR_INVALID_ARG otherwise); P a multiple of 4 for FB4_ROPE_HALVES
  *               (FB4_ERR_UNSUPPORTED otherwise)
  *   q_out, k_out  device, bf16 [batch][heads][tokens][dim], contiguous, 16-byte
- *               aligned; not the memory of q or k
+ *               aligned; memory of q, of k or of the other output only in place:
+ *               q_out = q and k_out = k where those are contiguous themselves
+ *               (FB4_ERR_INVALID_ARG otherwise)
  */
 #define FB4_ROPE_ADJACENT 0
 #define FB4_ROPE_HALVES 1

@@ -524,7 +524,8 @@ def fb4_qk_norm_rope(q, k, positions, freqs, axis_pairs, gamma_q=None, gamma_k=N
     """q, k: bf16 cuda [batch][heads][tokens][dim], any strides with contiguous channels (views of a packed projection);
     k may be None.  positions: int32 cuda [batch or 1][tokens][axes]; freqs: float64 cuda [sum(axis_pairs)], radians per position;
     axis_pairs: pairs of channels per axis (empty: no rotation, positions and freqs None); gamma_q, gamma_k: float32 cuda [dim] or
-    None; norm=False: rotation alone.  Returns contiguous (q_out, k_out) of the inputs' shapes."""
+    None; norm=False: rotation alone.  Returns contiguous (q_out, k_out) of the inputs' shapes; given ones may be q and k themselves where
+    those are contiguous, and share no other memory with them."""
     _require(q.is_cuda, "fb4_qk_norm_rope")
     if q_out is None:
         q_out = _output(q.shape, torch.bfloat16, q.device, stream)

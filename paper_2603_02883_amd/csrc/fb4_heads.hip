@@ -27,6 +27,47 @@ int strides_of(const int64_t* strides, T* out)
     return FB4_OK;
 }
 
+// A [batch][heads][tokens] tensor's rows: levels (count, stride in bytes) by falling strides, the row's bytes; whether they lie one
+// upon the other, as an output's.
+struct RowSet {
+    int64_t count[3], stride[3], row;
+    bool dense = true;
+    RowSet(const int64_t* strides, int64_t batch, int64_t heads, int64_t tokens, int64_t row_bytes) : count{batch, heads, tokens}, row(row_bytes)
+    {
+        int64_t next = row;
+        for (int i = 2; i >= 0; --i) {
+            stride[i] = count[i] > 1 ? strides[i] * 2 : 0;
+            dense = dense && (count[i] == 1 || stride[i] == next);
+            next *= count[i];
+        }
+        for (int i : {0, 1, 0}) {
+            if (stride[i] < stride[i + 1]) {
+                std::swap(stride[i], stride[i + 1]);
+                std::swap(count[i], count[i + 1]);
+            }
+        }
+    }
+};
+
+// Whether a row of the set at `base` has bytes of [from, to).
+bool meets(const RowSet& s, uintptr_t base, uintptr_t from, uintptr_t to, int level = 0)
+{
+    if (level == 3) return base < to && base + (uintptr_t)s.row > from;
+    uintptr_t extent = (uintptr_t)s.row;   // of one of this level's parts
+    for (int i = level + 1; i < 3; ++i) extent += (uintptr_t)(s.count[i] - 1) * (uintptr_t)s.stride[i];
+    const uintptr_t stride = (uintptr_t)s.stride[level];
+    if (stride == 0) return meets(s, base, from, to, level + 1);
+    if (base >= to) return false;
+    // the parts that begin before `to` and end behind `from`; one that begins inside has its first row there
+    const uintptr_t last = std::min<uintptr_t>((uintptr_t)s.count[level] - 1, (to - 1 - base) / stride);
+    if (base + last * stride >= from) return true;
+    const uintptr_t first = base + extent > from ? 0 : (from - base - extent) / stride + 1;
+    for (uintptr_t i = first; i <= last; ++i) {
+        if (meets(s, base + i * stride, from, to, level + 1)) return true;
+    }
+    return false;
+}
+
 // What the choice of blocks and the attention have in common.
 int check_blocks(int64_t batch, int heads, int heads_k, int64_t tokens_q, int64_t tokens_k, int64_t dim, int block_q, int block_k, BlockShape* s)
 {
@@ -102,6 +143,17 @@ int fb4_qk_norm_rope(const void* q, const int64_t* q_strides, const void* k, con
         !aligned(gamma_k, 4) || !aligned(positions, 4) || !aligned(freqs, 8))
         return FB4_ERR_UNSUPPORTED;
     if (batch > (1 << 25) || tokens > (1 << 25) || batch * tokens > (1 << 25)) return FB4_ERR_UNSUPPORTED;   // (2^26 wavefronts to a launch)
+    // Outputs on memory that another workgroup may still read.  In place a row is read and written by the same lanes, in that order.
+    const int64_t row = dim * 2, size_q = batch * heads_q * tokens * row, size_k = batch * heads_k * tokens * row;
+    const uintptr_t at_q = (uintptr_t)q_out, at_k = (uintptr_t)k_out;
+    const RowSet rows_q(q_strides, batch, heads_q, tokens, row);
+    if (!(rows_q.dense && q == q_out) && meets(rows_q, (uintptr_t)q, at_q, at_q + (uintptr_t)size_q)) return FB4_ERR_INVALID_ARG;
+    if (heads_k > 0) {
+        const RowSet rows_k(k_strides, batch, heads_k, tokens, row);
+        if ((!(rows_k.dense && k == k_out) && meets(rows_k, (uintptr_t)k, at_k, at_k + (uintptr_t)size_k)) || meets(rows_q, (uintptr_t)q, at_k, at_k + (uintptr_t)size_k) ||
+            meets(rows_k, (uintptr_t)k, at_q, at_q + (uintptr_t)size_q) || (at_q < at_k + (uintptr_t)size_k && at_k < at_q + (uintptr_t)size_q))
+            return FB4_ERR_INVALID_ARG;
+    }
     const int pieces = (int)(dim / 8);
     // A wavefront per run of tokens; several, each with some of the heads, while there are few tokens: up to 8192 wavefronts (16384: the
     // permuted input of fb4_rope.hpp 58.5 us and not 61, the packed one 87 and not 83; 4096: 66 and 82).

@@ -778,3 +778,25 @@ def test_numbers_that_c_would_cut_off(F):
                     raise AssertionError(i)
     finally:
         B._heads_call = module
+
+
+def test_rotation_in_place(F):
+    """Row upon row an output may be its input; on memory that is read elsewhere it is refused."""
+    pos = torch.randint(0, 99, (1, 333, 1), device="cuda", dtype=torch.int32)
+    freqs = 50.0 ** (-torch.arange(36, device="cuda", dtype=torch.float64) / 36)
+    for halves in (F.ROPE_ADJACENT, F.ROPE_HALVES):
+        q, k = rand(3, 20, 333, 72, seed=180), rand(3, 11, 333, 72, seed=181)
+        ref = F.fb4_qk_norm_rope(q, k, pos, freqs, (36,), pairing=halves)
+        qi, ki = q.clone(), k.clone()
+        got = F.fb4_qk_norm_rope(qi, ki, pos, freqs, (36,), pairing=halves, q_out=qi, k_out=ki)
+        assert got[0] is qi and got[1] is ki and all(torch.equal(a, b) for a, b in zip(got, ref))
+    packed = rand(2, 333, 3, 72, seed=182)
+    view = packed.permute(0, 2, 1, 3)
+    memory = packed.view(-1)
+    for out in (memory[:2 * 333 * 72].view(2, 1, 333, 72), memory[-2 * 333 * 72:].view(2, 1, 333, 72)):
+        for args in ((view[:, :1], None), (q[:2, :1].contiguous(), view[:, 1:2])):
+            with pytest.raises(F.Fb4Error) as e:
+                F.fb4_qk_norm_rope(*args, pos, freqs, (36,), q_out=out)
+            assert e.value.code == F.ERR_INVALID_ARG
+    with pytest.raises(F.Fb4Error):
+        F.fb4_qk_norm_rope(q, q, pos, freqs, (36,), q_out=qi, k_out=qi)

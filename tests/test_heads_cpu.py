@@ -241,3 +241,25 @@ def test_scales_whose_product_with_log2_e_leaves_fp32_are_refused():
     assert attention(ws=P(AL), size=1 << 40, scale=2.0 ** 127 * 1.0001) == F.ERR_UNSUPPORTED
     if not torch.cuda.is_available():   # (as far as the device)
         assert attention(ws=P(AL), size=1 << 40, scale=2.0 ** 127) == F.ERR_HIP
+
+
+def test_rotation_refuses_outputs_on_memory_that_is_read_elsewhere():
+    """A row that is written while another workgroup still reads it.  In place, row upon row, is none; neither is a gap between rows."""
+    n = 2 * 2 * 4 * 64 * 2                                  # bytes of [2][2][4][64]
+    dense, packed, swapped = strides(512, 256, 64), strides(4 * 6 * 64, 64, 6 * 64), strides(64, 2 * 64, 4 * 64)
+    far = P(AL + (1 << 30))
+    served = F.ERR_HIP if not torch.cuda.is_available() else None
+    base = dict(pairs=(8,), sq=dense, sk=dense, k=far, ko=P(AL + (1 << 31)))
+    bad = [dict(sq=packed, qo=P(AL)), dict(sq=packed, qo=P(AL + 6 * 64 * 2 * 7)), dict(sq=swapped, qo=P(AL)), dict(qo=P(AL + 16)), dict(qo=P(AL + n - 16)),
+           dict(q=P(AL + n - 16), qo=P(AL)), dict(k=P(AL), q=far, qo=P(AL)), dict(k=P(AL), q=far, sk=packed, ko=P(AL + 6 * 64 * 2)),
+           dict(qo=far), dict(q=far, qo=P(AL + (1 << 32)), ko=P(AL + (1 << 32) + n - 16)),
+           dict(q=P(AL), sq=strides(0, 0, 0), qo=P(AL)), dict(q=P(AL), sq=strides(8, 8, 8), qo=P(AL + 128))]
+    good = [dict(qo=P(AL)), dict(qo=P(AL + n)), dict(q=P(AL + n), qo=P(AL)), dict(k=P(AL), q=far, qo=P(AL + n), ko=P(AL)),
+            # one sequence of four tokens in its packed projection's last gap; all of an output between two sequences far apart
+            dict(batch=1, hq=1, tokens=1, sq=packed, qo=P(AL + 128)), dict(sq=strides(1 << 20, 256, 64), qo=P(AL + 4096)),
+            dict(q=P(AL), sq=strides(0, 0, 0), qo=P(AL + 128)), dict(hk=0, k=None, ko=None, qo=P(AL)), dict(k=P(AL + n), sk=strides(0, 0, 64), qo=P(AL + 2 * n))]
+    for case in bad:
+        assert rope(**{**base, "qo": P(AL + (1 << 33)), **case}) == F.ERR_INVALID_ARG, case
+    if served is not None:                                  # (as far as the device)
+        for case in good:
+            assert rope(**{**base, "qo": P(AL + (1 << 33)), **case}) == served, case
