@@ -492,7 +492,8 @@ int fb4_seda_main_anchor_3d(const float* scores, int64_t frames, int heads, int 
  * normalized in double (a NaN makes its row NaN, an Inf is NaN and the rest of
  * its row 0, a zero row with eps = 0 is NaN).
  *   q, k        device, bf16 [batch][heads][tokens][dim] by strides: the
- *               channels contiguous, rows 16-byte aligned.  heads_k = 0: no keys
+ *               channels contiguous, rows 16-byte aligned, at most 65535 heads
+ *               (FB4_ERR_UNSUPPORTED beyond).  heads_k = 0: no keys
  *   *_strides   host, (batch, head, token) strides in elements, each a multiple
  *               of 8, at least 0 and below 2^35 (FB4_ERR_UNSUPPORTED otherwise):
  *               a packed projection [batch][tokens][q | k | v] is read in place, and one
@@ -529,7 +530,7 @@ int fb4_qk_norm_rope(const void* q, const int64_t* q_strides, const void* k, con
  *   q       device, bf16 [batch][heads][tokens_q][dim], contiguous, 16-byte aligned
  *   k       device, bf16 [batch][heads_k][tokens_k][dim], likewise; head h reads
  *           key head h / (heads / heads_k) (FB4_ERR_INVALID_ARG if heads_k does not
- *           divide heads)
+ *           divide heads; at most 65535 heads, FB4_ERR_UNSUPPORTED beyond)
  *   dim     a multiple of 8, at most 128 (FB4_ERR_UNSUPPORTED otherwise)
  *   lens    device, int32 [batch][2]: queries and keys of each sequence of a
  *           padded batch, clamped to 0 .. tokens; NULL = all.  What lies behind is not read

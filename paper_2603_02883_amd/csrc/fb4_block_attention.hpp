@@ -104,14 +104,15 @@ typedef double select_f64x4 __attribute__((ext_vector_type(4)));
 constexpr int select_sets(int values) { return values == 16 ? 2 : 1; }
 constexpr int select_threads(int values) { return 512 * select_sets(values); }
 
-// A workgroup takes 16 blocks of queries of one head: their scores with all the head's blocks of keys by 16x16x4 MFMAs in double,
+// A workgroup takes 16 blocks of queries of one head (32 with 513 to 1024 blocks of keys): their scores with all the head's blocks of keys by 16x16x4 MFMAs in double,
 // then the largest `top` of every row.  The channels of a product may come in any order as long as both operands have the same:
 // lane group k of 16 holds channels 16 c + 4 k .. + 3 for the four steps of chunk c, which are 32 bytes of its row.
-// LDS keeps the scores rounded to fp32, half of what the doubles would take, so that one workgroup's search runs beside another's
-// products.  Rounding keeps the order but for what becomes equal, so the fp32 values decide unless the border falls between
+// LDS keeps the scores rounded to fp32, half of what the doubles would take: up to 512 blocks of keys three workgroups and more share a
+// compute unit and one's search runs beside another's products; beyond, one fills it (144 to 160 KiB) and products and search take turns.
+// Rounding keeps the order but for what becomes equal, so the fp32 values decide unless the border falls between
 // equal ones; those blocks' scores are then formed again in double.
 // D16: channels / 16, rounded up; kValues: scores of a row per lane.
-// Measured, means included (24 heads x 1024 x 1024 blocks x 128 channels): 353 us, of which the means' kernel 148 at 5.5 TB/s; 424
+// Measured, means included (24 heads x 1024 x 1024 blocks x 128 channels): 346-356 us, of which the means' kernel 148 at 5.5 TB/s; 424
 // with doubles in LDS and a search bit by bit on four wavefronts.  The MFMAs alone are 82 us; the rest is reads of the keys' means from
 // L2 and the search.
 template <int D16, int kValues>

@@ -8,7 +8,7 @@
 // lines that they read in part (16 heads of 72 channels of 17 frames, permuted input: 87 us with a token's heads side by side on 9 of
 // 16 lanes).
 // Bound by the memory stream.  Measured, queries and keys of 128 channels: 16 x 1024 tokens, 24 + 24 heads of a packed projection
-// 83.7 us (4.8 TB/s, what a copy reaches); 65536 tokens, 24 + 8 heads 195 us (5.5 TB/s; 229 with neighbouring workgroups on different
+// 83.5 us (4.8 TB/s; why not more was not found); 65536 tokens, 24 + 8 heads 191 us (5.6 TB/s; 229 with neighbouring workgroups on different
 // XCDs and four heads ahead); the permuted input above 61.5 us (3.4 TB/s: a row of 144 bytes lies in two lines or three, in channels 36
 // apart, of which others read the rest).
 //   t = positions[a] * freqs[p] in double, brought to (-1/2, 1/2] revolutions there (a far position times a frequency
