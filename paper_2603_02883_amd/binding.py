@@ -519,6 +519,7 @@ def _workspace(size, device, stream):
         return torch.empty(size, dtype=torch.uint8, device=device)
 
 
+# Calls of the attention path take `stream` as the others do; outputs that they make themselves are made on it.
 def fb4_qk_norm_rope(q, k, positions, freqs, axis_pairs, gamma_q=None, gamma_k=None, eps=1e-6, norm=True, pairing=ROPE_ADJACENT, q_out=None,
                      k_out=None, stream=None):
     """q, k: bf16 cuda [batch][heads][tokens][dim], any strides with contiguous channels (views of a packed projection);

@@ -104,9 +104,9 @@ typedef double select_f64x4 __attribute__((ext_vector_type(4)));
 constexpr int select_sets(int values) { return values == 16 ? 2 : 1; }
 constexpr int select_threads(int values) { return 512 * select_sets(values); }
 
-// A workgroup takes 16 blocks of queries of one head (32 with 513 to 1024 blocks of keys): their scores with all the head's blocks of keys by 16x16x4 MFMAs in double,
-// then the largest `top` of every row.  The channels of a product may come in any order as long as both operands have the same:
-// lane group k of 16 holds channels 16 c + 4 k .. + 3 for the four steps of chunk c, which are 32 bytes of its row.
+// A workgroup takes 16 blocks of queries of one head (32 with 513 to 1024 blocks of keys): their scores with all the head's blocks of
+// keys by 16x16x4 MFMAs in double, then the largest `top` of every row.  The channels of a product may come in any order as long as both
+// operands have the same: lane group k of 16 holds channels 16 c + 4 k .. + 3 for the four steps of chunk c, which are 32 bytes of its row.
 // LDS keeps the scores rounded to fp32, half of what the doubles would take: up to 512 blocks of keys three workgroups and more share a
 // compute unit and one's search runs beside another's products; beyond, one fills it (144 to 160 KiB) and products and search take turns.
 // Rounding keeps the order but for what becomes equal, so the fp32 values decide unless the border falls between

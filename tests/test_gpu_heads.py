@@ -800,3 +800,33 @@ def test_rotation_in_place(F):
             assert e.value.code == F.ERR_INVALID_ARG
     with pytest.raises(F.Fb4Error):
         F.fb4_qk_norm_rope(q, q, pos, freqs, (36,), q_out=qi, k_out=qi)
+
+
+def test_captured_on_a_stream_beside_the_captured_one(F):
+    """A call on a second stream of a capture, with outputs of its own making: replays give what eager calls do."""
+    q, k, v = rand(2, 4, 300, 64, seed=190), rand(2, 2, 500, 64, seed=191), rand(2, 2, 500, 64, seed=192)
+    lens = torch.tensor([[300, 450], [77, 500]], dtype=torch.int32, device="cuda")
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+
+    def both():
+        side.wait_stream(torch.cuda.current_stream())
+        lists = F.fb4_select_key_blocks(q, k, 3, 64, 64, lens, stream=side)
+        a = F.fb4_block_attention(q, k, v, lists, None, 64, 64, lens, want_lse=True, stream=side)
+        b = F.fb4_block_attention(q, k, v, None, None, 64, 64, lens, want_lse=True)
+        del lists
+        torch.cuda.current_stream().wait_stream(side)
+        return (*a, *b)
+    main.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(main):
+        both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=main):
+        held = both()
+    for i in range(4):
+        q.copy_(rand(2, 4, 300, 64, seed=200 + i))
+        k.copy_(rand(2, 2, 500, 64, seed=210 + i))
+        graph.replay()
+        eager = both()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, eager)), i
