@@ -36,8 +36,9 @@
  *     FB4_ERR_INVALID_ARG.  The entry points without a handle
  *     (fb4_attention_scores, fb4_select_salient_tokens, fb4_seda_assign,
  *     fb4_seda_main_anchor, fb4_seda_main_anchor_3d, fb4_qk_norm_rope,
- *     fb4_select_key_blocks, fb4_block_attention, fb4_probe_mfma_rate) run on
- *     the current device.
+ *     fb4_select_key_blocks, fb4_block_attention, fb4_cache_plan,
+ *     fb4_cache_store, fb4_cache_attention, fb4_probe_mfma_rate) run on the
+ *     current device.
  *   - The producer-fused entry points (fb4_layernorm_quantize,
  *     fb4_gelu_quantize) read x as plain IEEE bf16 and hand the quantizer the
  *     producer's bf16 result, to which the rules above then apply.
@@ -89,8 +90,8 @@ int fb4_version(void);
 const char* fb4_strerror(int code);
 
 /* Bytes of caller-provided device workspace any call needs that has no workspace
- * argument: always 0.  (fb4_select_key_blocks and fb4_block_attention have one,
- * and a call of their own that says how much.) */
+ * argument: always 0.  (fb4_select_key_blocks, fb4_block_attention and
+ * fb4_cache_attention have one, and a call of their own that says how much.) */
 size_t fb4_workspace_bytes(void);
 
 /*
@@ -593,6 +594,151 @@ int fb4_block_attention(const void* q, const void* k, const void* v, const int64
                         int heads_k, int64_t tokens_q, int64_t tokens_k, int64_t dim, const int32_t* lens,
                         const int32_t* blocks, int64_t top, int block_q, int block_k, float scale, void* out,
                         const int64_t* out_strides, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Few rows times FB4 weights, without the weights in 16 bits:
+ *   out[r][n] = sum_c x[r][c] * W[n][c] + bias[n],  W = fb4_dequantize(codes, meta)
+ * The weights are decoded exactly, products and sums run on the matrix cores in
+ * fp32 (bias added there), one rounding to the output's type.  What a model
+ * that is run a token or a few at a time does in every layer: a time embedding
+ * through the modulation, new tokens through the projections.
+ *   luts        handle from fb4_build_luts (the weights' formatbook)
+ *   x           device, bf16 [rows][x_row_stride], rows 16-byte aligned; plain
+ *               IEEE bf16 (a NaN or Inf stays in its row); at least 0 rows, at
+ *               most 64 (FB4_ERR_UNSUPPORTED beyond)
+ *   codes,meta  device, one plane as written by fb4_quantize: uint8
+ *               [n][cols/2], 16-byte aligned, and uint16 [n][cols/block], 4-byte
+ *               aligned with block 16 (FB4_ERR_UNSUPPORTED otherwise); a
+ *               DID >= n_dialects gives zero magnitudes
+ *   n           at least 0, below 2^28 (FB4_ERR_UNSUPPORTED beyond)
+ *   cols        a multiple of 32, below 2^28 (FB4_ERR_UNSUPPORTED otherwise); 0:
+ *               the bias, or zeros
+ *   block       32 or 16
+ *   bias        device, float [n] or NULL
+ *   out         device, bf16 or float (out_dtype) [rows][out_row_stride],
+ *               aligned to its elements, on no memory of another argument
+ * A result's sums are formed in an order that depends on rows, n and cols (the
+ * same call always gives the same results).
+ */
+int fb4_matvec(const fb4_luts* luts, const void* x, int64_t rows, int64_t x_row_stride, const uint8_t* codes,
+               const uint16_t* meta, int64_t n, int64_t cols, int block, const float* bias, void* out, int out_dtype,
+               int64_t out_row_stride, void* stream);
+
+/*
+ * A cache of keys and values in pages, for attention over what came before.
+ * Shared by the three calls below:
+ *   page        tokens to a page: 16, 32, 64 or 128 (FB4_ERR_UNSUPPORTED
+ *               otherwise)
+ *   tables      int32 [batch][max_pages]: the pages of every sequence, its
+ *               token t in page tables[b][t / page] at place t % page
+ *   slot        page number * page + place
+ *   cache       uint8 [2][pages][heads_k][page * dim], 16-byte aligned: OCP FP8
+ *               E4M3 elements; per page and head the keys [page][dim], the
+ *               values [dim][page]
+ *   scales      uint8 [2][pages][heads_k], E8M0 (value 2^(s - 127)): one for a
+ *               page's keys and one for its values of every head; element times scale is
+ *               always a bf16 number
+ * fb4_cache_plan: the pages and slots of new tokens, from the sequences'
+ * lengths, on the GPU.  In the order of the sequences:
+ *   adds[b] < 0   the sequence loses its last -adds[b] tokens (all, if it has
+ *                 fewer); pages without a token left go to the end of the free list
+ *   adds[b] > 0   it grows by adds[b] tokens, for which pages are taken off the
+ *                 free list's end.  The first sequence for which pages or token
+ *                 rows do not suffice, and all that would grow behind it, get
+ *                 nothing; so does, by itself, one that would pass max_pages
+ * All that shrink come before all that grow.  Lists and tables beyond what is named here
+ * stay as they were, so a call may be repeated on the same inputs.
+ *   lens, adds  device, int32 [batch]; lens is clamped to 0 .. max_pages * page;
+ *               at most 4096 sequences, batch * max_pages and max_pages * page below 2^31
+ *               (FB4_ERR_UNSUPPORTED beyond)
+ *   free_pages  device, int32 [n_free]: the first free_count[0] entries are
+ *               free; a page that comes back behind the last entry is lost
+ *   lens_out    device, int32 [batch]: the new lengths (may be lens)
+ *   free_count_out  device, int32 [1] (may be free_count)
+ *   starts      device, int32 [batch + 1]: the first new token of every
+ *               sequence among the call's; the last entry is their number
+ *   slots       device, int32 [tokens]: the new tokens' slots, -1 behind the last
+ *               (and for a page that is negative or whose slots pass 31 bits)
+ *   positions   device, int32 [tokens] or NULL: the new tokens' places in their
+ *               sequences, 0 behind the last: the `positions` argument of fb4_qk_norm_rope
+ *               with one axis
+ *   tokens      rows for new tokens, 0 .. 2^31 - 1 (FB4_ERR_UNSUPPORTED beyond)
+ * None of the outputs, tables and free_pages among them, on memory of another
+ * argument but where said.
+ */
+int fb4_cache_plan(const int32_t* lens, const int32_t* adds, int64_t batch, int page, int32_t* tables, int64_t max_pages,
+                   int32_t* free_pages, int64_t n_free, const int32_t* free_count, int32_t* lens_out,
+                   int32_t* free_count_out, int32_t* starts, int32_t* slots, int32_t* positions, int64_t tokens,
+                   void* stream);
+
+/*
+ * Keys and values of new tokens into their slots.  A page's scale is the
+ * smallest power of two whose 448-fold reaches its largest magnitude, and at
+ * least 2^-117; where a token needs a larger one than its page has, the page's
+ * other elements are rounded to it (exact but for those that become subnormal in
+ * E4M3).  A token at place 0 begins its page anew: what the page held before, its scale too,
+ * is forgotten.  Every element is rounded once, to nearest even; Inf and NaN are
+ * stored as NaN and do not count for the scale.
+ *   k, v        device, bf16 [heads_k][tokens][dim] by strides: the channels
+ *               contiguous, rows 16-byte aligned (FB4_ERR_UNSUPPORTED otherwise), on no
+ *               memory of cache or scales
+ *   *_strides   host, (head, token) in elements, each a multiple of 8, at least
+ *               0 and below 2^35 (FB4_ERR_UNSUPPORTED otherwise)
+ *   dim         a multiple of 8, at most 128; heads_k 1..65535; at most
+ *               2^31 - 1 tokens and slots (FB4_ERR_UNSUPPORTED otherwise)
+ *   slots       device, int32 [tokens]; one outside 0 .. pages * page - 1 is
+ *               not stored.  The tokens of a page stand side by side (as
+ *               fb4_cache_plan leaves them); of several for one slot the last counts.  A
+ *               page whose tokens stand in several places is left with any
+ *               of their values
+ */
+int fb4_cache_store(const void* k, const int64_t* k_strides, const void* v, const int64_t* v_strides, int64_t tokens,
+                    int heads_k, int64_t dim, const int32_t* slots, uint8_t* cache, uint8_t* scales, int64_t pages,
+                    int page, void* stream);
+
+/*
+ * Attention of every sequence's last tokens over its pages:
+ *   out[i] = sum_j P[i][j] V[j], P[i] = softmax of scale * Q[i] . K[j]
+ * over the keys j < lens[b], or (causal) the keys up to the query's own place:
+ * query i of the n of a sequence stands at lens[b] - n + i.  Keys and values are decoded
+ * exactly to bf16; products, softmax and roundings as in fb4_block_attention.
+ *   q           device, bf16 [heads][tokens][dim] by q_strides (head, token), as
+ *               k in fb4_cache_store
+ *   heads, heads_k  as in fb4_block_attention (heads at most 65535)
+ *   cache, scales, pages, page, dim  as in fb4_cache_store
+ *   tables      device, int32 [batch][max_pages]; the keys of an entry outside
+ *               0 .. pages - 1 are skipped
+ *   lens        device, int32 [batch]: keys of every sequence, clamped to 0 ..
+ *               max_pages * page (below 2^31, FB4_ERR_UNSUPPORTED beyond)
+ *   starts      device, int32 [batch + 1], ascending: the queries of sequence b
+ *               are the rows starts[b] .. starts[b + 1] - 1, clamped to 0 ..
+ *               tokens (what fb4_cache_plan gives)
+ *   batch       at most 4096; tokens * heads / heads_k below 2^31
+ *               (FB4_ERR_UNSUPPORTED beyond)
+ *   causal      0 or 1
+ *   scale       as in fb4_block_attention
+ *   out         device, bf16 [tokens][heads][dim] by out_strides (head, token), rows
+ *               16-byte aligned, none overlapping another or an input: the rows that
+ *               fb4_quantize takes
+ *   lse         device, float [tokens][heads] or NULL
+ *   workspace   device, 16-byte aligned, at least
+ *               fb4_cache_attention_workspace() bytes (FB4_ERR_INVALID_ARG
+ *               otherwise; 0 for a negative or unserved size); may be NULL where that is 0; free
+ *               again when the call's work on the stream is done
+ * A query without a key, infinite and NaN scores: as in fb4_block_attention.  A
+ * value behind a query's last key never touches its result, NaN or not.  Rows of no sequence keep what
+ * they held, in out and in lse.  A row's sums are formed in an order that depends on
+ * the call's sizes and all sequences' lengths (the same call always gives the
+ * same results); the launch does not depend on what lens, starts and tables hold, so a
+ * captured call may be replayed with other lengths.
+ */
+size_t fb4_cache_attention_workspace(int64_t tokens, int heads, int heads_k, int64_t dim, int page, int64_t max_pages,
+                                     int64_t batch);
+int fb4_cache_attention(const void* q, const int64_t* q_strides, int64_t tokens, int heads, int heads_k, int64_t dim,
+                        const uint8_t* cache, const uint8_t* scales, int64_t pages, int page, const int32_t* tables,
+                        int64_t max_pages, const int32_t* lens, const int32_t* starts, int64_t batch, int causal,
+                        float scale, void* out, const int64_t* out_strides, float* lse, void* workspace,
+                        size_t workspace_bytes, void* stream);
 
 /*
  * Diagnostic, not part of the paper's method: launches a kernel that does

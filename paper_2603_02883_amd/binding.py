@@ -89,6 +89,12 @@ def _load():
     lib.fb4_block_attention.argtypes = [p, p, p, st, i64, i32, i32, i64, i64, i64, p, p, i64, i32, i32, ctypes.c_float, p, st, p, p, size, p]
     lib.fb4_block_attention_workspace.argtypes = [i64, i32, i32, i64, i64, i64, i64, i32, i32]
     lib.fb4_block_attention_workspace.restype = size
+    lib.fb4_matvec.argtypes = [p, p, i64, i64, p, p, i64, i64, i32, p, p, i32, i64, p]
+    lib.fb4_cache_plan.argtypes = [p, p, i64, i32, p, i64, p, i64, p, p, p, p, p, p, i64, p]
+    lib.fb4_cache_store.argtypes = [p, st, p, st, i64, i32, i64, p, p, p, i64, i32, p]
+    lib.fb4_cache_attention.argtypes = [p, st, i64, i32, i32, i64, p, p, i64, i32, p, i64, p, p, i64, i32, ctypes.c_float, p, st, p, p, size, p]
+    lib.fb4_cache_attention_workspace.argtypes = [i64, i32, i32, i64, i32, i64, i64]
+    lib.fb4_cache_attention_workspace.restype = size
     lib.fb4_probe_mfma_rate.argtypes = [i64, i64, i32, p, ctypes.POINTER(ctypes.c_double), p]
     lib.fb4_gelu_table_host.argtypes = [i32, p, ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t)]
     lib.fb4_gelu_quantize.argtypes = [p, ctypes.POINTER(fb4_opts), p, i64, i64, i64, i32, p, p, i32, p, p, p]
@@ -106,6 +112,7 @@ EXPORTS = ["fb4_version", "fb4_strerror", "fb4_workspace_bytes", "fb4_build_luts
            "fb4_gelu_table_host", "fb4_attention_scores", "fb4_select_salient_tokens",
            "fb4_seda_assign", "fb4_seda_main_anchor", "fb4_seda_main_anchor_3d", "fb4_qk_norm_rope",
            "fb4_select_key_blocks", "fb4_select_key_blocks_workspace", "fb4_block_attention", "fb4_block_attention_workspace",
+           "fb4_matvec", "fb4_cache_plan", "fb4_cache_store", "fb4_cache_attention", "fb4_cache_attention_workspace",
            "fb4_probe_mfma_rate"]
 
 
@@ -321,6 +328,88 @@ class HeadsCall:
                                         0 if workspace is None else workspace.numel(), s)
 
 
+def _pair_strides(t):
+    """(head, token) strides of a [heads][tokens][dim] tensor, likewise."""
+    return (ctypes.c_int64 * 2)(*[t.stride(i) if t.shape[i] > 1 else 0 for i in range(2)])
+
+
+class ServingCall:
+    """The calls that serve a few tokens at a time through ctypes, checked likewise."""
+
+    @staticmethod
+    def matvec(h, x, codes, meta, block, bias, out, device, s):
+        where = "fb4_matvec"
+        _on_device(where, device, (x, torch.bfloat16), (codes, torch.uint8), (meta, torch.int16), (bias, torch.float32))
+        _require(out.is_cuda and out.device.index == device and out.dtype in (torch.bfloat16, torch.float32), where)
+        _require(x.dim() == 2 and codes.dim() == 2 and block in (16, 32), where)
+        (rows, cols), n = x.shape, codes.shape[0]
+        _require(codes.shape[1] * 2 == cols and meta.shape == (n, cols // block) and out.shape == (rows, n) and (bias is None or bias.shape == (n,)), where)
+        for t in (codes, meta, bias):
+            _require(t is None or t.is_contiguous(), where, ERR_UNSUPPORTED)
+        for t in (x, out):
+            _require(t.shape[1] <= 1 or t.numel() == 0 or t.stride(1) == 1, where, ERR_UNSUPPORTED)
+        return _lib.fb4_matvec(h, _dp(x), rows, x.stride(0) if rows > 1 else cols, _dp(codes), _dp(meta), n, cols, block, _dp(bias), _dp(out),
+                               DTYPE_F32 if out.dtype is torch.float32 else DTYPE_BF16, out.stride(0) if rows > 1 else n, s)
+
+    @staticmethod
+    def cache_plan(lens, adds, tables, free_pages, free_count, page, lens_out, free_count_out, starts, slots, positions, device, s):
+        where = "fb4_cache_plan"
+        every = (lens, adds, tables, free_pages, free_count, lens_out, free_count_out, starts, slots, positions)
+        _on_device(where, device, *[(t, torch.int32) for t in every])
+        _require(tables.dim() == 2 and free_pages.dim() == slots.dim() == 1 and 0 < page <= INT_MAX, where)
+        (batch, max_pages), tokens = tables.shape, slots.shape[0]
+        for t, n in ((lens, batch), (adds, batch), (lens_out, batch), (starts, batch + 1), (free_count, 1), (free_count_out, 1), (positions, tokens)):
+            _require(t is None or t.shape == (n,), where)
+        for t in every:
+            _require(t is None or t.is_contiguous(), where, ERR_UNSUPPORTED)
+        return _lib.fb4_cache_plan(_dp(lens), _dp(adds), batch, page, _dp(tables), max_pages, _dp(free_pages), free_pages.shape[0], _dp(free_count),
+                                   _dp(lens_out), _dp(free_count_out), _dp(starts), _dp(slots), _dp(positions), tokens, s)
+
+    @staticmethod
+    def _cache(where, cache, scales, heads_k, dim, page):
+        """Pages of a cache for these heads and channels, checked."""
+        _require(0 < page <= INT_MAX and scales.dim() == 3, where)
+        pages = scales.shape[1]
+        _require(scales.shape == (2, pages, heads_k) and cache.shape == (2, pages, heads_k, page * dim), where)
+        for t in (cache, scales):
+            _require(t.is_contiguous(), where, ERR_UNSUPPORTED)
+        return pages
+
+    @staticmethod
+    def cache_store(k, v, slots, cache, scales, page, device, s):
+        where = "fb4_cache_store"
+        _on_device(where, device, (k, torch.bfloat16), (v, torch.bfloat16), (slots, torch.int32), (cache, torch.uint8), (scales, torch.uint8))
+        _require(k.dim() == 3 and v.shape == k.shape and slots.shape == (k.shape[1],), where)
+        heads, tokens, dim = k.shape
+        pages = ServingCall._cache(where, cache, scales, heads, dim, page)
+        _require(heads <= INT_MAX and slots.is_contiguous(), where, ERR_UNSUPPORTED)
+        for t in (k, v):
+            _require(dim == 1 or t.numel() == 0 or t.stride(2) == 1, where, ERR_UNSUPPORTED)
+        return _lib.fb4_cache_store(_dp(k), _pair_strides(k), _dp(v), _pair_strides(v), tokens, heads, dim, _dp(slots), _dp(cache), _dp(scales), pages, page, s)
+
+    @staticmethod
+    def cache_attention(q, cache, scales, tables, lens, starts, page, scale, causal, out, lse, workspace, device, s):
+        """(the bytes needed, where there is no workspace and has to be one)"""
+        where = "fb4_cache_attention"
+        _on_device(where, device, (q, torch.bfloat16), (cache, torch.uint8), (scales, torch.uint8), (tables, torch.int32), (lens, torch.int32),
+                   (starts, torch.int32), (out, torch.bfloat16), (lse, torch.float32), (workspace, torch.uint8))
+        _require(q.dim() == 3 and scales.dim() == 3 and tables.dim() == 2, where)
+        (heads, tokens, dim), heads_k, (batch, max_pages) = q.shape, scales.shape[2], tables.shape
+        pages = ServingCall._cache(where, cache, scales, heads_k, dim, page)
+        _require(lens.shape == (batch,) and starts.shape == (batch + 1,) and out.shape == (tokens, heads, dim) and (lse is None or lse.shape == (tokens, heads)), where)
+        _require(max(heads, heads_k) <= INT_MAX, where, ERR_UNSUPPORTED)
+        for t in (tables, lens, starts, lse):
+            _require(t is None or t.is_contiguous(), where, ERR_UNSUPPORTED)
+        for t in (q, out):
+            _require(dim == 1 or t.numel() == 0 or t.stride(2) == 1, where, ERR_UNSUPPORTED)
+        size = _lib.fb4_cache_attention_workspace(tokens, heads, heads_k, dim, page, max_pages, batch)
+        if workspace is None and size:
+            return size
+        return _lib.fb4_cache_attention(_dp(q), _pair_strides(q), tokens, heads, heads_k, dim, _dp(cache), _dp(scales), pages, page, _dp(tables), max_pages,
+                                        _dp(lens), _dp(starts), batch, 1 if causal else 0, float(scale), _dp(out), _pair_strides(out.transpose(0, 1)), _dp(lse),
+                                        _dp(workspace), 0 if workspace is None else workspace.numel(), s)
+
+
 def _load_call():
     """The C module of this interpreter (by its path: a module of another one is not taken), built if it is missing and can be."""
     if not os.path.exists(_build.CALL):
@@ -345,6 +434,7 @@ def _load_call():
 
 _call = _load_call()
 _heads_call = HeadsCall if _call is CtypesCall else _call
+_serving_call = ServingCall
 
 
 def _stream(stream):
@@ -579,6 +669,68 @@ def fb4_block_attention(q, k, v, blocks=None, scale=None, block_q=128, block_k=1
     if rc > 0:
         rc = _heads_call.block_attention(q, k, v, blocks, float(scale), block_q, block_k, lens, out, lse, _workspace(rc, q.device, stream), _get_device(), s)
     _check(rc, "fb4_block_attention")
+    return out if lse is None else (out, lse)
+
+
+# Serving a few tokens at a time: weights in 4 bits, keys and values in 8.
+def fb4_matvec(luts, x, codes, meta, block=32, bias=None, out=None, out_dtype=DTYPE_BF16, stream=None):
+    """x: bf16 cuda [rows][cols] (row stride allowed), at most 64 rows; codes, meta: one plane of fb4_quantize of the weights [n][cols]; bias:
+    float32 cuda [n] or None.  Returns x @ fb4_dequantize(codes, meta).T + bias, bf16 or float32 [rows][n] (out's type, if that is given)."""
+    _require(x.is_cuda, "fb4_matvec")
+    if out is None:
+        _require(x.dim() == 2 and codes.dim() == 2, "fb4_matvec")
+        out = _output((x.shape[0], codes.shape[0]), torch.bfloat16 if out_dtype == DTYPE_BF16 else torch.float32, x.device, stream)
+    _check(_serving_call.matvec(luts.handle, x, codes, meta, block, bias, out, _get_device(), _stream(stream)), "fb4_matvec")
+    return out
+
+
+def fb4_cache_plan(lens, adds, tables, free_pages, free_count, page, tokens, lens_out=None, free_count_out=None, starts=None, slots=None, positions=None,
+                   stream=None):
+    """lens, adds: int32 cuda [batch], tokens that every sequence holds and gets (negative: loses); tables: int32 cuda [batch][max_pages] and
+    free_pages: int32 cuda [n], the free pages first, both updated in place; free_count: int32 cuda [1]; tokens: rows for new tokens.
+    Returns (lens_out, free_count_out, starts [batch + 1], slots [tokens], positions [tokens]), int32; lens and free_count may be given as
+    their own outputs."""
+    _require(lens.is_cuda and tokens >= 0, "fb4_cache_plan")
+    make = lambda t, n: _output((n,), torch.int32, lens.device, stream) if t is None else t
+    batch = lens.shape[0]
+    lens_out, free_count_out, starts = make(lens_out, batch), make(free_count_out, 1), make(starts, batch + 1)
+    slots, positions = make(slots, tokens), make(positions, tokens)
+    _require(slots.shape == (tokens,), "fb4_cache_plan")
+    _check(_serving_call.cache_plan(lens, adds, tables, free_pages, free_count, page, lens_out, free_count_out, starts, slots, positions, _get_device(),
+                                    _stream(stream)), "fb4_cache_plan")
+    return lens_out, free_count_out, starts, slots, positions
+
+
+def fb4_cache_store(k, v, slots, cache, scales, page, stream=None):
+    """k, v: bf16 cuda [heads_k][tokens][dim], any strides with contiguous channels; slots: int32 cuda [tokens] (fb4_cache_plan); cache: uint8
+    cuda [2][pages][heads_k][page * dim] and scales: uint8 cuda [2][pages][heads_k], updated in place.  Returns (cache, scales)."""
+    _require(k.is_cuda, "fb4_cache_store")
+    _check(_serving_call.cache_store(k, v, slots, cache, scales, page, _get_device(), _stream(stream)), "fb4_cache_store")
+    return cache, scales
+
+
+def fb4_cache_attention(q, cache, scales, tables, lens, starts, page, scale=None, causal=True, out=None, lse=None, want_lse=False, workspace=None, stream=None):
+    """q: bf16 cuda [heads][tokens][dim], any strides with contiguous channels; cache, scales, page as in fb4_cache_store; tables: int32 cuda
+    [batch][max_pages]; lens: int32 cuda [batch], keys of every sequence; starts: int32 cuda [batch + 1], their first queries (both as
+    fb4_cache_plan gives them); scale: dim ** -0.5 if None.  Returns bf16 [tokens][heads][dim] -- rows of fb4_quantize -- (and the logarithms
+    of the sums, float32 [tokens][heads], if asked).  Rows of no sequence are left as they were (zeros if not given)."""
+    _require(q.is_cuda, "fb4_cache_attention")
+    if out is None or scale is None or (want_lse and lse is None):
+        _require(q.dim() == 3, "fb4_cache_attention")
+        heads, tokens, dim = q.shape
+        if out is None:
+            out = _output((tokens, heads, dim), torch.bfloat16, q.device, stream, zeros=True)
+        if want_lse and lse is None:
+            lse = _output((tokens, heads), torch.float32, q.device, stream, zeros=True)
+        if scale is None:
+            _require(dim > 0, "fb4_cache_attention")
+            scale = dim ** -0.5
+    s = _stream(stream)
+    args = (q, cache, scales, tables, lens, starts, page, float(scale), bool(causal), out, lse)
+    rc = _serving_call.cache_attention(*args, workspace, _get_device(), s)
+    if rc > 0:
+        rc = _serving_call.cache_attention(*args, _workspace(rc, q.device, stream), _get_device(), s)
+    _check(rc, "fb4_cache_attention")
     return out if lse is None else (out, lse)
 
 

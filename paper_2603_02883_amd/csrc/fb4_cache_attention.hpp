@@ -1,0 +1,493 @@
+// Attention over a cache of pages in 8 bits (fb4_cache_attention).
+//
+// S^T = K Q^T and O^T = V^T P^T as 16x16x32 bf16 MFMAs, one pass over the keys with the running maximum and sum of the softmax, 64 keys a
+// step of a wavefront.  A first operand's lane holds eight successive values of one row of 16, so keys come [key][channel] and values
+// [channel][key] out of the cache straight into registers; the converter from E4M3 to bf16 takes the page's scale along (a power of two:
+// exact).  Which keys make up the 16 rows of a product is free, and so is the order of the channels as long as both operands agree: lane group g =
+// lane / 16 of the accumulators holds rows 4 g .. 4 g + 3, and row r of tile t is key 16 (r / 4) + 4 t + r % 4 of the 64, so that after four
+// tiles group g has the 16 successive keys 16 g .. of the lane's query -- as the second product's operands want them: P goes from
+// accumulators to operand without leaving the lane, and a lane reads 16 bytes of V, the same 16 keys of one channel.  A page has at
+// least 16 tokens, so each of these sixteenths lies in one page.
+//
+// Rows of a product's second operand are the queries of a key head: the n tokens of a sequence times the query heads that share it, token
+// by token, cut into tiles of 16 kSets.  A workgroup takes one tile, and its wavefronts every fourth step.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace fb4 {
+
+constexpr uint32_t kCacheWaves = 4, kCacheStep = 64;   // keys
+constexpr uint32_t kCacheMaxBatch = 4096;
+constexpr float kCacheLog2E = 1.44269504088896340736f, kCacheLn2 = 0.69314718055994530942f;
+
+typedef __bf16 cache_bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 cache_bf16x8 __attribute__((ext_vector_type(8)));
+typedef float cache_f32x2 __attribute__((ext_vector_type(2)));
+typedef float cache_f32x4 __attribute__((ext_vector_type(4)));
+
+struct CacheStrides {
+    uint32_t head, token;   // in units of 8 elements
+};
+struct CacheShape {
+    uint32_t tokens, max_pages, pages;
+    uint16_t batch, heads, heads_k, target;   // target: workgroups that the keys are shared among, where parts are made
+    uint8_t page_bits, dim8;                  // dim / 8
+    uint8_t causal, rows16;                   // rows of a tile / 16
+    float scale;
+};
+
+#define FB4_INLINE __attribute__((always_inline))
+
+// ------------------------------------------------------------------------------------------------ which part of the work
+// Sequences lie in `starts` one behind the other; the tiles of sequence b are numbered from place(b) = starts[b] * group / rows + b on, which
+// leaves each its whole tiles and a begun one, so that a workgroup finds its sequence from `starts` alone.
+struct CacheRows {
+    uint32_t first, n;      // first query token, query tokens
+    uint32_t len;           // keys
+};
+__device__ __forceinline__ uint32_t start_of(const int32_t* starts, uint32_t b, uint32_t tokens) { return (uint32_t)min(max(starts[b], 0), (int32_t)tokens); }
+// (group 0: the start itself, for the sequence of a token)
+__device__ __forceinline__ uint32_t place_of(uint32_t start, uint32_t b, uint32_t group, uint32_t tile_rows) { return group ? start * group / tile_rows + b : start; }
+__device__ __forceinline__ CacheRows rows_of(const int32_t* starts, const int32_t* lens, uint32_t b, const CacheShape& s)
+{
+    CacheRows r;
+    r.first = start_of(starts, b, s.tokens);
+    const uint32_t end = start_of(starts, b + 1u, s.tokens);
+    r.n = end > r.first ? end - r.first : 0u;
+    r.len = (uint32_t)min(max((int64_t)lens[b], (int64_t)0), (int64_t)s.max_pages << s.page_bits);
+    return r;
+}
+__device__ __forceinline__ uint32_t tiles_of(uint32_t n, uint32_t group, uint32_t tile_rows) { return (n * group + tile_rows - 1u) / tile_rows; }
+__device__ __forceinline__ uint32_t steps_of(uint32_t len) { return (len + kCacheStep - 1u) / kCacheStep; }
+
+// The last sequence whose place is at most `slot`, by a wavefront: 64 candidates at a time.
+__device__ __forceinline__ uint32_t sequence_of(const int32_t* starts, uint32_t slot, uint32_t group, uint32_t tile_rows, const CacheShape& s)
+{
+    const uint32_t lane = threadIdx.x & 63u, stride = (s.batch + 63u) / 64u;
+    uint32_t b = lane * stride;
+    uint64_t yes = __ballot(b < s.batch && place_of(start_of(starts, b < s.batch ? b : 0u, s.tokens), b, group, tile_rows) <= slot);
+    const uint32_t base = (uint32_t)(63 - __builtin_clzll(yes | 1ull)) * stride;
+    if (stride == 1u) return base;
+    b = base + lane;
+    yes = __ballot(lane < stride && b < s.batch && place_of(start_of(starts, min(b, s.batch - 1u), s.tokens), b, group, tile_rows) <= slot);
+    return base + (uint32_t)(63 - __builtin_clzll(yes | 1ull));
+}
+
+// Parts: where tiles are few, the keys of each are shared by several workgroups, of `share` steps at most -- the same for all, so that
+// sequences of unlike lengths get parts by their lengths.  share: all tiles' steps over s.target workgroups.
+constexpr uint32_t kCacheLeastShare = 2 * kCacheWaves;
+__device__ __forceinline__ uint32_t share_of(const int32_t* starts, const int32_t* lens, uint32_t group, uint32_t tile_rows, const CacheShape& s)
+{
+    uint64_t sum = 0;
+    for (uint32_t b = threadIdx.x & 63u; b < s.batch; b += 64u) {
+        const CacheRows r = rows_of(starts, lens, b, s);
+        sum += (uint64_t)tiles_of(r.n, group, tile_rows) * steps_of(r.len);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    sum *= s.heads_k;
+    return (uint32_t)max((sum + s.target - 1u) / s.target, (uint64_t)kCacheLeastShare);
+}
+__device__ __forceinline__ uint32_t parts_of(uint32_t len, uint32_t share) { return max((steps_of(len) + share - 1u) / share, 1u); }
+
+// Walks the sequences' tiles times parts, by a wavefront: until position `at` (-> its sequence, and `at` from its first one on), or
+// to sequence `stop` (-> the position of its first one in `at`).  Behind all: batch.
+__device__ __forceinline__ uint32_t walk_parts(const int32_t* starts, const int32_t* lens, uint32_t group, uint32_t tile_rows, uint32_t share, uint32_t stop,
+                                               uint32_t& at, const CacheShape& s)
+{
+    const uint32_t lane = threadIdx.x & 63u;
+    uint32_t before = 0;
+    for (uint32_t b0 = 0; b0 < s.batch; b0 += 64u) {
+        const uint32_t b = b0 + lane;
+        uint32_t mine = 0;
+        if (b < s.batch) {
+            const CacheRows r = rows_of(starts, lens, b, s);
+            mine = tiles_of(r.n, group, tile_rows) * parts_of(r.len, share);
+        }
+        uint32_t sum = mine;
+#pragma unroll
+        for (uint32_t d = 1; d < 64; d *= 2) {
+            const uint32_t y = __shfl_up(sum, d);
+            if (lane >= d) sum += y;
+        }
+        if (stop < b0 + 64u) {
+            at = before + __shfl(sum - mine, stop - b0);
+            return stop;
+        }
+        const uint64_t behind = __ballot(before + sum > at);
+        if (stop == 0xFFFFFFFFu && behind) {
+            const uint32_t l = (uint32_t)__builtin_ctzll(behind);
+            at -= before + __shfl(sum - mine, l);
+            return b0 + l;
+        }
+        before += __shfl(sum, 63);
+    }
+    return s.batch;
+}
+
+// ------------------------------------------------------------------------------------------------ attention
+// kD32: channels / 32, rounded up; kWhole: a row is kD32 whole steps and 16-byte pieces.  kSplit: parts, into the workspace: floats
+// [position][16 kSets][dim], then {maximum, sum} of every row; position = (parts in front) * heads_k + key head.
+//
+// Weights are exp2((s - m) c), c = scale log2 e, m a reference that moves only when a weight would pass 2^8: the difference of two scores is
+// small where its weight is not, however large both are.
+template <int kD32, int kSets, bool kWhole, bool kSplit>
+__global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* scales, const int32_t* tables,
+                                                                          const int32_t* lens, const int32_t* starts, uint16_t* out, float* lse, CacheStrides sq,
+                                                                          CacheStrides so, CacheShape s)
+{
+    constexpr uint32_t kRows = 16 * kSets, kPitch = 32 * kD32 + 4;
+    __shared__ __align__(16) float meet[kCacheWaves][16][kPitch];
+    __shared__ float2 state[kCacheWaves][16];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t r = lane & 15u, g = lane >> 4;
+    auto scalar = [](uint32_t x) FB4_INLINE { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
+    const uint32_t position = scalar(blockIdx.x / s.heads_k), hk = blockIdx.x - position * s.heads_k, group = scalar((uint32_t)s.heads / s.heads_k);
+    // ---- sequence, tile, steps
+    uint32_t b, tile, from = 0, to;
+    CacheRows rows;
+    if (kSplit) {
+        const uint32_t share = scalar(share_of(starts, lens, group, kRows, s));
+        uint32_t at = position;
+        b = scalar(walk_parts(starts, lens, group, kRows, share, 0xFFFFFFFFu, at, s));
+        if (b >= s.batch) return;
+        rows = rows_of(starts, lens, b, s);
+        const uint32_t parts = parts_of(rows.len, share);
+        tile = scalar(at) / parts;
+        const uint32_t part = scalar(at) - tile * parts, steps = steps_of(rows.len);
+        from = (uint32_t)((uint64_t)steps * part / parts);
+        to = (uint32_t)((uint64_t)steps * (part + 1u) / parts);
+    } else {
+        b = scalar(sequence_of(starts, position, group, kRows, s));
+        rows = rows_of(starts, lens, b, s);
+        tile = position - place_of(rows.first, b, group, kRows);
+        if (tile >= tiles_of(rows.n, group, kRows)) return;
+        to = steps_of(rows.len);
+    }
+    const uint32_t n_rows = min(rows.n * group - tile * kRows, kRows);
+    // ---- this lane's queries (behind the last that one again), and the keys before which each ends
+    const uint32_t pieces = s.dim8, dim = pieces * 8u;
+    cache_bf16x8 qf[kSets][kD32];
+    uint32_t limit[kSets];
+    auto limit_of = [&](uint32_t row) FB4_INLINE {
+        const uint32_t token = (tile * kRows + row) / group;
+        return s.causal ? (uint32_t)max((int64_t)rows.len - (int64_t)rows.n + (int64_t)token + 1, (int64_t)0) : rows.len;
+    };
+#pragma unroll
+    for (int u = 0; u < kSets; ++u) {
+        const uint32_t row = min(16u * u + r, n_rows - 1u), at = tile * kRows + row, token = at / group, head = hk * group + (at - token * group);
+        limit[u] = limit_of(row);
+        const uint16_t* x = q + ((size_t)head * sq.head + (size_t)(rows.first + token) * sq.token) * 8u;
+#pragma unroll
+        for (int i = 0; i < kD32; ++i) {
+            uint4 w = make_uint4(0, 0, 0, 0);
+            if (kWhole || kD32 * g + i < pieces) w = reinterpret_cast<const uint4*>(x)[kD32 * g + i];
+            qf[u][i] = __builtin_bit_cast(cache_bf16x8, w);
+        }
+    }
+    const uint32_t least = scalar(limit_of(0)), end = scalar(limit_of(n_rows - 1u));
+    to = min(to, steps_of(end));
+    const uint32_t bits = s.page_bits, in_page = (1u << bits) - 1u, held = (rows.len + in_page) >> bits;   // pages with a key
+    const int32_t* table = tables + (size_t)b * s.max_pages;
+    const size_t page_bytes = (size_t)dim << bits;
+    const uint8_t* values = cache + (size_t)s.pages * s.heads_k * page_bytes;
+
+    // ---- a step's operands.  For the keys a lane is in the sixteenth r / 4, for the values in the sixteenth g.
+    struct Where {
+        int32_t k, v;   // pages, -1: none
+    };
+    auto page_of = [&](uint32_t key) FB4_INLINE {
+        const uint32_t i = key >> bits;
+        const int32_t p = i < held ? table[i] : -1;
+        return (uint32_t)p < s.pages ? p : -1;
+    };
+    auto find = [&](uint32_t step) FB4_INLINE { return Where{page_of(step * kCacheStep + 16u * (r >> 2)), page_of(step * kCacheStep + 16u * g)}; };
+    uint4 kr[4][(kD32 + 1) / 2], vr[2 * kD32];   // four tiles of keys; 16 channels each
+    float k_scale = 0.0f, v_scale = 0.0f;
+    auto scale_of = [&](uint32_t byte) FB4_INLINE { return __builtin_bit_cast(float, byte << 23); };
+    auto fetch_k = [&](uint32_t step, int32_t p) FB4_INLINE {
+        const size_t at = (size_t)max(p, 0) * s.heads_k + hk;   // (what no page has: another's, whose products are replaced)
+        k_scale = scale_of(scales[at]);
+        const uint8_t* base = cache + at * page_bytes + (size_t)((step * kCacheStep + 16u * (r >> 2) + (r & 3u)) & in_page) * dim + kD32 * 8u * g;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const uint8_t* x = base + 4u * t * dim;
+            if (kWhole && kD32 % 2 == 0) {
+#pragma unroll
+                for (int i = 0; i < kD32 / 2; ++i) kr[t][i] = reinterpret_cast<const uint4*>(x)[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < kD32; ++i) {
+                    uint2 w = make_uint2(0, 0);
+                    if (kWhole || kD32 * g + i < pieces) w = reinterpret_cast<const uint2*>(x)[i];
+                    if (i % 2) kr[t][i / 2].z = w.x, kr[t][i / 2].w = w.y;
+                    else kr[t][i / 2].x = w.x, kr[t][i / 2].y = w.y;
+                }
+            }
+        }
+    };
+    auto fetch_v = [&](uint32_t step, int32_t p) FB4_INLINE {
+        const size_t at = (size_t)max(p, 0) * s.heads_k + hk;
+        v_scale = scale_of(scales[(size_t)s.pages * s.heads_k + at]);
+        const uint8_t* base = values + at * page_bytes + ((size_t)r << bits) + ((step * kCacheStep + 16u * g) & in_page);
+#pragma unroll
+        for (int d = 0; d < 2 * kD32; ++d) {
+            vr[d] = make_uint4(0, 0, 0, 0);
+            if (p >= 0 && (kWhole || 16u * d + r < dim)) vr[d] = *reinterpret_cast<const uint4*>(base + ((size_t)(16u * d) << bits));
+        }
+    };
+    auto decode = [&](uint32_t lo, uint32_t hi, float f) FB4_INLINE {
+        const cache_bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, f, false), b2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, f, true);
+        const cache_bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, f, true);
+        return cache_bf16x8{a[0], a[1], b2[0], b2[1], c[0], c[1], d[0], d[1]};
+    };
+
+    const float factor = s.scale * kCacheLog2E;
+    cache_f32x4 o[kSets][2 * kD32];
+    float reference[kSets], sum[kSets];
+#pragma unroll
+    for (int u = 0; u < kSets; ++u) {
+        reference[u] = -__builtin_inff();
+        sum[u] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < 2 * kD32; ++d) o[u][d] = cache_f32x4{0, 0, 0, 0};
+    }
+    uint32_t step = from + wave;
+    Where here = {-1, -1}, next = {-1, -1};
+    if (step < to) {
+        here = find(step);
+        fetch_k(step, here.k);
+        fetch_v(step, here.v);
+        next = find(step + kCacheWaves);
+    }
+    for (; step < to; step += kCacheWaves) {
+        const bool more = step + kCacheWaves < to;
+        // ---- S^T
+        cache_f32x4 sc[kSets][4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+            for (int u = 0; u < kSets; ++u) sc[u][t] = cache_f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < kD32; ++i) {
+                const cache_bf16x8 a = i % 2 ? decode(kr[t][i / 2].z, kr[t][i / 2].w, k_scale) : decode(kr[t][i / 2].x, kr[t][i / 2].y, k_scale);
+#pragma unroll
+                for (int u = 0; u < kSets; ++u) sc[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[u][i], sc[u][t], 0, 0, 0);
+            }
+        }
+        const Where after = next;
+        if (more) {
+            fetch_k(step + kCacheWaves, after.k);
+            next = find(step + 2u * kCacheWaves);
+        }
+        // ---- what a query does not see
+        const uint32_t key = step * kCacheStep + 16u * g;   // the first of this lane's
+        const bool cut = step * kCacheStep + kCacheStep > least || __any(here.v < 0);
+        if (cut) {
+#pragma unroll
+            for (int u = 0; u < kSets; ++u) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sc[u][t][i] = here.v < 0 || key + 4u * t + i >= limit[u] ? -__builtin_inff() : sc[u][t][i];
+                }
+            }
+        }
+        // ---- weights
+        cache_bf16x8 p[kSets][2];
+#pragma unroll
+        for (int u = 0; u < kSets; ++u) {
+            float larger = -__builtin_inff();
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) larger = fmaxf(larger, sc[u][t][i]);
+            }
+            if (__any((larger - reference[u]) * factor > 8.0f)) {
+                // (finite, so that a score of +Inf has an infinite weight and sum: no number in the output, +Inf in lse)
+                larger = fmaxf(larger, reference[u]);
+                larger = fmaxf(larger, __shfl_xor(larger, 16));
+                larger = fminf(fmaxf(larger, __shfl_xor(larger, 32)), 0x1.fffffep127f);
+                const float shrink = reference[u] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((reference[u] - larger) * factor);
+                reference[u] = larger;
+                sum[u] *= shrink;
+#pragma unroll
+                for (int d = 0; d < 2 * kD32; ++d) o[u][d] *= shrink;
+            }
+            const float base = reference[u] == -__builtin_inff() ? 0.0f : reference[u];
+            float w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = __builtin_amdgcn_exp2f((sc[u][i / 4][i % 4] - base) * factor);
+            // (the sum from the unrounded weights, pairwise: one rounding of the row's a step)
+            sum[u] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7])) + (((w[8] + w[9]) + (w[10] + w[11])) + ((w[12] + w[13]) + (w[14] + w[15])));
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t y[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    y[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((cache_f32x2{w[8 * h + 2 * i], w[8 * h + 2 * i + 1]}), cache_bf16x2));
+                p[u][h] = __builtin_bit_cast(cache_bf16x8, make_uint4(y[0], y[1], y[2], y[3]));
+            }
+        }
+        // ---- O^T.  What lies behind a query's last key has weight 0, but 0 times NaN is none: behind the sequence's end (where a page may
+        // hold anything) the values become zeros; a NaN in sight of some of the queries only takes the products query by query.
+        bool bad = false;
+        if (cut) {
+            auto ahead = [](uint32_t n, int w) FB4_INLINE { return n >= 4u * w + 4u ? 0xFFFFFFFFu : n <= 4u * w ? 0u : (1u << (8u * (n - 4u * w))) - 1u; };
+            const uint32_t n = rows.len > key ? min(rows.len - key, 16u) : 0u;
+#pragma unroll
+            for (int d = 0; d < 2 * kD32; ++d) {
+                vr[d] = make_uint4(vr[d].x & ahead(n, 0), vr[d].y & ahead(n, 1), vr[d].z & ahead(n, 2), vr[d].w & ahead(n, 3));
+                const uint32_t w[4] = {vr[d].x, vr[d].y, vr[d].z, vr[d].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) bad = bad || (((w[i] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u);   // (0x7F, no sum carries over)
+            }
+            bad = __any(bad);
+            if (bad) {
+#pragma unroll 1
+                for (uint32_t c = 0; c < 16; ++c) {
+#pragma unroll
+                    for (int u = 0; u < kSets; ++u) {
+                        const uint32_t sees = __shfl(limit[u], c), m = sees > key ? min(sees - key, 16u) : 0u;
+#pragma unroll
+                        for (int d = 0; d < 2 * kD32; ++d) {
+                            cache_f32x4 x = {0, 0, 0, 0};
+                            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode(vr[d].x & ahead(m, 0), vr[d].y & ahead(m, 1), v_scale), p[u][0], x, 0, 0, 0);
+                            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode(vr[d].z & ahead(m, 2), vr[d].w & ahead(m, 3), v_scale), p[u][1], x, 0, 0, 0);
+                            if (r == c) o[u][d] += x;
+                        }
+                    }
+                }
+            }
+        }
+        if (!bad) {
+#pragma unroll
+            for (int d = 0; d < 2 * kD32; ++d) {
+                const cache_bf16x8 a0 = decode(vr[d].x, vr[d].y, v_scale), a1 = decode(vr[d].z, vr[d].w, v_scale);
+#pragma unroll
+                for (int u = 0; u < kSets; ++u) {
+                    o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, p[u][0], o[u][d], 0, 0, 0);
+                    o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, p[u][1], o[u][d], 0, 0, 0);
+                }
+            }
+        }
+        here = after;
+        if (more) fetch_v(step + kCacheWaves, here.v);
+    }
+    // ---- the wavefronts meet
+#pragma unroll
+    for (int u = 0; u < kSets; ++u) {
+        sum[u] += __shfl_xor(sum[u], 16);
+        sum[u] += __shfl_xor(sum[u], 32);
+#pragma unroll
+        for (int d = 0; d < 2 * kD32; ++d) *reinterpret_cast<cache_f32x4*>(&meet[wave][r][16 * d + 4 * g]) = o[u][d];
+        if (g == 0) state[wave][r] = make_float2(reference[u], sum[u]);
+        __syncthreads();
+        const uint32_t row = threadIdx.x >> 4, at_row = 16u * u + row;
+        if (at_row < n_rows) {
+            float most = state[0][row].x, w[kCacheWaves], total = 0.0f;
+#pragma unroll
+            for (int i = 1; i < (int)kCacheWaves; ++i) most = fmaxf(most, state[i][row].x);
+            const float base = most == -__builtin_inff() ? 0.0f : most;
+#pragma unroll
+            for (int i = 0; i < (int)kCacheWaves; ++i) {
+                w[i] = __builtin_amdgcn_exp2f((state[i][row].x - base) * factor);
+                total = fmaf(state[i][row].y, w[i], total);
+            }
+            const uint32_t at = tile * kRows + at_row, token = at / group, head = hk * group + (at - token * group);
+            const float inverse = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;   // (a NaN stays; no key: zeros)
+            for (uint32_t c = 4u * (threadIdx.x & 15u); c < dim; c += 64u) {
+                cache_f32x4 x = *reinterpret_cast<const cache_f32x4*>(&meet[0][row][c]) * w[0];
+#pragma unroll
+                for (int i = 1; i < (int)kCacheWaves; ++i) {
+                    const cache_f32x4 y = *reinterpret_cast<const cache_f32x4*>(&meet[i][row][c]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[j] = fmaf(y[j], w[i], x[j]);
+                }
+                if (kSplit) {
+                    *reinterpret_cast<cache_f32x4*>(reinterpret_cast<float*>(out) + ((size_t)blockIdx.x * kRows + at_row) * dim + c) = x;
+                } else {
+                    const cache_bf16x2 lo = __builtin_convertvector((cache_f32x2{x[0] * inverse, x[1] * inverse}), cache_bf16x2);
+                    const cache_bf16x2 hi = __builtin_convertvector((cache_f32x2{x[2] * inverse, x[3] * inverse}), cache_bf16x2);
+                    uint16_t* place = out + ((size_t)head * so.head + (size_t)(rows.first + token) * so.token) * 8u + c;
+                    *reinterpret_cast<uint2*>(place) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+                }
+            }
+            if ((threadIdx.x & 15u) == 0) {
+                if (kSplit) reinterpret_cast<float2*>(lse)[(size_t)blockIdx.x * kRows + at_row] = make_float2(most, total);
+                else if (lse) lse[(size_t)(rows.first + token) * s.heads + head] = total == 0.0f ? -__builtin_inff() : fmaf(base, s.scale, kCacheLn2 * __builtin_amdgcn_logf(total));
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// The parts of a row meet.  kWaves wavefronts to a row: four where rows are few and parts many.  Half a wavefront takes a part, four channels a
+// lane.
+template <int kWaves>
+__global__ __launch_bounds__(256) void cache_join_kernel(const float* workspace, const float2* states, const int32_t* lens, const int32_t* starts, uint16_t* out,
+                                                         float* lse, uint32_t n_positions, CacheStrides so, CacheShape s)
+{
+    __shared__ cache_f32x4 meet[4][32];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    auto scalar = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
+    const uint32_t group = scalar((uint32_t)s.heads / s.heads_k), tile_rows = 16u * s.rows16, dim = s.dim8 * 8u;
+    const uint32_t row = kWaves == 4 ? blockIdx.x : blockIdx.x * 4u + wave;
+    const uint32_t token = scalar(row / s.heads), head = row - token * s.heads, hk = scalar(head / group);
+    const uint32_t b = scalar(sequence_of(starts, token, 0u, 1u, s));
+    const CacheRows rows = rows_of(starts, lens, b, s);
+    if (token < rows.first || token - rows.first >= rows.n) return;   // (a whole workgroup, or a wavefront by itself)
+    const uint32_t share = scalar(share_of(starts, lens, group, tile_rows, s));
+    uint32_t base = 0;
+    walk_parts(starts, lens, group, tile_rows, share, b, base, s);
+    const uint32_t at = (token - rows.first) * group + (head - hk * group), tile = at / tile_rows, parts = parts_of(rows.len, share);
+    const uint32_t first = (scalar(base) + tile * parts) * s.heads_k + hk;   // of the parts' positions
+    const uint32_t n = min(parts, first < n_positions ? (n_positions - first + s.heads_k - 1u) / s.heads_k : 0u);
+    const size_t step = (size_t)s.heads_k * tile_rows, from = (size_t)first * tile_rows + (at - tile * tile_rows);
+    const float factor = s.scale * kCacheLog2E;
+    float most = -__builtin_inff(), sum = 0.0f;
+    for (uint32_t p = lane; p < n; p += 64u) most = fmaxf(most, states[from + p * step].x);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+    const float reference = most == -__builtin_inff() ? 0.0f : most;
+    for (uint32_t p = lane; p < n; p += 64u) {
+        const float2 st = states[from + p * step];
+        sum = fmaf(st.y, __builtin_amdgcn_exp2f((st.x - reference) * factor), sum);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    const uint32_t c = 4u * (lane & 31u);
+    cache_f32x4 o = {0, 0, 0, 0};
+    if (c < dim) {
+#pragma unroll 4
+        for (uint32_t p = (kWaves == 4 ? 2u * wave : 0u) + (lane >> 5); p < n; p += 2u * kWaves) {
+            const float w = __builtin_amdgcn_exp2f((states[from + p * step].x - reference) * factor);
+            const cache_f32x4 x = *reinterpret_cast<const cache_f32x4*>(workspace + (from + p * step) * dim + c);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = fmaf(x[j], w, o[j]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] += __shfl_xor(o[j], 32);
+    if (kWaves == 4) {
+        if (lane < 32u) meet[wave][lane] = o;
+        __syncthreads();
+        if (wave > 0 || lane >= 32u) return;
+        for (int i = 1; i < 4; ++i) o += meet[i][lane];
+    }
+    if (lane >= 32u) return;
+    const float inverse = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
+    if (c < dim) {
+        const cache_bf16x2 lo = __builtin_convertvector((cache_f32x2{o[0] * inverse, o[1] * inverse}), cache_bf16x2);
+        const cache_bf16x2 hi = __builtin_convertvector((cache_f32x2{o[2] * inverse, o[3] * inverse}), cache_bf16x2);
+        uint16_t* place = out + ((size_t)head * so.head + (size_t)token * so.token) * 8u + c;
+        *reinterpret_cast<uint2*>(place) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+    }
+    if (lse && lane == 0) lse[(size_t)token * s.heads + head] = sum == 0.0f ? -__builtin_inff() : fmaf(reference, s.scale, kCacheLn2 * __builtin_amdgcn_logf(sum));
+}
+
+#undef FB4_INLINE
+
+}  // namespace fb4
