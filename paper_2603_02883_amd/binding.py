@@ -423,10 +423,11 @@ def _load_call():
     loader = importlib.machinery.ExtensionFileLoader(name, _build.CALL)
     module = importlib.util.module_from_spec(importlib.util.spec_from_file_location(name, _build.CALL, loader=loader))
     loader.exec_module(module)
-    if not hasattr(module, "block_attention"):   # built from an earlier source, without all of the calls
+    if not hasattr(module, "cache_attention"):   # built from an earlier source, without all of the calls
         return CtypesCall
     module.bind(fb4_opts, ctypes.c_void_p, CtypesCall)
     module.bind_heads(HeadsCall)
+    module.bind_serving(ServingCall)
     # (a torch without the protocol has its tensors read by their methods)
     module.read_through(torch.Tensor, getattr(torch.Tensor, "__dlpack_c_exchange_api__", None))
     return module
@@ -434,7 +435,7 @@ def _load_call():
 
 _call = _load_call()
 _heads_call = HeadsCall if _call is CtypesCall else _call
-_serving_call = ServingCall
+_serving_call = ServingCall if _call is CtypesCall else _call
 
 
 def _stream(stream):

@@ -198,8 +198,11 @@ static const char* const call_names[kCalls] = {"quantize", "quantize_seda", "qua
                                                "layernorm_quantize", "gelu_quantize", "attention_scores",
                                                "select_salient_tokens", "seda_assign", "seda_main_anchor", "seda_profile"};
 // ... and the attention path's (bind_heads).
-enum { k_qk_norm_rope = kCalls, k_select_key_blocks, k_block_attention, kAll };
-static const char* const heads_names[kAll - kCalls] = {"qk_norm_rope", "select_key_blocks", "block_attention"};
+enum { k_qk_norm_rope = kCalls, k_select_key_blocks, k_block_attention, kHeads };
+static const char* const heads_names[kHeads - kCalls] = {"qk_norm_rope", "select_key_blocks", "block_attention"};
+// ... and those that serve a few tokens at a time (bind_serving).
+enum { k_matvec = kHeads, k_cache_plan, k_cache_store, k_cache_attention, kAll };
+static const char* const serving_names[kAll - kHeads] = {"matvec", "cache_plan", "cache_store", "cache_attention"};
 static PyObject* through_ctypes[kAll];
 
 static PyObject* elsewhere(int call, PyObject* const* a, Py_ssize_t n)
@@ -560,6 +563,102 @@ static PyObject* py_block_attention(ARGS)
                                     top, (int)bq, (int)bk, scale, o.data, so, lse, ws, size, s));
 }
 
+// Serving a few tokens at a time, checked likewise.
+extern __typeof__(fb4_matvec) fb4_matvec __attribute__((weak));
+extern __typeof__(fb4_cache_plan) fb4_cache_plan __attribute__((weak));
+extern __typeof__(fb4_cache_store) fb4_cache_store __attribute__((weak));
+extern __typeof__(fb4_cache_attention) fb4_cache_attention __attribute__((weak));
+extern __typeof__(fb4_cache_attention_workspace) fb4_cache_attention_workspace __attribute__((weak));
+
+// (luts, x, codes, meta, block, bias, out, device, stream)
+static PyObject* py_matvec(ARGS)
+{
+    view x, c, o;
+    void *h, *meta, *bias, *s;
+    int64_t device, block;
+    int f32 = 0;
+    if (!fb4_matvec || n != 9 || integer(a[7], &device) || address(a[0], &h) || address(a[8], &s) || whole(a[4], &block) || (block != 16 && block != 32) ||
+        viewed(a[1], 2, kBfloat, 16, device, &x) || viewed(a[2], 2, kUint, 8, device, &c) || !packed(&c, 2) || x.size[1] != 2 * c.size[1] ||
+        (x.size[1] > 1 && x.stride[1] != 1) || dense(a[3], 0, 2, kInt, 16, device, c.size[0], x.size[1] / block, 0, 0, &meta) ||
+        dense(a[5], 1, 1, kFloat, 32, device, c.size[0], 0, 0, 0, &bias))
+        return elsewhere(k_matvec, a, n);
+    if (viewed(a[6], 2, kBfloat, 16, device, &o)) {
+        f32 = 1;
+        if (viewed(a[6], 2, kFloat, 32, device, &o)) return elsewhere(k_matvec, a, n);
+    }
+    if (!sizes_are(&o, 2, x.size[0], c.size[0], 0, 0) || (o.size[1] > 1 && o.stride[1] != 1)) return elsewhere(k_matvec, a, n);
+    RETURN_CALL(fb4_matvec(h, x.data, x.size[0], x.size[0] > 1 ? x.stride[0] : x.size[1], c.data, meta, c.size[0], x.size[1], (int)block, bias, o.data,
+                           f32 ? FB4_DTYPE_F32 : FB4_DTYPE_BF16, o.size[0] > 1 ? o.stride[0] : o.size[1], s));
+}
+
+// (lens, adds, tables, free_pages, free_count, page, lens_out, free_count_out, starts, slots, positions, device, stream)
+static PyObject* py_cache_plan(ARGS)
+{
+    view t, f, sl;
+    void *lens, *adds, *count, *lens_out, *count_out, *starts, *positions, *s;
+    int64_t device, page;
+    if (!fb4_cache_plan || n != 13 || integer(a[11], &device) || address(a[12], &s) || whole(a[5], &page) || page < 1 || page > INT32_MAX ||
+        viewed(a[2], 2, kInt, 32, device, &t) || !packed(&t, 2) || viewed(a[3], 1, kInt, 32, device, &f) || !packed(&f, 1) ||
+        viewed(a[9], 1, kInt, 32, device, &sl) || !packed(&sl, 1) || dense(a[0], 0, 1, kInt, 32, device, t.size[0], 0, 0, 0, &lens) ||
+        dense(a[1], 0, 1, kInt, 32, device, t.size[0], 0, 0, 0, &adds) || dense(a[4], 0, 1, kInt, 32, device, 1, 0, 0, 0, &count) ||
+        dense(a[6], 0, 1, kInt, 32, device, t.size[0], 0, 0, 0, &lens_out) || dense(a[7], 0, 1, kInt, 32, device, 1, 0, 0, 0, &count_out) ||
+        dense(a[8], 0, 1, kInt, 32, device, t.size[0] + 1, 0, 0, 0, &starts) || dense(a[10], 1, 1, kInt, 32, device, sl.size[0], 0, 0, 0, &positions))
+        return elsewhere(k_cache_plan, a, n);
+    RETURN_CALL(fb4_cache_plan(lens, adds, t.size[0], (int)page, t.data, t.size[1], f.data, f.size[0], count, lens_out, count_out, starts, sl.data, positions,
+                               sl.size[0], s));
+}
+
+// [heads][tokens][dim] with contiguous channels
+static int head_rows(PyObject* t, int64_t device, view* v)
+{
+    return viewed(t, 3, kBfloat, 16, device, v) || (v->size[2] > 1 && v->stride[2] != 1) ? -1 : 0;
+}
+
+// A cache's pages for these heads and channels, with its scales.
+static int cache_of(PyObject* oc, PyObject* os, PyObject* opage, int64_t device, int64_t dim, int64_t* page, view* scales, void** cache)
+{
+    if (whole(opage, page) || *page < 1 || *page > 128 || dim > INT32_MAX || viewed(os, 3, kUint, 8, device, scales) || scales->size[0] != 2 || !packed(scales, 3))
+        return -1;
+    return dense(oc, 0, 4, kUint, 8, device, 2, scales->size[1], scales->size[2], *page * dim, cache);
+}
+
+// (k, v, slots, cache, scales, page, device, stream)
+static PyObject* py_cache_store(ARGS)
+{
+    view k, v, sc;
+    void *slots, *cache, *s;
+    int64_t device, page;
+    if (!fb4_cache_store || n != 8 || integer(a[6], &device) || address(a[7], &s) || head_rows(a[0], device, &k) || head_rows(a[1], device, &v) ||
+        !sizes_are(&v, 3, k.size[0], k.size[1], k.size[2], 0) || dense(a[2], 0, 1, kInt, 32, device, k.size[1], 0, 0, 0, &slots) ||
+        cache_of(a[3], a[4], a[5], device, k.size[2], &page, &sc, &cache) || sc.size[2] != k.size[0] || k.size[0] > INT32_MAX)
+        return elsewhere(k_cache_store, a, n);
+    RETURN_CALL(fb4_cache_store(k.data, k.stride, v.data, v.stride, k.size[1], (int)k.size[0], k.size[2], slots, cache, sc.data, sc.size[1], (int)page, s));
+}
+
+// (q, cache, scales, tables, lens, starts, page, scale, causal, out, lse, workspace, device, stream)
+static PyObject* py_cache_attention(ARGS)
+{
+    view q, sc, t, o;
+    void *cache, *lens, *starts, *lse, *ws, *s;
+    size_t size;
+    int64_t device, page;
+    if (!fb4_cache_attention || !fb4_cache_attention_workspace || n != 14 || integer(a[12], &device) || address(a[13], &s) || !PyFloat_Check(a[7]) || !PyBool_Check(a[8]) ||
+        head_rows(a[0], device, &q) || cache_of(a[1], a[2], a[6], device, q.size[2], &page, &sc, &cache) || viewed(a[3], 2, kInt, 32, device, &t) || !packed(&t, 2) ||
+        dense(a[4], 0, 1, kInt, 32, device, t.size[0], 0, 0, 0, &lens) || dense(a[5], 0, 1, kInt, 32, device, t.size[0] + 1, 0, 0, 0, &starts) ||
+        head_rows(a[9], device, &o) || !sizes_are(&o, 3, q.size[1], q.size[0], q.size[2], 0) || dense(a[10], 1, 2, kFloat, 32, device, q.size[1], q.size[0], 0, 0, &lse) ||
+        q.size[0] > INT32_MAX || sc.size[2] > INT32_MAX)
+        return elsewhere(k_cache_attention, a, n);
+    const size_t needed = fb4_cache_attention_workspace(q.size[1], (int)q.size[0], (int)sc.size[2], q.size[2], (int)page, t.size[1], t.size[0]);
+    const int rc_ws = workspace_of(a[11], device, needed, &ws, &size);
+    if (rc_ws < 0) return elsewhere(k_cache_attention, a, n);
+    if (rc_ws > 0) return PyLong_FromSize_t(needed);
+    const float scale = (float)PyFloat_AS_DOUBLE(a[7]);
+    const int causal = a[8] == Py_True;
+    const int64_t so[2] = {o.stride[1], o.stride[0]};   // (out is [tokens][heads][dim])
+    RETURN_CALL(fb4_cache_attention(q.data, q.stride, q.size[1], (int)q.size[0], (int)sc.size[2], q.size[2], cache, sc.data, sc.size[1], (int)page, t.data, t.size[1],
+                                    lens, starts, t.size[0], causal, scale, o.data, so, lse, ws, size, s));
+}
+
 // The named attributes of `from` into `to`, all or (-1) none.
 static int take_calls(PyObject* from, const char* const* names, int n, PyObject** to)
 {
@@ -582,7 +681,18 @@ static PyObject* py_bind_heads(ARGS)
         PyErr_SetString(PyExc_TypeError, "bind_heads(calls through ctypes)");
         return NULL;
     }
-    if (take_calls(a[0], heads_names, kAll - kCalls, through_ctypes + kCalls)) return NULL;
+    if (take_calls(a[0], heads_names, kHeads - kCalls, through_ctypes + kCalls)) return NULL;
+    Py_RETURN_NONE;
+}
+
+// (object with the serving calls through ctypes)
+static PyObject* py_bind_serving(ARGS)
+{
+    if (n != 1) {
+        PyErr_SetString(PyExc_TypeError, "bind_serving(calls through ctypes)");
+        return NULL;
+    }
+    if (take_calls(a[0], serving_names, kAll - kHeads, through_ctypes + kHeads)) return NULL;
     Py_RETURN_NONE;
 }
 
@@ -619,7 +729,8 @@ static PyObject* py_read_through(ARGS)
 static PyMethodDef methods[] = {METHOD(quantize), METHOD(quantize_seda), METHOD(quantize_decompose), METHOD(dequantize), METHOD(repack_mxfp8),
                                 METHOD(layernorm_quantize), METHOD(gelu_quantize), METHOD(attention_scores), METHOD(select_salient_tokens),
                                 METHOD(seda_assign), METHOD(seda_main_anchor), METHOD(seda_profile), METHOD(qk_norm_rope),
-                                METHOD(select_key_blocks), METHOD(block_attention), METHOD(bind), METHOD(bind_heads),
+                                METHOD(select_key_blocks), METHOD(block_attention), METHOD(matvec), METHOD(cache_plan),
+                                METHOD(cache_store), METHOD(cache_attention), METHOD(bind), METHOD(bind_heads), METHOD(bind_serving),
                                 METHOD(read_through), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fb4call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 

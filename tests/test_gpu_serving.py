@@ -703,3 +703,41 @@ def test_given_workspaces(F):
         with pytest.raises(F.Fb4Error) as e:
             F.fb4_cache_attention(q, c.cache, c.scales, c.tables, c.lens, ints([0, 3]), 64, workspace=bad)
         assert e.value.code == code
+
+
+def test_both_bindings_answer_alike(F, luts, monkeypatch):
+    B = F.binding
+    if B._call is B.CtypesCall:
+        pytest.skip("no C module for this interpreter")
+    monkeypatch.setattr(B, "_serving_call", B.ServingCall)
+    ctypes_outs, ctypes_state = run_steps(F, luts, 4)
+    ws_outs = ctypes_state.step(randn(gen(1), 1, ctypes_state.width).bfloat16(), ints([1, 0, 0, 0, 0]))[0]
+    asked = []
+
+    class Noted:
+        def __getattr__(self, name):
+            def call(*a):
+                asked.append(name)
+                raise AssertionError("handed over: " + name)
+            return call
+    monkeypatch.setattr(B, "_serving_call", B._call)
+    B._call.bind_serving(type("Elsewhere", (), {n: staticmethod(getattr(Noted(), n)) for n in ("matvec", "cache_plan", "cache_store", "cache_attention")}))
+    try:
+        outs, state = run_steps(F, luts, 4)
+        rows = state.step(randn(gen(1), 1, state.width).bfloat16(), ints([1, 0, 0, 0, 0]))[0]
+    finally:
+        B._call.bind_serving(B.ServingCall)
+    assert not asked and all(torch.equal(a, b) for a, b in zip(outs, ctypes_outs)) and torch.equal(rows, ws_outs)
+    assert torch.equal(state.cache, ctypes_state.cache)
+    # what the module does not take is refused by the same rules
+    x = randn(gen(1), 2, state.width).bfloat16()
+    for bad in (lambda: F.fb4_matvec(luts, x.float(), *state.qkv), lambda: F.fb4_matvec(luts, x.cpu(), *state.qkv), lambda: F.fb4_matvec(luts, x, *state.qkv, block=16),
+                lambda: F.fb4_matvec(luts, x[:, ::2], *state.qkv), lambda: F.fb4_matvec(luts, x, *state.qkv, block=2 ** 32 + 32),
+                lambda: F.fb4_cache_plan(state.lens, state.lens[:2], state.tables, state.free, state.count, 16, 4),
+                lambda: F.fb4_cache_plan(state.lens, state.lens, state.tables, state.free, state.count, 2 ** 32 + 16, 4),
+                lambda: F.fb4_cache_plan(state.lens, state.lens, state.tables.t(), state.free, state.count, 16, 4),
+                lambda: F.fb4_cache_plan(state.lens, state.lens, state.tables, state.free, state.count, 24, 4),
+                lambda: F.fb4_cache_store(x.view(2, -1, 64), x.view(2, -1, 64), state.lens, state.cache, state.scales, 16),
+                lambda: F.fb4_cache_attention(x.view(2, -1, 64), state.cache, state.scales, state.tables, state.lens, state.lens, 16)):
+        with pytest.raises(F.Fb4Error):
+            bad()
