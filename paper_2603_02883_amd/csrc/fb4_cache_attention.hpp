@@ -127,6 +127,99 @@ __device__ __forceinline__ uint32_t walk_parts(const int32_t* starts, const int3
     return s.batch;
 }
 
+// ------------------------------------------------------------------------------------------------ a step's weights, and bytes
+// Weights of four tiles of products (16 keys of this lane's query) as the second product's operands; the reference moves, and what is relative
+// to it, when a weight would pass 2^8.
+template <int kD16>
+__device__ __forceinline__ void cache_weights(const cache_f32x4 (&sc)[4], float& reference, float& sum, cache_f32x4 (&o)[kD16], cache_bf16x8 (&p)[2], float factor)
+{
+    float larger = -__builtin_inff();
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) larger = fmaxf(larger, sc[t][i]);
+    }
+    if (__any((larger - reference) * factor > 8.0f)) {
+        // (finite, so that a score of +Inf has an infinite weight and sum: no number in the output, +Inf in lse)
+        larger = fmaxf(larger, reference);
+        larger = fmaxf(larger, __shfl_xor(larger, 16));
+        larger = fminf(fmaxf(larger, __shfl_xor(larger, 32)), 0x1.fffffep127f);
+        const float shrink = reference == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((reference - larger) * factor);
+        reference = larger;
+        sum *= shrink;
+#pragma unroll
+        for (int d = 0; d < kD16; ++d) o[d] *= shrink;
+    }
+    const float base = reference == -__builtin_inff() ? 0.0f : reference;
+    float w[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w[i] = __builtin_amdgcn_exp2f((sc[i / 4][i % 4] - base) * factor);
+    // (the sum from the unrounded weights, pairwise: one rounding of the row's a step)
+    sum += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7])) + (((w[8] + w[9]) + (w[10] + w[11])) + ((w[12] + w[13]) + (w[14] + w[15])));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            y[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((cache_f32x2{w[8 * h + 2 * i], w[8 * h + 2 * i + 1]}), cache_bf16x2));
+        p[h] = __builtin_bit_cast(cache_bf16x8, make_uint4(y[0], y[1], y[2], y[3]));
+    }
+}
+
+// Eight E4M3 bytes times a power of two, in bf16.
+__device__ __forceinline__ cache_bf16x8 cache_decode(uint32_t lo, uint32_t hi, float f)
+{
+    const cache_bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, f, true);
+    const cache_bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, f, true);
+    return cache_bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// The first n of 16 bytes, zeros behind.
+__device__ __forceinline__ uint4 first_bytes(uint4 w, uint32_t n)
+{
+    auto mask = [&](uint32_t i) { return n >= 4u * i + 4u ? 0xFFFFFFFFu : n <= 4u * i ? 0u : (1u << (8u * (n - 4u * i))) - 1u; };
+    return make_uint4(w.x & mask(0), w.y & mask(1), w.z & mask(2), w.w & mask(3));
+}
+// Bytes that are NaN, as 1 each (0x7F is E4M3's NaN; one more carries into the sign and no further).
+__device__ __forceinline__ uint4 nans_of(uint4 w)
+{
+    auto some = [](uint32_t x) { return (((x & 0x7F7F7F7Fu) + 0x01010101u) >> 7) & 0x01010101u; };
+    return make_uint4(some(w.x), some(w.y), some(w.z), some(w.w));
+}
+__device__ __forceinline__ uint4 without(uint4 w, uint4 nans) { return make_uint4(w.x & ~(nans.x * 0xFFu), w.y & ~(nans.y * 0xFFu), w.z & ~(nans.z * 0xFFu), w.w & ~(nans.w * 0xFFu)); }
+// Eight keys from `key` on as an operand: 1 for those before `limit`.
+__device__ __forceinline__ cache_bf16x8 seen_keys(uint32_t key, uint32_t limit)
+{
+    uint32_t y[4];
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) y[i] = (key + 2u * i < limit ? 0x3F80u : 0u) | (key + 2u * i + 1u < limit ? 0x3F800000u : 0u);
+    return __builtin_bit_cast(cache_bf16x8, make_uint4(y[0], y[1], y[2], y[3]));
+}
+// What lies behind a query's last key has weight 0, but 0 times NaN is none.  So the keys that some query does not see come into the products without
+// NaN; where there was one, a walk over these keys at the end, with products of ones, says which accumulators it belongs to.
+template <int kD16, int kSets, typename Pieces>
+__device__ __forceinline__ void mark_nans(cache_f32x4 (&o)[kSets][kD16], Pieces pieces, uint32_t key, const uint32_t (&limit)[kSets])
+{
+#pragma unroll
+    for (int d = 0; d < kD16; ++d) {
+        const uint4 n = pieces(d);
+        const cache_bf16x8 a0 = cache_decode(n.x * 0x38u, n.y * 0x38u, 1.0f), a1 = cache_decode(n.z * 0x38u, n.w * 0x38u, 1.0f);   // (0x38: 1)
+#pragma unroll
+        for (int u = 0; u < kSets; ++u) {
+            cache_f32x4 x = {0, 0, 0, 0};
+            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, seen_keys(key, limit[u]), x, 0, 0, 0);
+            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, seen_keys(key + 8u, limit[u]), x, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[u][d][i] = x[i] > 0.0f ? __builtin_nanf("") : o[u][d][i];
+        }
+    }
+}
+__device__ __forceinline__ uint2 rounded(cache_f32x4 x, float f)
+{
+    const cache_bf16x2 lo = __builtin_convertvector((cache_f32x2{x[0] * f, x[1] * f}), cache_bf16x2), hi = __builtin_convertvector((cache_f32x2{x[2] * f, x[3] * f}), cache_bf16x2);
+    return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+}
+
 // ------------------------------------------------------------------------------------------------ attention
 // kD32: channels / 32, rounded up; kWhole: a row is kD32 whole steps and 16-byte pieces.  kSplit: parts, into the workspace: floats
 // [position][16 kSets][dim], then {maximum, sum} of every row; position = (parts in front) * heads_k + key head.
@@ -238,11 +331,6 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
             if (p >= 0 && (kWhole || 16u * d + r < dim)) vr[d] = *reinterpret_cast<const uint4*>(base + ((size_t)(16u * d) << bits));
         }
     };
-    auto decode = [&](uint32_t lo, uint32_t hi, float f) FB4_INLINE {
-        const cache_bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, f, false), b2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, f, true);
-        const cache_bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, f, true);
-        return cache_bf16x8{a[0], a[1], b2[0], b2[1], c[0], c[1], d[0], d[1]};
-    };
 
     const float factor = s.scale * kCacheLog2E;
     cache_f32x4 o[kSets][2 * kD32];
@@ -254,7 +342,7 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
 #pragma unroll
         for (int d = 0; d < 2 * kD32; ++d) o[u][d] = cache_f32x4{0, 0, 0, 0};
     }
-    uint32_t step = from + wave;
+    uint32_t step = from + wave, nans = 0;
     Where here = {-1, -1}, next = {-1, -1};
     if (step < to) {
         here = find(step);
@@ -272,7 +360,7 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
             for (int u = 0; u < kSets; ++u) sc[u][t] = cache_f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int i = 0; i < kD32; ++i) {
-                const cache_bf16x8 a = i % 2 ? decode(kr[t][i / 2].z, kr[t][i / 2].w, k_scale) : decode(kr[t][i / 2].x, kr[t][i / 2].y, k_scale);
+                const cache_bf16x8 a = i % 2 ? cache_decode(kr[t][i / 2].z, kr[t][i / 2].w, k_scale) : cache_decode(kr[t][i / 2].x, kr[t][i / 2].y, k_scale);
 #pragma unroll
                 for (int u = 0; u < kSets; ++u) sc[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[u][i], sc[u][t], 0, 0, 0);
             }
@@ -298,83 +386,37 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
         // ---- weights
         cache_bf16x8 p[kSets][2];
 #pragma unroll
-        for (int u = 0; u < kSets; ++u) {
-            float larger = -__builtin_inff();
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) larger = fmaxf(larger, sc[u][t][i]);
-            }
-            if (__any((larger - reference[u]) * factor > 8.0f)) {
-                // (finite, so that a score of +Inf has an infinite weight and sum: no number in the output, +Inf in lse)
-                larger = fmaxf(larger, reference[u]);
-                larger = fmaxf(larger, __shfl_xor(larger, 16));
-                larger = fminf(fmaxf(larger, __shfl_xor(larger, 32)), 0x1.fffffep127f);
-                const float shrink = reference[u] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((reference[u] - larger) * factor);
-                reference[u] = larger;
-                sum[u] *= shrink;
-#pragma unroll
-                for (int d = 0; d < 2 * kD32; ++d) o[u][d] *= shrink;
-            }
-            const float base = reference[u] == -__builtin_inff() ? 0.0f : reference[u];
-            float w[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) w[i] = __builtin_amdgcn_exp2f((sc[u][i / 4][i % 4] - base) * factor);
-            // (the sum from the unrounded weights, pairwise: one rounding of the row's a step)
-            sum[u] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7])) + (((w[8] + w[9]) + (w[10] + w[11])) + ((w[12] + w[13]) + (w[14] + w[15])));
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t y[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    y[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((cache_f32x2{w[8 * h + 2 * i], w[8 * h + 2 * i + 1]}), cache_bf16x2));
-                p[u][h] = __builtin_bit_cast(cache_bf16x8, make_uint4(y[0], y[1], y[2], y[3]));
-            }
-        }
-        // ---- O^T.  What lies behind a query's last key has weight 0, but 0 times NaN is none: behind the sequence's end (where a page may
-        // hold anything) the values become zeros; a NaN in sight of some of the queries only takes the products query by query.
-        bool bad = false;
-        if (cut) {
-            auto ahead = [](uint32_t n, int w) FB4_INLINE { return n >= 4u * w + 4u ? 0xFFFFFFFFu : n <= 4u * w ? 0u : (1u << (8u * (n - 4u * w))) - 1u; };
-            const uint32_t n = rows.len > key ? min(rows.len - key, 16u) : 0u;
+        for (int u = 0; u < kSets; ++u) cache_weights(sc[u], reference[u], sum[u], o[u], p[u], factor);
+        // ---- O^T
+        if (step * kCacheStep + kCacheStep > least) {
+            const uint32_t n = rows.len > key ? min(rows.len - key, 16u) : 0u;   // (behind a sequence's end a page may hold anything)
 #pragma unroll
             for (int d = 0; d < 2 * kD32; ++d) {
-                vr[d] = make_uint4(vr[d].x & ahead(n, 0), vr[d].y & ahead(n, 1), vr[d].z & ahead(n, 2), vr[d].w & ahead(n, 3));
-                const uint32_t w[4] = {vr[d].x, vr[d].y, vr[d].z, vr[d].w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) bad = bad || (((w[i] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u);   // (0x7F, no sum carries over)
-            }
-            bad = __any(bad);
-            if (bad) {
-#pragma unroll 1
-                for (uint32_t c = 0; c < 16; ++c) {
-#pragma unroll
-                    for (int u = 0; u < kSets; ++u) {
-                        const uint32_t sees = __shfl(limit[u], c), m = sees > key ? min(sees - key, 16u) : 0u;
-#pragma unroll
-                        for (int d = 0; d < 2 * kD32; ++d) {
-                            cache_f32x4 x = {0, 0, 0, 0};
-                            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode(vr[d].x & ahead(m, 0), vr[d].y & ahead(m, 1), v_scale), p[u][0], x, 0, 0, 0);
-                            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode(vr[d].z & ahead(m, 2), vr[d].w & ahead(m, 3), v_scale), p[u][1], x, 0, 0, 0);
-                            if (r == c) o[u][d] += x;
-                        }
-                    }
-                }
+                vr[d] = first_bytes(vr[d], n);
+                const uint4 bad = nans_of(vr[d]);
+                nans |= bad.x | bad.y | bad.z | bad.w;
+                vr[d] = without(vr[d], bad);
             }
         }
-        if (!bad) {
 #pragma unroll
-            for (int d = 0; d < 2 * kD32; ++d) {
-                const cache_bf16x8 a0 = decode(vr[d].x, vr[d].y, v_scale), a1 = decode(vr[d].z, vr[d].w, v_scale);
+        for (int d = 0; d < 2 * kD32; ++d) {
+            const cache_bf16x8 a0 = cache_decode(vr[d].x, vr[d].y, v_scale), a1 = cache_decode(vr[d].z, vr[d].w, v_scale);
 #pragma unroll
-                for (int u = 0; u < kSets; ++u) {
-                    o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, p[u][0], o[u][d], 0, 0, 0);
-                    o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, p[u][1], o[u][d], 0, 0, 0);
-                }
+            for (int u = 0; u < kSets; ++u) {
+                o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, p[u][0], o[u][d], 0, 0, 0);
+                o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, p[u][1], o[u][d], 0, 0, 0);
             }
         }
         here = after;
         if (more) fetch_v(step + kCacheWaves, here.v);
+    }
+    if (__any(nans != 0u)) {
+        const uint32_t first = max(from, least / kCacheStep);
+        for (step = first + (wave + kCacheWaves - (first - from) % kCacheWaves) % kCacheWaves; step < to; step += kCacheWaves) {
+            const uint32_t key = step * kCacheStep + 16u * g, n = rows.len > key ? min(rows.len - key, 16u) : 0u;
+            fetch_v(step, page_of(key));
+            mark_nans(o, [&](int d) FB4_INLINE { return nans_of(first_bytes(vr[d], n)); }, key, limit);
+        }
     }
     // ---- the wavefronts meet
 #pragma unroll
@@ -409,10 +451,8 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
                 if (kSplit) {
                     *reinterpret_cast<cache_f32x4*>(reinterpret_cast<float*>(out) + ((size_t)blockIdx.x * kRows + at_row) * dim + c) = x;
                 } else {
-                    const cache_bf16x2 lo = __builtin_convertvector((cache_f32x2{x[0] * inverse, x[1] * inverse}), cache_bf16x2);
-                    const cache_bf16x2 hi = __builtin_convertvector((cache_f32x2{x[2] * inverse, x[3] * inverse}), cache_bf16x2);
                     uint16_t* place = out + ((size_t)head * so.head + (size_t)(rows.first + token) * so.token) * 8u + c;
-                    *reinterpret_cast<uint2*>(place) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+                    *reinterpret_cast<uint2*>(place) = rounded(x, inverse);
                 }
             }
             if ((threadIdx.x & 15u) == 0) {
@@ -421,6 +461,262 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
             }
         }
         __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ attention of many queries
+// As above, for 128 rows to a workgroup, 32 to a wavefront.  A step's keys and values come into LDS once for all four, decoded: wavefront w asks
+// for the w-th sixteenth of each two steps ahead and puts it down as bf16 one step ahead, so that the converter's half rate (7 cycles for two
+// elements) is paid once for 128 rows.  Rows of keys lie by tile and operand row, 16 bytes further apart than they are long, channels of
+// values likewise: the 16 rows that a read takes start in different banks.
+constexpr uint32_t kTileRows = 128;
+template <int kD32, bool kWhole, bool kSplit>
+__global__ __launch_bounds__(64 * kCacheWaves) __attribute__((amdgpu_waves_per_eu(2)))
+void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* scales, const int32_t* tables, const int32_t* lens, const int32_t* starts, uint16_t* out,
+                        float* lse, CacheStrides sq, CacheStrides so, CacheShape s)
+{
+    constexpr int kSets = 2;
+    constexpr uint32_t kPitchK = 64 * kD32 + 16, kPitchV = 2 * kCacheStep + 16;
+    constexpr uint32_t kKeys = kCacheStep * kPitchK, kBuffer = kKeys + 32 * kD32 * kPitchV;
+    constexpr int kAsksK = kD32, kAsksV = (kD32 + 1) / 2;   // of 64 lanes: 8 bytes of a key each, 16 of a channel
+    __shared__ __align__(16) uint8_t lds[2 * kBuffer];
+    __shared__ uint32_t notes[2][4];                        // of a buffer's sixteenths: kNone, kNan
+    constexpr uint32_t kNone = 1, kNan = 2;
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t r = lane & 15u, g = lane >> 4;
+    auto scalar = [](uint32_t x) FB4_INLINE { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
+    const uint32_t position = scalar(blockIdx.x / s.heads_k), hk = blockIdx.x - position * s.heads_k, group = scalar((uint32_t)s.heads / s.heads_k);
+    uint32_t b, tile, from = 0, to;
+    CacheRows rows;
+    if (kSplit) {
+        const uint32_t share = scalar(share_of(starts, lens, group, kTileRows, s));
+        uint32_t at = position;
+        b = scalar(walk_parts(starts, lens, group, kTileRows, share, 0xFFFFFFFFu, at, s));
+        if (b >= s.batch) return;
+        rows = rows_of(starts, lens, b, s);
+        const uint32_t parts = parts_of(rows.len, share);
+        tile = scalar(at) / parts;
+        const uint32_t part = scalar(at) - tile * parts, steps = steps_of(rows.len);
+        from = (uint32_t)((uint64_t)steps * part / parts);
+        to = (uint32_t)((uint64_t)steps * (part + 1u) / parts);
+    } else {
+        b = scalar(sequence_of(starts, position, group, kTileRows, s));
+        rows = rows_of(starts, lens, b, s);
+        tile = position - place_of(rows.first, b, group, kTileRows);
+        if (tile >= tiles_of(rows.n, group, kTileRows)) return;
+        to = steps_of(rows.len);
+    }
+    rows.first = scalar(rows.first), rows.n = scalar(rows.n), rows.len = scalar(rows.len), tile = scalar(tile), from = scalar(from), to = scalar(to);
+    const uint32_t n_rows = min(rows.n * group - tile * kTileRows, kTileRows), first_row = wave * 32u;
+    const uint32_t pieces = s.dim8, dim = pieces * 8u;
+    cache_bf16x8 qf[kSets][kD32];
+    uint32_t limit[kSets];
+    auto limit_of = [&](uint32_t row) FB4_INLINE {
+        const uint32_t token = (tile * kTileRows + row) / group;
+        return s.causal ? (uint32_t)max((int64_t)rows.len - (int64_t)rows.n + (int64_t)token + 1, (int64_t)0) : rows.len;
+    };
+#pragma unroll
+    for (int u = 0; u < kSets; ++u) {
+        const uint32_t row = min(first_row + 16u * u + r, n_rows - 1u), at = tile * kTileRows + row, token = at / group, head = hk * group + (at - token * group);
+        limit[u] = limit_of(row);
+        const uint16_t* x = q + ((size_t)head * sq.head + (size_t)(rows.first + token) * sq.token) * 8u;
+#pragma unroll
+        for (int i = 0; i < kD32; ++i) {
+            uint4 w = make_uint4(0, 0, 0, 0);
+            if (kWhole || kD32 * g + i < pieces) w = reinterpret_cast<const uint4*>(x)[kD32 * g + i];
+            qf[u][i] = __builtin_bit_cast(cache_bf16x8, w);
+        }
+    }
+    // the keys that all rows of this wavefront see, of the workgroup; the keys that any sees
+    const uint32_t least = scalar(limit_of(min(first_row, n_rows - 1u))), least_of_all = scalar(limit_of(0)), end = scalar(limit_of(n_rows - 1u));
+    to = min(to, steps_of(end));
+    const uint32_t bits = s.page_bits, in_page = (1u << bits) - 1u, held = (rows.len + in_page) >> bits;
+    const int32_t* table = tables + (size_t)b * s.max_pages;
+    const size_t page_bytes = (size_t)dim << bits;
+    const uint8_t* values = cache + (size_t)s.pages * s.heads_k * page_bytes;
+    auto page_of = [&](uint32_t key) FB4_INLINE {   // -1: none
+        const uint32_t i = key >> bits;
+        const int32_t p = i < held ? table[i] : -1;
+        return (uint32_t)p < s.pages ? p : -1;
+    };
+    // ---- this wavefront's sixteenth of a step, into registers and from there into LDS
+    const uint32_t mine = 16u * wave;
+    uint2 kr[kAsksK];
+    uint4 vr[kAsksV];
+    uint32_t k_byte = 0, v_byte = 0;
+    bool there = false;
+    auto ask = [&](uint32_t step, int32_t page) FB4_INLINE {
+        const uint32_t p = scalar((uint32_t)max(page, 0)), place = (step * kCacheStep + mine) & in_page;
+        there = (int32_t)scalar((uint32_t)page) >= 0;
+        const size_t at = (size_t)p * s.heads_k + hk;
+        const uint8_t* k = cache + at * page_bytes + place * dim;
+        const uint8_t* v = values + at * page_bytes + place;
+        k_byte = scales[at];
+        v_byte = scales[(size_t)s.pages * s.heads_k + at];
+#pragma unroll
+        for (int i = 0; i < kAsksK; ++i) {
+            const uint32_t j = 64u * i + lane;
+            kr[i] = make_uint2(0, 0);
+            if (kWhole || j < 16u * pieces) kr[i] = reinterpret_cast<const uint2*>(k)[j];
+        }
+#pragma unroll
+        for (int i = 0; i < kAsksV; ++i) {
+            const uint32_t c = 64u * i + lane;
+            vr[i] = make_uint4(0, 0, 0, 0);
+            if (c < dim) vr[i] = *reinterpret_cast<const uint4*>(v + ((size_t)c << bits));
+        }
+    };
+    auto put = [&](uint32_t step, uint32_t buffer) FB4_INLINE {
+        const float fk = __builtin_bit_cast(float, k_byte << 23), fv = __builtin_bit_cast(float, v_byte << 23);
+        uint8_t* to_k = lds + buffer;
+        uint8_t* to_v = lds + buffer + kKeys + 2u * mine;
+#pragma unroll
+        for (int i = 0; i < kAsksK; ++i) {
+            const uint32_t j = 64u * i + lane, key = kWhole ? j / (4u * kD32) : j / pieces, c = j - key * (kWhole ? 4u * kD32 : pieces);
+            // key 4 t + x of sixteenth w: row 4 w + x of tile t
+            if (kWhole || j < 16u * pieces)
+                *reinterpret_cast<cache_bf16x8*>(to_k + ((key & ~3u) * 4u + 4u * wave + (key & 3u)) * kPitchK + 16u * c) = cache_decode(kr[i].x, kr[i].y, fk);
+        }
+        // a page that is not there, what lies behind the end: zeros; and no NaN that a query does not see
+        const uint32_t key = step * kCacheStep + mine;
+        uint32_t note = there ? 0u : kNone;
+        if (!there || key + 16u > least_of_all) {
+            const uint32_t n = there && rows.len > key ? min(rows.len - key, 16u) : 0u;
+            uint32_t some = 0;
+#pragma unroll
+            for (int i = 0; i < kAsksV; ++i) {
+                vr[i] = first_bytes(vr[i], n);
+                const uint4 bad = nans_of(vr[i]);
+                some |= bad.x | bad.y | bad.z | bad.w;
+                vr[i] = without(vr[i], bad);
+            }
+            if (__any(some != 0u)) note |= kNan;
+        }
+#pragma unroll
+        for (int i = 0; i < kAsksV; ++i) {
+            const uint32_t c = 64u * i + lane;
+            if (c < 32u * kD32) {   // (channels past the row: zeros)
+                cache_bf16x8* at = reinterpret_cast<cache_bf16x8*>(to_v + c * kPitchV);
+                at[0] = cache_decode(vr[i].x, vr[i].y, fv);
+                at[1] = cache_decode(vr[i].z, vr[i].w, fv);
+            }
+        }
+        if (lane == 0) notes[buffer != 0u][wave] = note;
+    };
+    const float factor = s.scale * kCacheLog2E;
+    cache_f32x4 o[kSets][2 * kD32];
+    float reference[kSets], sum[kSets];
+#pragma unroll
+    for (int u = 0; u < kSets; ++u) {
+        reference[u] = -__builtin_inff();
+        sum[u] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < 2 * kD32; ++d) o[u][d] = cache_f32x4{0, 0, 0, 0};
+    }
+    const uint32_t k_at = r * kPitchK + 16u * kD32 * g, v_at = kKeys + r * kPitchV + 32u * g;
+    const bool idle = first_row >= n_rows;
+    int32_t page = -1;
+    if (!kWhole) {   // channels past the row, of keys: zeros for good (the queries' are too, but 0 times what was here need not be)
+        for (uint32_t i = threadIdx.x; i < 2u * kBuffer / 16u; i += 64u * kCacheWaves) reinterpret_cast<uint4*>(lds)[i] = make_uint4(0, 0, 0, 0);
+        __syncthreads();
+    }
+    if (from < to) {
+        ask(from, page_of(from * kCacheStep + mine));
+        page = page_of((from + 1u) * kCacheStep + mine);
+        put(from, 0);
+        if (from + 1u < to) ask(from + 1u, page);
+        page = page_of((from + 2u) * kCacheStep + mine);
+    }
+    uint32_t buffer = 0, seen_notes = 0;
+    for (uint32_t step = from; step < to; ++step) {
+        __syncthreads();   // this step's operands are there; everyone is done with the other buffer
+        const uint8_t* keys = lds + buffer + k_at;
+        const uint8_t* vals = lds + buffer + v_at;
+        if (!idle) {
+            const uint32_t note = notes[buffer != 0u][g];
+            cache_f32x4 sc[kSets][4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+#pragma unroll
+                for (int u = 0; u < kSets; ++u) sc[u][t] = cache_f32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < kD32; ++i) {
+                    const cache_bf16x8 a = *reinterpret_cast<const cache_bf16x8*>(keys + 16u * t * kPitchK + 16u * i);
+#pragma unroll
+                    for (int u = 0; u < kSets; ++u) sc[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[u][i], sc[u][t], 0, 0, 0);
+                }
+            }
+            const uint32_t key = step * kCacheStep + 16u * g;
+            if (step * kCacheStep + kCacheStep > least || __any(note & kNone)) {
+#pragma unroll
+                for (int u = 0; u < kSets; ++u) {
+                    const uint32_t seen = note & kNone ? 0u : limit[u];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sc[u][t][i] = key + 4u * t + i >= seen ? -__builtin_inff() : sc[u][t][i];
+                    }
+                }
+            }
+            cache_bf16x8 p[kSets][2];
+#pragma unroll
+            for (int u = 0; u < kSets; ++u) cache_weights(sc[u], reference[u], sum[u], o[u], p[u], factor);
+#pragma unroll
+            for (int d = 0; d < 2 * kD32; ++d) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const cache_bf16x8 a = *reinterpret_cast<const cache_bf16x8*>(vals + 16u * d * kPitchV + 16u * h);
+#pragma unroll
+                    for (int u = 0; u < kSets; ++u) o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[u][h], o[u][d], 0, 0, 0);
+                }
+            }
+            seen_notes |= note;
+        }
+        buffer = kBuffer - buffer;
+        if (step + 1u < to) {
+            put(step + 1u, buffer);
+            if (step + 2u < to) {
+                ask(step + 2u, page);
+                page = page_of((step + 3u) * kCacheStep + mine);
+            }
+        }
+    }
+    if (__any(seen_notes & kNan)) {
+        for (uint32_t step = max(from, least_of_all / kCacheStep); step < to; ++step) {
+            const uint32_t key = step * kCacheStep + 16u * g;
+            const int32_t at = page_of(key);
+            const uint8_t* v = values + ((size_t)max(at, 0) * s.heads_k + hk) * page_bytes + (key & in_page);
+            const uint32_t n = at >= 0 && rows.len > key ? min(rows.len - key, 16u) : 0u;
+            mark_nans(o, [&](int d) FB4_INLINE {
+                const uint32_t c = 16u * d + r;
+                return nans_of(c < dim ? first_bytes(*reinterpret_cast<const uint4*>(v + ((size_t)c << bits)), n) : make_uint4(0, 0, 0, 0));
+            }, key, limit);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kSets; ++u) {
+        sum[u] += __shfl_xor(sum[u], 16);
+        sum[u] += __shfl_xor(sum[u], 32);
+        const uint32_t row = first_row + 16u * u + r;
+        if (row >= n_rows) continue;
+        const uint32_t at = tile * kTileRows + row, token = at / group, head = hk * group + (at - token * group);
+        const float total = sum[u], inverse = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
+#pragma unroll
+        for (int d = 0; d < 2 * kD32; ++d) {
+            const uint32_t c = 16u * d + 4u * g;
+            if (!kWhole && c >= dim) continue;
+            if (kSplit) {
+                *reinterpret_cast<cache_f32x4*>(reinterpret_cast<float*>(out) + ((size_t)blockIdx.x * kTileRows + row) * dim + c) = o[u][d];
+            } else {
+                uint16_t* place = out + ((size_t)head * so.head + (size_t)(rows.first + token) * so.token) * 8u + c;
+                *reinterpret_cast<uint2*>(place) = rounded(o[u][d], inverse);
+            }
+        }
+        if (g == 0) {
+            const float base = reference[u] == -__builtin_inff() ? 0.0f : reference[u];
+            if (kSplit) reinterpret_cast<float2*>(lse)[(size_t)blockIdx.x * kTileRows + row] = make_float2(reference[u], total);
+            else if (lse) lse[(size_t)(rows.first + token) * s.heads + head] = total == 0.0f ? -__builtin_inff() : fmaf(base, s.scale, kCacheLn2 * __builtin_amdgcn_logf(total));
+        }
     }
 }
 
@@ -480,10 +776,8 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const float* workspace,
     if (lane >= 32u) return;
     const float inverse = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
     if (c < dim) {
-        const cache_bf16x2 lo = __builtin_convertvector((cache_f32x2{o[0] * inverse, o[1] * inverse}), cache_bf16x2);
-        const cache_bf16x2 hi = __builtin_convertvector((cache_f32x2{o[2] * inverse, o[3] * inverse}), cache_bf16x2);
         uint16_t* place = out + ((size_t)head * so.head + (size_t)token * so.token) * 8u + c;
-        *reinterpret_cast<uint2*>(place) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+        *reinterpret_cast<uint2*>(place) = rounded(o, inverse);
     }
     if (lse && lane == 0) lse[(size_t)token * s.heads + head] = sum == 0.0f ? -__builtin_inff() : fmaf(reference, s.scale, kCacheLn2 * __builtin_amdgcn_logf(sum));
 }

@@ -31,7 +31,7 @@ int strides_of(const int64_t* strides, T* out)
 }
 
 struct CachePlan {
-    int sets;               // of 16 rows to a tile
+    int rows16;             // rows of a tile / 16: 8 for the kernel of many queries
     bool split;
     int64_t tiles, positions;
 };
@@ -46,8 +46,8 @@ int plan_attention(int64_t tokens, int heads, int heads_k, int64_t dim, int page
     const int64_t rows = tokens * (heads / heads_k);
     if (rows > kMaxInt) return FB4_ERR_UNSUPPORTED;
     const int64_t each = batch ? rows / batch : 0;
-    p->sets = each > 16 ? 2 : 1;
-    p->tiles = rows / (16 * p->sets) + batch;
+    p->rows16 = each > 40 || (tokens - batch) * (heads / heads_k) >= 1024 ? 8 : each > 16 ? 2 : 1;
+    p->tiles = rows / (16 * p->rows16) + batch;
     p->split = p->tiles * heads_k < kCacheTarget && (max_pages << bits) > (int64_t)kCacheLeastShare * kCacheStep;
     p->positions = p->tiles * heads_k + (p->split ? kCacheTarget : 0);
     if (p->positions > (1 << 24) - 1) return FB4_ERR_UNSUPPORTED;
@@ -143,7 +143,7 @@ size_t fb4_cache_attention_workspace(int64_t tokens, int heads, int heads_k, int
 {
     CachePlan p;
     if (plan_attention(tokens, heads, heads_k, dim, page, max_pages, batch, &p) != FB4_OK || !p.split || tokens == 0 || batch == 0) return 0;
-    return (size_t)p.positions * (size_t)(16 * p.sets) * (size_t)(dim + 2) * sizeof(float);
+    return (size_t)p.positions * (size_t)(16 * p.rows16) * (size_t)(dim + 2) * sizeof(float);
 }
 
 int fb4_cache_attention(const void* q, const int64_t* q_strides, int64_t tokens, int heads, int heads_k, int64_t dim, const uint8_t* cache, const uint8_t* scales,
@@ -166,15 +166,18 @@ int fb4_cache_attention(const void* q, const int64_t* q_strides, int64_t tokens,
         return FB4_ERR_UNSUPPORTED;
     // (no pages: no sequence has a key)
     const CacheShape s = {(uint32_t)tokens, pages ? (uint32_t)max_pages : 0u, (uint32_t)pages, (uint16_t)batch, (uint16_t)heads, (uint16_t)heads_k,
-                          (uint16_t)kCacheTarget, (uint8_t)page_bits_of(page), (uint8_t)(dim / 8), (uint8_t)causal, (uint8_t)p.sets, scale};
+                          (uint16_t)kCacheTarget, (uint8_t)page_bits_of(page), (uint8_t)(dim / 8), (uint8_t)causal, (uint8_t)p.rows16, scale};
     hipStream_t st = static_cast<hipStream_t>(stream);
     float* parts = static_cast<float*>(workspace);
-    float* states = p.split ? parts + (size_t)p.positions * (16 * p.sets) * dim : nullptr;
+    float* states = p.split ? parts + (size_t)p.positions * (16 * p.rows16) * dim : nullptr;
     const dim3 grid((unsigned)p.positions);
-#define FB4_CACHE_LAUNCH(d, u, w, split) launch(cache_attention_kernel<d, u, w, split>, grid, dim3(64 * kCacheWaves), 0, st, static_cast<const uint16_t*>(q), cache, scales, tables, lens, starts, static_cast<uint16_t*>(split ? workspace : out), split ? states : lse, sq, so, s)
+#define FB4_CACHE_KERNEL(kernel, split) launch(kernel, grid, dim3(64 * kCacheWaves), 0, st, static_cast<const uint16_t*>(q), cache, scales, tables, lens, starts, static_cast<uint16_t*>(split ? workspace : out), split ? states : lse, sq, so, s)
+#define FB4_CACHE_LAUNCH(d, u, w, split) FB4_CACHE_KERNEL((cache_attention_kernel<d, u, w, split>), split)
+#define FB4_CACHE_TILES(d, w, split) FB4_CACHE_KERNEL((cache_tiles_kernel<d, w, split>), split)
 #define FB4_CACHE_SETS(d, w, split)                     \
-    if (p.sets == 1) FB4_CACHE_LAUNCH(d, 1, w, split); \
-    else FB4_CACHE_LAUNCH(d, 2, w, split)
+    if (p.rows16 == 8) FB4_CACHE_TILES(d, w, split);     \
+    else if (p.rows16 == 2) FB4_CACHE_LAUNCH(d, 2, w, split); \
+    else FB4_CACHE_LAUNCH(d, 1, w, split)
 #define FB4_CACHE_CASE(d)                               \
     case d:                                             \
         if (dim == 32 * d) {                            \
@@ -190,7 +193,9 @@ int fb4_cache_attention(const void* q, const int64_t* q_strides, int64_t tokens,
     }
 #undef FB4_CACHE_CASE
 #undef FB4_CACHE_SETS
+#undef FB4_CACHE_TILES
 #undef FB4_CACHE_LAUNCH
+#undef FB4_CACHE_KERNEL
     if (p.split) {
         const int64_t rows = tokens * heads;   // (below the target's tiles of 64 rows and the batch's)
         const bool few = rows <= 4096;
