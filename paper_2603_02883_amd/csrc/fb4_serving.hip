@@ -134,7 +134,7 @@ int fb4_cache_store(const void* k, const int64_t* k_strides, const void* v, cons
     const int64_t groups = (tokens + span - 1) / span * heads_k * 2;
     if (groups > (1 << 24) - 1) return FB4_ERR_UNSUPPORTED;
     const StoreShape s = {(uint32_t)tokens, (uint32_t)pages, (uint32_t)span, (uint16_t)heads_k, (uint8_t)bits, (uint8_t)(dim / 8)};
-    launch(cache_store_kernel, dim3((unsigned)groups), dim3(kStoreThreads), 0, static_cast<hipStream_t>(stream), static_cast<const uint16_t*>(k),
+    launch(dim / 8 * page / 4 > kStoreThreads ? cache_store_kernel<2> : cache_store_kernel<1>, dim3((unsigned)groups), dim3(kStoreThreads), 0, static_cast<hipStream_t>(stream), static_cast<const uint16_t*>(k),
            static_cast<const uint16_t*>(v), slots, cache, scales, sk, sv, s);
     return hipGetLastError() == hipSuccess ? FB4_OK : FB4_ERR_HIP;
 }
