@@ -109,9 +109,13 @@ int fb4_cache_plan(const int32_t* lens, const int32_t* adds, int64_t batch, int 
                           static_cast<const void*>(starts), static_cast<const void*>(slots), static_cast<const void*>(positions)}) {
         if (!aligned(p, 4)) return FB4_ERR_UNSUPPORTED;
     }
-    const PlanShape s = {(uint32_t)batch, (uint32_t)max_pages, (uint32_t)n_free, (uint32_t)tokens, (uint32_t)bits};
+    // (few sequences and tokens: few wavefronts to wait for each other)
+    const int64_t most = std::max(batch, std::min<int64_t>(tokens / 4, kPlanMost));
+    const uint32_t threads = most <= 64 ? 64 : most <= 256 ? 256 : kPlanMost;
+    const PlanShape s = {(uint32_t)batch, (uint32_t)max_pages, (uint32_t)n_free, (uint32_t)tokens, (uint32_t)bits, threads};
     hipStream_t st = static_cast<hipStream_t>(stream);
-    launch(cache_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, lens, adds, free_count, tables, free_pages, lens_out, free_count_out, starts, slots, positions, s);
+    launch(batch > (int64_t)kPlanMost ? cache_plan_kernel<4> : cache_plan_kernel<1>, dim3(1), dim3(threads), 0, st, lens, adds, free_count, tables, free_pages, lens_out,
+           free_count_out, starts, slots, positions, s);
     if (tokens > (int64_t)kPlanOwnTokens)
         launch(cache_slots_kernel, dim3((unsigned)((tokens + 1023) / 1024)), dim3(256), 0, st, starts, lens_out, tables, slots, positions, s);
     return hipGetLastError() == hipSuccess ? FB4_OK : FB4_ERR_HIP;
