@@ -611,7 +611,7 @@ int fb4_block_attention(const void* q, const void* k, const void* v, const int64
  *               aligned with block 16 (FB4_ERR_UNSUPPORTED otherwise); a
  *               DID >= n_dialects gives zero magnitudes
  *   n           at least 0, below 2^28 (FB4_ERR_UNSUPPORTED beyond)
- *   cols        a multiple of 32, below 2^28 (FB4_ERR_UNSUPPORTED otherwise); 0:
+ *   cols        a multiple of 32, below 2^25 (FB4_ERR_UNSUPPORTED otherwise); 0:
  *               the bias, or zeros
  *   block       32 or 16
  *   bias        device, float [n] or NULL

@@ -30,6 +30,9 @@ struct MatvecShape {
     uint16_t f32;                  // float results
 };
 
+// Chunks whose scales and dialects a workgroup holds at a time: 32 KiB of all its rows, at most.
+constexpr uint32_t matvec_chunks(int tiles, bool half) { return 1024u / tiles / (half ? 2 : 1); }
+
 // Two registers of E4M3 bytes of eight codes (a word), even elements and odd ones.
 __device__ __forceinline__ void e4m3_of_codes(uint32_t w, uint2 table, uint32_t& even, uint32_t& odd)
 {
@@ -54,17 +57,22 @@ __device__ __forceinline__ mv_bf16x8 channels_of(uint4 v)
     return __builtin_bit_cast(mv_bf16x8, o);
 }
 
-// A workgroup takes 16 kTiles rows of the weights and all rows of x (16 kSets at most); its wavefronts share the channels, kSteps times
-// 128 in turn, and meet in LDS.
-template <int kTiles, int kSets, bool kHalf>
+// A workgroup takes 16 kTiles rows of the weights and all rows of x (16 kSets at most); its wavefronts share the channels, 128 at a time in
+// turn, and meet in LDS.  What a turn reads is asked for while the one before it is computed.  Scales and dialects come through LDS, up to 16
+// KiB of a row's words side by side at a time: as a lane's own reads, two bytes to a chunk of 16, they are as many requests as the codes (49152 x
+// 8192, one row: 61 us so, 52.7 through LDS).  kDirect: those reads all the same, where a wavefront has a turn or two and the way
+// through LDS would be one more wait (6912 x 1152: 3.7 and 4.4 us).
+template <int kTiles, int kSets, bool kHalf, bool kDirect>
 __global__ __launch_bounds__(512) void matvec_kernel(const uint8_t* codes, const uint16_t* meta, const uint16_t* x, const uint8_t* blob,
                                                      const float* bias, void* out, MatvecShape s)
 {
-    constexpr int kSteps = 2;                    // a row's whole lines of 128 bytes
     constexpr uint32_t kOut = 16 * kTiles;
+    constexpr int kScales = kHalf ? 2 : 1;
+    constexpr uint32_t kWord = kHalf ? 4 : 2, kMost = matvec_chunks(kTiles, kHalf);   // bytes of a chunk's scales and dialects; chunks at a time
     extern __shared__ __align__(16) uint8_t lds[];
     uint2* tables = reinterpret_cast<uint2*>(lds);                 // [32] dialects' magnitudes
-    float* meet = reinterpret_cast<float*>(lds + 256);             // [waves][16 kSets][kOut]
+    uint8_t* words = lds + 256;                                    // [kOut] rows, 16 bytes further apart than they are long
+    float* meet = reinterpret_cast<float*>(lds + 256);             // [waves][16 kSets][kOut], when the words are done with
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t r = lane & 15u, g = lane >> 4;
     if (threadIdx.x < 64) {                      // (an integer's bf16 exponent and upper mantissa bits, rebiased)
@@ -77,15 +85,19 @@ __global__ __launch_bounds__(512) void matvec_kernel(const uint8_t* codes, const
         }
         reinterpret_cast<uint32_t*>(tables)[threadIdx.x] = b;
     }
+    // Tile t's rows from `from` on: a tile that would pass the last row ends there, and one of fewer rows than 16 has the last one
+    // several times.  One offset for all tiles and a base each, which stays in scalar registers.
     const uint32_t first = blockIdx.x * kOut;
-    const uint8_t* code_row[kTiles];
-    const uint8_t* meta_row[kTiles];
+    const uint8_t* code_base[kTiles];
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {           // (behind the last row that one again)
-        const size_t row = min(first + 16u * t + r, s.n - 1u);
-        code_row[t] = codes + row * s.chunks * 16u;
-        meta_row[t] = reinterpret_cast<const uint8_t*>(meta) + row * s.chunks * (kHalf ? 4u : 2u);
+    for (int t = 0; t < kTiles; ++t) {
+        const size_t from = min(first + 16u * t, max(s.n, 16u) - 16u);
+        code_base[t] = codes + from * s.chunks * 16u;
     }
+    const uint32_t row = min(r, s.n - 1u);
+    auto row_of = [&](uint32_t at) __attribute__((always_inline)) {   // of the workgroup's rows as they are computed
+        return (size_t)min(first + (at & ~15u), max(s.n, 16u) - 16u) + min(at & 15u, s.n - 1u);
+    };
     const uint16_t* x_row[kSets];
     bool has[kSets];
 #pragma unroll
@@ -93,67 +105,112 @@ __global__ __launch_bounds__(512) void matvec_kernel(const uint8_t* codes, const
         has[u] = 16u * u + r < s.rows;
         x_row[u] = x + (size_t)(16u * u + r) * s.x_stride * 8u;
     }
+    struct Turn {
+        uint4 codes[kTiles], x[kSets][4];
+        uint32_t meta[kDirect ? kTiles : 1];
+    };
+    auto ask = [&](uint32_t c0, Turn& w) __attribute__((always_inline)) {
+        const uint32_t c = c0 + g, code_at = (row * s.chunks + c) * 16u;
+        const bool live = c < s.chunks;          // (codes of zeros are weights of zero)
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            w.codes[t] = make_uint4(0, 0, 0, 0);
+            if (live) w.codes[t] = *reinterpret_cast<const uint4*>(code_base[t] + code_at);
+            if (kDirect) {
+                const size_t at = row_of(16u * t + r) * s.chunks + c;
+                w.meta[t] = 0;
+                if (live) w.meta[t] = kHalf ? reinterpret_cast<const uint32_t*>(meta)[at] : meta[at];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kSets; ++u) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                w.x[u][j] = make_uint4(0, 0, 0, 0);
+                if (live && has[u]) w.x[u][j] = reinterpret_cast<const uint4*>(x_row[u] + (size_t)c * 32u)[j];
+            }
+        }
+    };
     mv_f32x4 acc[kTiles][kSets];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
 #pragma unroll
         for (int u = 0; u < kSets; ++u) acc[t][u] = mv_f32x4{0, 0, 0, 0};
     }
-    __syncthreads();
-    for (uint32_t c0 = wave * 4u * kSteps; c0 < s.chunks; c0 += s.waves * 4u * kSteps) {
-        uint4 cw[kSteps][kTiles], xw[kSteps][kSets][4];
-        uint32_t mw[kSteps][kTiles];
+    const uint32_t pitch = min(s.chunks, kMost) * kWord + 16u & ~15u;
+    auto compute = [&](const Turn& w, uint32_t c0) __attribute__((always_inline)) {   // c0: from the words' first chunk on
+        uint32_t word[kTiles];
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const uint32_t c = c0 + 4u * i + g;
-            const bool live = c < s.chunks;
+        for (int t = 0; t < kTiles; ++t) {
+            const uint8_t* at = words + (16u * t + r) * pitch + min(c0 + g, kMost - 1u) * kWord;   // (behind the last chunk: any, its codes are zeros)
+            if (kDirect) word[t] = w.meta[t];
+            else word[t] = kHalf ? *reinterpret_cast<const uint32_t*>(at) : *reinterpret_cast<const uint16_t*>(at);
+        }
+        uint2 table[kTiles][kScales];
+        float scale[kTiles][kScales];
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) {   // (codes of zeros are weights of zero)
-                cw[i][t] = make_uint4(0, 0, 0, 0);
-                mw[i][t] = 0;
-                if (live) {
-                    cw[i][t] = *reinterpret_cast<const uint4*>(code_row[t] + (size_t)c * 16u);
-                    mw[i][t] = kHalf ? reinterpret_cast<const uint32_t*>(meta_row[t])[c] : reinterpret_cast<const uint16_t*>(meta_row[t])[c];
-                }
-            }
+        for (int t = 0; t < kTiles; ++t) {
 #pragma unroll
-            for (int u = 0; u < kSets; ++u) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    xw[i][u][j] = make_uint4(0, 0, 0, 0);
-                    if (live && has[u]) xw[i][u][j] = reinterpret_cast<const uint4*>(x_row[u] + (size_t)c * 32u)[j];
-                }
+            for (int k = 0; k < kScales; ++k) {
+                const uint32_t m = kHalf ? (word[t] >> (16 * k)) & 0xFFFFu : word[t], did = m & 0xFFu;
+                table[t][k] = tables[did & 31u];
+                if (did > 31u) table[t][k] = make_uint2(0, 0);
+                scale[t][k] = __builtin_bit_cast(float, (max(m >> 8, 4u) - 3u) << 23);
             }
         }
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            uint2 table[kTiles][kHalf ? 2 : 1];
-            float scale[kTiles][kHalf ? 2 : 1];
+        for (int j = 0; j < 4; ++j) {
+            mv_bf16x8 b[kSets];
+#pragma unroll
+            for (int u = 0; u < kSets; ++u) b[u] = channels_of(w.x[u][j]);
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
+                const uint32_t y = j == 0 ? w.codes[t].x : j == 1 ? w.codes[t].y : j == 2 ? w.codes[t].z : w.codes[t].w;
+                const mv_bf16x8 a = weights_of(y, table[t][kHalf ? j / 2 : 0], scale[t][kHalf ? j / 2 : 0]);
 #pragma unroll
-                for (int k = 0; k < (kHalf ? 2 : 1); ++k) {
-                    const uint32_t m = kHalf ? (mw[i][t] >> (16 * k)) & 0xFFFFu : mw[i][t], did = m & 0xFFu;
-                    table[t][k] = tables[did & 31u];
-                    if (did > 31u) table[t][k] = make_uint2(0, 0);
-                    scale[t][k] = __builtin_bit_cast(float, (max(m >> 8, 4u) - 3u) << 23);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                mv_bf16x8 b[kSets];
-#pragma unroll
-                for (int u = 0; u < kSets; ++u) b[u] = channels_of(xw[i][u][j]);
-#pragma unroll
-                for (int t = 0; t < kTiles; ++t) {
-                    const uint32_t w = j == 0 ? cw[i][t].x : j == 1 ? cw[i][t].y : j == 2 ? cw[i][t].z : cw[i][t].w;
-                    const mv_bf16x8 a = weights_of(w, table[t][kHalf ? j / 2 : 0], scale[t][kHalf ? j / 2 : 0]);
-#pragma unroll
-                    for (int u = 0; u < kSets; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[u], acc[t][u], 0, 0, 0);
-                }
+                for (int u = 0; u < kSets; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[u], acc[t][u], 0, 0, 0);
             }
         }
+    };
+    // The words of chunks `from` .. of all rows: 16 bytes a thread where they lie so, else one by one.
+    auto fetch_words = [&](uint32_t from, uint32_t n) __attribute__((always_inline)) {
+        const uint8_t* base = reinterpret_cast<const uint8_t*>(meta);
+        const size_t row_bytes = (size_t)s.chunks * kWord;
+        const uint32_t per = 16u / kWord, pieces = (n + per - 1u) / per;
+        if (n % per == 0 && row_bytes % 16u == 0 && (reinterpret_cast<uintptr_t>(meta) & 15u) == 0) {
+            for (uint32_t i = threadIdx.x; i < kOut * pieces; i += s.waves * 64u) {
+                const uint32_t at = i / pieces, p = i - at * pieces;
+                *reinterpret_cast<uint4*>(words + at * pitch + 16u * p) = *reinterpret_cast<const uint4*>(base + row_of(at) * row_bytes + from * kWord + 16u * p);
+            }
+        } else {
+            for (uint32_t i = threadIdx.x; i < kOut * n; i += s.waves * 64u) {
+                const uint32_t at = i / n, p = i - at * n;
+                const uint8_t* x0 = base + row_of(at) * row_bytes + (from + p) * kWord;
+                if (kHalf) *reinterpret_cast<uint32_t*>(words + at * pitch + 4u * p) = *reinterpret_cast<const uint32_t*>(x0);
+                else *reinterpret_cast<uint16_t*>(words + at * pitch + 2u * p) = *reinterpret_cast<const uint16_t*>(x0);
+            }
+        }
+    };
+    const uint32_t stride = s.waves * 4u;
+    Turn a, b;
+    for (uint32_t from = 0; from < s.chunks; from += kDirect ? s.chunks : kMost) {   // (kMost is whole rounds of the wavefronts' turns)
+        const uint32_t n = kDirect ? s.chunks : min(s.chunks - from, kMost);
+        uint32_t c = wave * 4u;
+        ask(from + c, a);
+        if (from) __syncthreads();
+        if (!kDirect) fetch_words(from, n);
+        __syncthreads();
+        while (c < n) {
+            if (c + stride < n) ask(from + c + stride, b);
+            compute(a, c);
+            c += stride;
+            if (c >= n) break;
+            if (c + stride < n) ask(from + c + stride, a);
+            compute(b, c);
+            c += stride;
+        }
     }
+    __syncthreads();
     // accumulator i: weight row 4 (lane / 16) + i, row of x lane % 16
 #pragma unroll
     for (int u = 0; u < kSets; ++u) {
@@ -162,11 +219,13 @@ __global__ __launch_bounds__(512) void matvec_kernel(const uint8_t* codes, const
     }
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < s.rows * kOut; i += s.waves * 64u) {
-        const uint32_t row = i / kOut, col = i - row * kOut;
+        const uint32_t at_row = i / kOut, col = i - at_row * kOut;
         if (first + col >= s.n) continue;
+        // (its place in its tile, which may begin earlier)
+        const uint32_t begin = first + (col & ~15u), place = col + (begin - min(begin, max(s.n, 16u) - 16u));
         float sum = bias ? bias[first + col] : 0.0f;
-        for (uint32_t w = 0; w < s.waves; ++w) sum += meet[(w * 16u * kSets + row) * kOut + col];
-        const size_t at = (size_t)((long long)row * s.out_stride) + first + col;
+        for (uint32_t w = 0; w < s.waves; ++w) sum += meet[(w * 16u * kSets + at_row) * kOut + place];
+        const size_t at = (size_t)((long long)at_row * s.out_stride) + first + col;
         if (s.f32) reinterpret_cast<float*>(out)[at] = sum;
         else reinterpret_cast<__bf16*>(out)[at] = (__bf16)sum;
     }

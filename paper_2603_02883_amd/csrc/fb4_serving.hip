@@ -64,7 +64,7 @@ int fb4_matvec(const fb4_luts* luts, const void* x, int64_t rows, int64_t x_row_
     if (!luts || rows < 0 || n < 0 || cols < 0 || x_row_stride < cols || out_row_stride < n || (block != 32 && block != 16) ||
         (out_dtype != FB4_DTYPE_BF16 && out_dtype != FB4_DTYPE_F32))
         return FB4_ERR_INVALID_ARG;
-    if (rows > kMatvecMaxRows || cols % 32 || n >= 1 << 28 || cols >= 1 << 28) return FB4_ERR_UNSUPPORTED;
+    if (rows > kMatvecMaxRows || cols % 32 || n >= 1 << 28 || cols >= 1 << 25) return FB4_ERR_UNSUPPORTED;
     if (rows == 0 || n == 0) return FB4_OK;
     if (!out || (cols > 0 && (!x || !codes || !meta))) return FB4_ERR_INVALID_ARG;
     if (!aligned(x, 16) || (rows > 1 && x_row_stride % 8) || x_row_stride / 8 > 0xFFFFFFFFll || !aligned(codes, 16) || !aligned(meta, block == 16 ? 4 : 2) ||
@@ -73,21 +73,26 @@ int fb4_matvec(const fb4_luts* luts, const void* x, int64_t rows, int64_t x_row_
     if (int rc = check_device(luts)) return rc;
     const int sets = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     const int64_t chunks = cols / 32;
-    const int tiles = n >= 64 * 512 && sets < 4 ? 4 : n >= 32 * 256 ? 2 : 1;
-    const int64_t steps = (chunks + 7) / 8;
-    const int waves = (int)std::max<int64_t>(1, std::min<int64_t>(steps, sets == 4 ? 4 : 8));
+    // Rows of the weights to a workgroup, 16 to a tile: as many as leave every compute unit a workgroup, since each reads all of x (16 rows,
+    // 16384 x 4096: 14.5 us with four tiles, 15.1 with two, 21 with one; 37 rows, 4610 x 1184: two 8.2, one 8.8; one row, 6912 x 1152: one 4.35, two 4.40)
+    const int tiles = sets == 4 ? (n >= 4096 ? 2 : 1) : n >= 16384 ? 4 : n >= 8192 ? 2 : 1;
+    const int64_t steps = (chunks + 3) / 4;
+    const int waves = (int)std::max<int64_t>(1, std::min<int64_t>(steps, 8));
+    const bool direct = tiles == 1 && steps <= 2 * waves;
     const MatvecShape s = {(uint32_t)n, (uint32_t)chunks, (uint32_t)(x_row_stride / 8), (uint32_t)waves, out_row_stride, (uint16_t)rows,
                            (uint16_t)(out_dtype == FB4_DTYPE_F32)};
     const dim3 grid((unsigned)((n + 16 * tiles - 1) / (16 * tiles)));
-    const size_t lds = 256 + (size_t)waves * 16 * sets * 16 * tiles * sizeof(float);
-#define FB4_MATVEC_LAUNCH(t, u, h) launch(matvec_kernel<t, u, h>, grid, dim3(64 * waves), lds, static_cast<hipStream_t>(stream), codes, meta, static_cast<const uint16_t*>(x), luts->dev_blob, bias, out, s)
-#define FB4_MATVEC_CASE(t, u)                          \
-    if (tiles == t && sets == u) {                     \
-        if (block == 16) FB4_MATVEC_LAUNCH(t, u, true); \
-        else FB4_MATVEC_LAUNCH(t, u, false);           \
+    const size_t words = direct ? 0 : (size_t)16 * tiles * (std::min<size_t>(chunks, matvec_chunks(tiles, block == 16)) * (block == 16 ? 4 : 2) + 16);
+    const size_t lds = 256 + std::max(words, (size_t)waves * 16 * sets * 16 * tiles * sizeof(float));
+#define FB4_MATVEC_LAUNCH(t, u, h, d) launch(matvec_kernel<t, u, h, d>, grid, dim3(64 * waves), lds, static_cast<hipStream_t>(stream), codes, meta, static_cast<const uint16_t*>(x), luts->dev_blob, bias, out, s)
+#define FB4_MATVEC_CASE(t, u, d)                             \
+    if (tiles == t && sets == u && direct == d) {            \
+        if (block == 16) FB4_MATVEC_LAUNCH(t, u, true, d);   \
+        else FB4_MATVEC_LAUNCH(t, u, false, d);              \
     }
-    FB4_MATVEC_CASE(1, 1) FB4_MATVEC_CASE(2, 1) FB4_MATVEC_CASE(4, 1) FB4_MATVEC_CASE(1, 2) FB4_MATVEC_CASE(2, 2) FB4_MATVEC_CASE(4, 2) FB4_MATVEC_CASE(1, 4)
-    FB4_MATVEC_CASE(2, 4)
+    FB4_MATVEC_CASE(1, 1, true) FB4_MATVEC_CASE(1, 2, true) FB4_MATVEC_CASE(1, 4, true) FB4_MATVEC_CASE(1, 1, false) FB4_MATVEC_CASE(1, 2, false)
+    FB4_MATVEC_CASE(1, 4, false) FB4_MATVEC_CASE(2, 1, false) FB4_MATVEC_CASE(2, 2, false) FB4_MATVEC_CASE(2, 4, false) FB4_MATVEC_CASE(4, 1, false)
+    FB4_MATVEC_CASE(4, 2, false)
 #undef FB4_MATVEC_CASE
 #undef FB4_MATVEC_LAUNCH
     return hipGetLastError() == hipSuccess ? FB4_OK : FB4_ERR_HIP;

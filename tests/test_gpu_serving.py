@@ -741,3 +741,21 @@ def test_both_bindings_answer_alike(F, luts, monkeypatch):
                 lambda: F.fb4_cache_attention(x.view(2, -1, 64), state.cache, state.scales, state.tables, state.lens, state.lens, 16)):
         with pytest.raises(F.Fb4Error):
             bad()
+
+
+@pytest.mark.parametrize("block", [32, 16])
+@pytest.mark.parametrize("rows,n,cols", [(1, 16500, 40032), (3, 8250, 33344), (40, 4100, 33024), (33, 5000, 1088), (18, 16400, 20000), (2, 300, 33568), (2, 100, 65600)])
+def test_products_of_many_channels(F, luts, rows, n, cols, block):
+    """More channels than a workgroup holds scales of at a time; words that lie 16 bytes apart and not."""
+    g = gen(rows + n)
+    codes = torch.randint(0, 256, (n, cols // 2), device="cuda", generator=g, dtype=torch.uint8)
+    meta = torch.randint(120, 125, (n, cols // block), device="cuda", generator=g, dtype=torch.int16) * 256 + torch.randint(0, 32, (n, cols // block), device="cuda", generator=g, dtype=torch.int16)
+    x = randn(g, rows, cols).bfloat16()
+    check_product(F, luts, x, codes, meta, block, None, F.fb4_matvec(luts, x, codes, meta, block=block, out_dtype=F.DTYPE_F32))
+    # words that begin at any multiple of their size
+    at = torch.empty(meta.numel() + 8, device="cuda", dtype=torch.int16)
+    shift = 2 if block == 16 else 1
+    at[shift:shift + meta.numel()] = meta.view(-1)
+    x = randn(g, rows, cols).bfloat16()
+    same = F.fb4_matvec(luts, x, codes, meta, block=block)
+    assert torch.equal(same, F.fb4_matvec(luts, x, codes, at[shift:shift + meta.numel()].view(meta.shape), block=block))

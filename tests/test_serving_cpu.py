@@ -92,7 +92,7 @@ def test_matvec_refusals():
     for bad in (dict(rows=-1), dict(n=-1), dict(cols=-32), dict(sx=63), dict(so=4), dict(block=8), dict(block=64), dict(dtype=2), dict(x=None), dict(codes=None), dict(meta=None),
                 dict(out=None)):
         assert call(h, **bad) == F.ERR_INVALID_ARG, bad
-    for bad in (dict(rows=65), dict(cols=48), dict(n=2 ** 28, so=2 ** 28), dict(cols=2 ** 28, sx=2 ** 28), dict(x=P(AL + 8)), dict(sx=68), dict(codes=P(AL + 8)), dict(meta=P(AL + 1)),
+    for bad in (dict(rows=65), dict(cols=48), dict(n=2 ** 28, so=2 ** 28), dict(cols=2 ** 25, sx=2 ** 25), dict(x=P(AL + 8)), dict(sx=68), dict(codes=P(AL + 8)), dict(meta=P(AL + 1)),
                 dict(meta=P(AL + 2), block=16), dict(bias=P(AL + 2)), dict(out=P(AL + 1)), dict(out=P(AL + 2), dtype=1), dict(sx=2 ** 36), dict(rows=2 ** 62),
                 dict(n=2 ** 62, so=2 ** 62), dict(cols=2 ** 62, sx=2 ** 62)):
         assert call(h, **bad) == F.ERR_UNSUPPORTED, bad
