@@ -128,34 +128,57 @@ __device__ __forceinline__ uint32_t walk_parts(const int32_t* starts, const int3
 }
 
 // ------------------------------------------------------------------------------------------------ a step's weights, and bytes
-// Weights of four tiles of products (16 keys of this lane's query) as the second product's operands; the reference moves, and what is relative
-// to it, when a weight would pass 2^8.
+// What a query's weights are relative to: the largest product so far (-Inf: none), and its rounded product with the factor c = scale log2 e
+// (0: none).  Weights are exp2(S c - off), by one fused multiply-add whose product is exact, so that the rounding of `off` is one factor in all
+// weights and in their sum.  Beyond |off| = 2^20 that factor could itself be no small number, and the wavefront goes on with exp2((S - most) c).
+struct CacheState {
+    float most, off, sum;
+};
+// Moves it, and what is relative to it, when a weight would pass 2^8.
 template <int kD16>
-__device__ __forceinline__ void cache_weights(const cache_f32x4 (&sc)[4], float& reference, float& sum, cache_f32x4 (&o)[kD16], cache_bf16x8 (&p)[2], float factor)
+__device__ __forceinline__ void cache_reference(const cache_f32x4 (&sc)[4], CacheState& s, bool& large, cache_f32x4 (&o)[kD16], float factor)
 {
+#pragma clang fp contract(off)   // (a rounded product is meant)
     float larger = -__builtin_inff();
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) larger = fmaxf(larger, sc[t][i]);
     }
-    if (__any((larger - reference) * factor > 8.0f)) {
+    if (__any((larger - s.most) * factor > 8.0f)) {
         // (finite, so that a score of +Inf has an infinite weight and sum: no number in the output, +Inf in lse)
-        larger = fmaxf(larger, reference);
+        larger = fmaxf(larger, s.most);
         larger = fmaxf(larger, __shfl_xor(larger, 16));
         larger = fminf(fmaxf(larger, __shfl_xor(larger, 32)), 0x1.fffffep127f);
-        const float shrink = reference == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((reference - larger) * factor);
-        reference = larger;
-        sum *= shrink;
+        const float fresh = larger == -__builtin_inff() ? 0.0f : larger * factor;
+        const bool was_large = large;
+        large = large || __any(fabsf(fresh) > 0x1p20f);
+        // from what the weights so far are relative to: the rounded product, or (large) the exact one
+        const float moved = was_large ? (s.most - larger) * factor : large ? fmaf(-larger, factor, s.off) : s.off - fresh;
+        const float shrink = s.most == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(moved);
+        s.most = larger;
+        s.off = fresh;
+        s.sum *= shrink;
 #pragma unroll
         for (int d = 0; d < kD16; ++d) o[d] *= shrink;
     }
-    const float base = reference == -__builtin_inff() ? 0.0f : reference;
+}
+// Weights of four tiles of products (16 keys of this lane's query) as the second product's operands.
+__device__ __forceinline__ void cache_powers(const cache_f32x4 (&sc)[4], CacheState& s, bool large, cache_bf16x8 (&p)[2], float factor)
+{
     float w[16];
+    if (large) {
+        const float base = s.most == -__builtin_inff() ? 0.0f : s.most;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) w[i] = __builtin_amdgcn_exp2f((sc[i / 4][i % 4] - base) * factor);
+        for (int i = 0; i < 16; ++i) w[i] = (sc[i / 4][i % 4] - base) * factor;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = fmaf(sc[i / 4][i % 4], factor, -s.off);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w[i] = __builtin_amdgcn_exp2f(w[i]);
     // (the sum from the unrounded weights, pairwise: one rounding of the row's a step)
-    sum += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7])) + (((w[8] + w[9]) + (w[10] + w[11])) + ((w[12] + w[13]) + (w[14] + w[15])));
+    s.sum += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7])) + (((w[8] + w[9]) + (w[10] + w[11])) + ((w[12] + w[13]) + (w[14] + w[15])));
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         uint32_t y[4];
@@ -164,6 +187,17 @@ __device__ __forceinline__ void cache_weights(const cache_f32x4 (&sc)[4], float&
             y[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((cache_f32x2{w[8 * h + 2 * i], w[8 * h + 2 * i + 1]}), cache_bf16x2));
         p[h] = __builtin_bit_cast(cache_bf16x8, make_uint4(y[0], y[1], y[2], y[3]));
     }
+}
+// At the end: relative to the exact product of maximum and factor, whose difference from another wavefront's or part's is then one of maxima.
+template <int kD16>
+__device__ __forceinline__ void cache_exact(CacheState& s, bool large, cache_f32x4 (&o)[kD16], float factor)
+{
+    s.sum += __shfl_xor(s.sum, 16);
+    s.sum += __shfl_xor(s.sum, 32);
+    const float f = large || s.most == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(fmaf(-s.most, factor, s.off));
+    s.sum *= f;
+#pragma unroll
+    for (int d = 0; d < kD16; ++d) o[d] *= f;
 }
 
 // Eight E4M3 bytes times a power of two, in bf16.
@@ -224,8 +258,6 @@ __device__ __forceinline__ uint2 rounded(cache_f32x4 x, float f)
 // kD32: channels / 32, rounded up; kWhole: a row is kD32 whole steps and 16-byte pieces.  kSplit: parts, into the workspace: floats
 // [position][16 kSets][dim], then {maximum, sum} of every row; position = (parts in front) * heads_k + key head.
 //
-// Weights are exp2((s - m) c), c = scale log2 e, m a reference that moves only when a weight would pass 2^8: the difference of two scores is
-// small where its weight is not, however large both are.
 template <int kD32, int kSets, bool kWhole, bool kSplit>
 __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* scales, const int32_t* tables,
                                                                           const int32_t* lens, const int32_t* starts, uint16_t* out, float* lse, CacheStrides sq,
@@ -233,7 +265,7 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
 {
     constexpr uint32_t kRows = 16 * kSets, kPitch = 32 * kD32 + 4;
     __shared__ __align__(16) float meet[kCacheWaves][16][kPitch];
-    __shared__ float2 state[kCacheWaves][16];
+    __shared__ float2 states[kCacheWaves][16];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t r = lane & 15u, g = lane >> 4;
     auto scalar = [](uint32_t x) FB4_INLINE { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
@@ -334,11 +366,11 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
 
     const float factor = s.scale * kCacheLog2E;
     cache_f32x4 o[kSets][2 * kD32];
-    float reference[kSets], sum[kSets];
+    CacheState state[kSets];
+    bool large = false;   // (of the wavefront)
 #pragma unroll
     for (int u = 0; u < kSets; ++u) {
-        reference[u] = -__builtin_inff();
-        sum[u] = 0.0f;
+        state[u] = CacheState{-__builtin_inff(), 0.0f, 0.0f};
 #pragma unroll
         for (int d = 0; d < 2 * kD32; ++d) o[u][d] = cache_f32x4{0, 0, 0, 0};
     }
@@ -386,7 +418,9 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
         // ---- weights
         cache_bf16x8 p[kSets][2];
 #pragma unroll
-        for (int u = 0; u < kSets; ++u) cache_weights(sc[u], reference[u], sum[u], o[u], p[u], factor);
+        for (int u = 0; u < kSets; ++u) cache_reference(sc[u], state[u], large, o[u], factor);
+#pragma unroll
+        for (int u = 0; u < kSets; ++u) cache_powers(sc[u], state[u], large, p[u], factor);
         // ---- O^T
         if (step * kCacheStep + kCacheStep > least) {
             const uint32_t n = rows.len > key ? min(rows.len - key, 16u) : 0u;   // (behind a sequence's end a page may hold anything)
@@ -421,22 +455,21 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
     // ---- the wavefronts meet
 #pragma unroll
     for (int u = 0; u < kSets; ++u) {
-        sum[u] += __shfl_xor(sum[u], 16);
-        sum[u] += __shfl_xor(sum[u], 32);
+        cache_exact(state[u], large, o[u], factor);
 #pragma unroll
         for (int d = 0; d < 2 * kD32; ++d) *reinterpret_cast<cache_f32x4*>(&meet[wave][r][16 * d + 4 * g]) = o[u][d];
-        if (g == 0) state[wave][r] = make_float2(reference[u], sum[u]);
+        if (g == 0) states[wave][r] = make_float2(state[u].most, state[u].sum);
         __syncthreads();
         const uint32_t row = threadIdx.x >> 4, at_row = 16u * u + row;
         if (at_row < n_rows) {
-            float most = state[0][row].x, w[kCacheWaves], total = 0.0f;
+            float most = states[0][row].x, w[kCacheWaves], total = 0.0f;
 #pragma unroll
-            for (int i = 1; i < (int)kCacheWaves; ++i) most = fmaxf(most, state[i][row].x);
+            for (int i = 1; i < (int)kCacheWaves; ++i) most = fmaxf(most, states[i][row].x);
             const float base = most == -__builtin_inff() ? 0.0f : most;
 #pragma unroll
             for (int i = 0; i < (int)kCacheWaves; ++i) {
-                w[i] = __builtin_amdgcn_exp2f((state[i][row].x - base) * factor);
-                total = fmaf(state[i][row].y, w[i], total);
+                w[i] = __builtin_amdgcn_exp2f((states[i][row].x - base) * factor);
+                total = fmaf(states[i][row].y, w[i], total);
             }
             const uint32_t at = tile * kRows + at_row, token = at / group, head = hk * group + (at - token * group);
             const float inverse = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;   // (a NaN stays; no key: zeros)
@@ -500,9 +533,10 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
         from = (uint32_t)((uint64_t)steps * part / parts);
         to = (uint32_t)((uint64_t)steps * (part + 1u) / parts);
     } else {
-        b = scalar(sequence_of(starts, position, group, kTileRows, s));
+        const uint32_t slot = s.tokens * group / kTileRows + s.batch - 1u - position;   // (of a causal prompt the longest first)
+        b = scalar(sequence_of(starts, slot, group, kTileRows, s));
         rows = rows_of(starts, lens, b, s);
-        tile = position - place_of(rows.first, b, group, kTileRows);
+        tile = slot - place_of(rows.first, b, group, kTileRows);
         if (tile >= tiles_of(rows.n, group, kTileRows)) return;
         to = steps_of(rows.len);
     }
@@ -605,11 +639,11 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
     };
     const float factor = s.scale * kCacheLog2E;
     cache_f32x4 o[kSets][2 * kD32];
-    float reference[kSets], sum[kSets];
+    CacheState state[kSets];
+    bool large = false;   // (of the wavefront)
 #pragma unroll
     for (int u = 0; u < kSets; ++u) {
-        reference[u] = -__builtin_inff();
-        sum[u] = 0.0f;
+        state[u] = CacheState{-__builtin_inff(), 0.0f, 0.0f};
 #pragma unroll
         for (int d = 0; d < 2 * kD32; ++d) o[u][d] = cache_f32x4{0, 0, 0, 0};
     }
@@ -660,7 +694,9 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
             }
             cache_bf16x8 p[kSets][2];
 #pragma unroll
-            for (int u = 0; u < kSets; ++u) cache_weights(sc[u], reference[u], sum[u], o[u], p[u], factor);
+            for (int u = 0; u < kSets; ++u) cache_reference(sc[u], state[u], large, o[u], factor);
+#pragma unroll
+            for (int u = 0; u < kSets; ++u) cache_powers(sc[u], state[u], large, p[u], factor);
 #pragma unroll
             for (int d = 0; d < 2 * kD32; ++d) {
 #pragma unroll
@@ -695,12 +731,11 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
     }
 #pragma unroll
     for (int u = 0; u < kSets; ++u) {
-        sum[u] += __shfl_xor(sum[u], 16);
-        sum[u] += __shfl_xor(sum[u], 32);
+        cache_exact(state[u], large, o[u], factor);
         const uint32_t row = first_row + 16u * u + r;
         if (row >= n_rows) continue;
         const uint32_t at = tile * kTileRows + row, token = at / group, head = hk * group + (at - token * group);
-        const float total = sum[u], inverse = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
+        const float total = state[u].sum, inverse = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
 #pragma unroll
         for (int d = 0; d < 2 * kD32; ++d) {
             const uint32_t c = 16u * d + 4u * g;
@@ -713,8 +748,8 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
             }
         }
         if (g == 0) {
-            const float base = reference[u] == -__builtin_inff() ? 0.0f : reference[u];
-            if (kSplit) reinterpret_cast<float2*>(lse)[(size_t)blockIdx.x * kTileRows + row] = make_float2(reference[u], total);
+            const float base = state[u].most == -__builtin_inff() ? 0.0f : state[u].most;
+            if (kSplit) reinterpret_cast<float2*>(lse)[(size_t)blockIdx.x * kTileRows + row] = make_float2(state[u].most, total);
             else if (lse) lse[(size_t)(rows.first + token) * s.heads + head] = total == 0.0f ? -__builtin_inff() : fmaf(base, s.scale, kCacheLn2 * __builtin_amdgcn_logf(total));
         }
     }

@@ -759,3 +759,22 @@ def test_products_of_many_channels(F, luts, rows, n, cols, block):
     x = randn(g, rows, cols).bfloat16()
     same = F.fb4_matvec(luts, x, codes, meta, block=block)
     assert torch.equal(same, F.fb4_matvec(luts, x, codes, at[shift:shift + meta.numel()].view(meta.shape), block=block))
+
+
+# (whether sums are relative to a rounded or an exact product changes at 2^20 powers of two)
+@pytest.mark.parametrize("n,long", [(1, 700), (3, 4000), (60, 700), (60, 5000)])
+@pytest.mark.parametrize("first,later,scale", [(1.0, 3e4, 1.0), (3e4, 1.0, 1.0), (-3e4, 3e4, 1.0), (3e4, 3e4, 2.0 ** 20), (3e4, -3e4, 2.0 ** 40), (1.0, 1.5, 2.0 ** 18), (1e-3, 1.0, 1e-30)])
+def test_attention_scores_that_rise_by_far(F, n, long, first, later, scale):
+    """Keys of one size and then of another: the maximum moves within a wavefront's walk, between wavefronts and between parts.  Scores are
+    products of few numbers, whose sums are exact in fp32, so that a weight far below its row's largest is nothing in both."""
+    c = Paged(F, 31, [long], 2, 16, 16, scale_spread=1)
+    held = c.tables[0, :-(-long // 16)].long()
+    keys = torch.zeros(held.numel() * 16, 16, device="cuda")
+    keys[:, 0] = torch.where(torch.arange(keys.shape[0], device="cuda") < long // 2, first, later)
+    keys[::7, 0] *= 0.5
+    sizes = torch.ldexp(torch.ones((), device="cuda"), torch.ceil(torch.log2(keys.abs().amax() / 448)).int())
+    c.cache[0, held] = (keys / sizes).to(torch.float8_e4m3fn).view(torch.uint8).view(-1, 1, 256).expand(-1, 2, -1).contiguous()
+    c.scales[0] = int(torch.log2(sizes).item()) + 127
+    q = torch.zeros(4, n, 16, device="cuda", dtype=torch.bfloat16)
+    q[..., 0] = (torch.arange(4 * n, device="cuda").view(4, n) % 5 - 2).bfloat16()
+    check_attention(F, c, q, [n], True, scale=scale)
