@@ -20,6 +20,7 @@ namespace fb4 {
 
 constexpr uint32_t kCacheWaves = 4, kCacheStep = 64;   // keys
 constexpr uint32_t kCacheMaxBatch = 4096;
+constexpr uint32_t kTileRows = 128;   // of the kernel for many queries
 constexpr float kCacheLog2E = 1.44269504088896340736f, kCacheLn2 = 0.69314718055994530942f;
 
 typedef __bf16 cache_bf16x2 __attribute__((ext_vector_type(2)));
@@ -75,22 +76,49 @@ __device__ __forceinline__ uint32_t sequence_of(const int32_t* starts, uint32_t 
     return base + (uint32_t)(63 - __builtin_clzll(yes | 1ull));
 }
 
-// Parts: where tiles are few, the keys of each are shared by several workgroups, of `share` steps at most -- the same for all, so that
-// sequences of unlike lengths get parts by their lengths.  share: all tiles' steps over s.target workgroups.
+// Parts: where tiles are few, the keys of each are shared by several workgroups, of about `share` steps each -- the same for all, so that
+// sequences of unlike lengths get parts by their lengths.  Tiles of few rows: all tiles' steps over s.target workgroups.  Tiles of 128, of which
+// 512 run at a time and take as long one by one: p parts to a tile take ceil(tiles p / 512) rounds of 1 / p of the steps and about six more for
+// their beginning and end; the best p, with at most s.target workgroups.  (Two clips' frame of 1350 queries over 22950 keys, 336 tiles, us: one part 715,
+// two 671, three 505, four 552 to 600; one clip's: two 386, five 315, eight 297.)
 constexpr uint32_t kCacheLeastShare = 2 * kCacheWaves;
 __device__ __forceinline__ uint32_t share_of(const int32_t* starts, const int32_t* lens, uint32_t group, uint32_t tile_rows, const CacheShape& s)
 {
     uint64_t sum = 0;
+    uint32_t tiles = 0;
     for (uint32_t b = threadIdx.x & 63u; b < s.batch; b += 64u) {
         const CacheRows r = rows_of(starts, lens, b, s);
-        sum += (uint64_t)tiles_of(r.n, group, tile_rows) * steps_of(r.len);
+        const uint32_t n = tiles_of(r.n, group, tile_rows);
+        sum += (uint64_t)n * steps_of(r.len);
+        tiles += n;
     }
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-    sum *= s.heads_k;
-    return (uint32_t)max((sum + s.target - 1u) / s.target, (uint64_t)kCacheLeastShare);
+    for (int d = 1; d < 64; d *= 2) {
+        sum += __shfl_xor(sum, d);
+        tiles += __shfl_xor(tiles, d);
+    }
+    if (tile_rows < kTileRows) {
+        sum *= s.heads_k;
+        return (uint32_t)max((sum + s.target - 1u) / s.target, (uint64_t)kCacheLeastShare);
+    }
+    const uint32_t n = max(tiles, 1u) * s.heads_k;
+    const float steps = (float)sum / (float)max(tiles, 1u);
+    float least = 0.0f;
+    uint32_t best = 1;
+    for (uint32_t p = 1; p <= 16u && (p == 1u || (n * p <= s.target && steps >= (float)(p * kCacheLeastShare))); ++p) {
+        const float cost = (float)((n * p + 511u) / 512u) * (steps / (float)p + 6.0f);
+        if (p == 1u || cost < least) {
+            best = p;
+            least = cost;
+        }
+    }
+    return max((uint32_t)ceilf(steps / (float)best), kCacheLeastShare);
 }
-__device__ __forceinline__ uint32_t parts_of(uint32_t len, uint32_t share) { return max((steps_of(len) + share - 1u) / share, 1u); }
+// (of 128 rows to the nearest number: one more than meant is a round more)
+__device__ __forceinline__ uint32_t parts_of(uint32_t len, uint32_t share, uint32_t tile_rows)
+{
+    return max((steps_of(len) + (tile_rows < kTileRows ? share - 1u : share / 2u)) / share, 1u);
+}
 
 // Walks the sequences' tiles times parts, by a wavefront: until position `at` (-> its sequence, and `at` from its first one on), or
 // to sequence `stop` (-> the position of its first one in `at`).  Behind all: batch.
@@ -104,7 +132,7 @@ __device__ __forceinline__ uint32_t walk_parts(const int32_t* starts, const int3
         uint32_t mine = 0;
         if (b < s.batch) {
             const CacheRows r = rows_of(starts, lens, b, s);
-            mine = tiles_of(r.n, group, tile_rows) * parts_of(r.len, share);
+            mine = tiles_of(r.n, group, tile_rows) * parts_of(r.len, share, tile_rows);
         }
         uint32_t sum = mine;
 #pragma unroll
@@ -271,7 +299,7 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
     auto scalar = [](uint32_t x) FB4_INLINE { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
     const uint32_t position = scalar(blockIdx.x / s.heads_k), hk = blockIdx.x - position * s.heads_k, group = scalar((uint32_t)s.heads / s.heads_k);
     // ---- sequence, tile, steps
-    uint32_t b, tile, from = 0, to;
+    uint32_t b, tile, part = 0, parts = 1;
     CacheRows rows;
     if (kSplit) {
         const uint32_t share = scalar(share_of(starts, lens, group, kRows, s));
@@ -279,17 +307,14 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
         b = scalar(walk_parts(starts, lens, group, kRows, share, 0xFFFFFFFFu, at, s));
         if (b >= s.batch) return;
         rows = rows_of(starts, lens, b, s);
-        const uint32_t parts = parts_of(rows.len, share);
+        parts = parts_of(rows.len, share, kRows);
         tile = scalar(at) / parts;
-        const uint32_t part = scalar(at) - tile * parts, steps = steps_of(rows.len);
-        from = (uint32_t)((uint64_t)steps * part / parts);
-        to = (uint32_t)((uint64_t)steps * (part + 1u) / parts);
+        part = scalar(at) - tile * parts;
     } else {
         b = scalar(sequence_of(starts, position, group, kRows, s));
         rows = rows_of(starts, lens, b, s);
         tile = position - place_of(rows.first, b, group, kRows);
         if (tile >= tiles_of(rows.n, group, kRows)) return;
-        to = steps_of(rows.len);
     }
     const uint32_t n_rows = min(rows.n * group - tile * kRows, kRows);
     // ---- this lane's queries (behind the last that one again), and the keys before which each ends
@@ -312,8 +337,8 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
             qf[u][i] = __builtin_bit_cast(cache_bf16x8, w);
         }
     }
-    const uint32_t least = scalar(limit_of(0)), end = scalar(limit_of(n_rows - 1u));
-    to = min(to, steps_of(end));
+    const uint32_t least = scalar(limit_of(0)), steps = steps_of(scalar(limit_of(n_rows - 1u)));
+    const uint32_t from = (uint32_t)((uint64_t)steps * part / parts), to = (uint32_t)((uint64_t)steps * (part + 1u) / parts);
     const uint32_t bits = s.page_bits, in_page = (1u << bits) - 1u, held = (rows.len + in_page) >> bits;   // pages with a key
     const int32_t* table = tables + (size_t)b * s.max_pages;
     const size_t page_bytes = (size_t)dim << bits;
@@ -502,7 +527,6 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
 // for the w-th sixteenth of each two steps ahead and puts it down as bf16 one step ahead, so that the converter's half rate (7 cycles for two
 // elements) is paid once for 128 rows.  Rows of keys lie by tile and operand row, 16 bytes further apart than they are long, channels of
 // values likewise: the 16 rows that a read takes start in different banks.
-constexpr uint32_t kTileRows = 128;
 template <int kD32, bool kWhole, bool kSplit>
 __global__ __launch_bounds__(64 * kCacheWaves) __attribute__((amdgpu_waves_per_eu(2)))
 void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* scales, const int32_t* tables, const int32_t* lens, const int32_t* starts, uint16_t* out,
@@ -519,7 +543,7 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
     const uint32_t r = lane & 15u, g = lane >> 4;
     auto scalar = [](uint32_t x) FB4_INLINE { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
     const uint32_t position = scalar(blockIdx.x / s.heads_k), hk = blockIdx.x - position * s.heads_k, group = scalar((uint32_t)s.heads / s.heads_k);
-    uint32_t b, tile, from = 0, to;
+    uint32_t b, tile, part = 0, parts = 1;
     CacheRows rows;
     if (kSplit) {
         const uint32_t share = scalar(share_of(starts, lens, group, kTileRows, s));
@@ -527,20 +551,17 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
         b = scalar(walk_parts(starts, lens, group, kTileRows, share, 0xFFFFFFFFu, at, s));
         if (b >= s.batch) return;
         rows = rows_of(starts, lens, b, s);
-        const uint32_t parts = parts_of(rows.len, share);
+        parts = parts_of(rows.len, share, kTileRows);
         tile = scalar(at) / parts;
-        const uint32_t part = scalar(at) - tile * parts, steps = steps_of(rows.len);
-        from = (uint32_t)((uint64_t)steps * part / parts);
-        to = (uint32_t)((uint64_t)steps * (part + 1u) / parts);
+        part = scalar(at) - tile * parts;
     } else {
         const uint32_t slot = s.tokens * group / kTileRows + s.batch - 1u - position;   // (of a causal prompt the longest first)
         b = scalar(sequence_of(starts, slot, group, kTileRows, s));
         rows = rows_of(starts, lens, b, s);
         tile = slot - place_of(rows.first, b, group, kTileRows);
         if (tile >= tiles_of(rows.n, group, kTileRows)) return;
-        to = steps_of(rows.len);
     }
-    rows.first = scalar(rows.first), rows.n = scalar(rows.n), rows.len = scalar(rows.len), tile = scalar(tile), from = scalar(from), to = scalar(to);
+    rows.first = scalar(rows.first), rows.n = scalar(rows.n), rows.len = scalar(rows.len), tile = scalar(tile), part = scalar(part), parts = scalar(parts);
     const uint32_t n_rows = min(rows.n * group - tile * kTileRows, kTileRows), first_row = wave * 32u;
     const uint32_t pieces = s.dim8, dim = pieces * 8u;
     cache_bf16x8 qf[kSets][kD32];
@@ -562,8 +583,8 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
         }
     }
     // the keys that all rows of this wavefront see, of the workgroup; the keys that any sees
-    const uint32_t least = scalar(limit_of(min(first_row, n_rows - 1u))), least_of_all = scalar(limit_of(0)), end = scalar(limit_of(n_rows - 1u));
-    to = min(to, steps_of(end));
+    const uint32_t least = scalar(limit_of(min(first_row, n_rows - 1u))), least_of_all = scalar(limit_of(0)), steps = steps_of(scalar(limit_of(n_rows - 1u)));
+    const uint32_t from = scalar((uint32_t)((uint64_t)steps * part / parts)), to = scalar((uint32_t)((uint64_t)steps * (part + 1u) / parts));
     const uint32_t bits = s.page_bits, in_page = (1u << bits) - 1u, held = (rows.len + in_page) >> bits;
     const int32_t* table = tables + (size_t)b * s.max_pages;
     const size_t page_bytes = (size_t)dim << bits;
@@ -575,33 +596,36 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
     };
     // ---- this wavefront's sixteenth of a step, into registers and from there into LDS
     const uint32_t mine = 16u * wave;
-    uint2 kr[kAsksK];
-    uint4 vr[kAsksV];
-    uint32_t k_byte = 0, v_byte = 0;
-    bool there = false;
-    auto ask = [&](uint32_t step, int32_t page) FB4_INLINE {
+    struct Asked {   // two steps' are on their way
+        uint2 k[kAsksK];
+        uint4 v[kAsksV];
+        uint32_t k_byte, v_byte;
+        bool there;
+    };
+    Asked even, odd;
+    auto ask = [&](Asked& w, uint32_t step, int32_t page) FB4_INLINE {
         const uint32_t p = scalar((uint32_t)max(page, 0)), place = (step * kCacheStep + mine) & in_page;
-        there = (int32_t)scalar((uint32_t)page) >= 0;
+        w.there = (int32_t)scalar((uint32_t)page) >= 0;
         const size_t at = (size_t)p * s.heads_k + hk;
         const uint8_t* k = cache + at * page_bytes + place * dim;
         const uint8_t* v = values + at * page_bytes + place;
-        k_byte = scales[at];
-        v_byte = scales[(size_t)s.pages * s.heads_k + at];
+        w.k_byte = scales[at];
+        w.v_byte = scales[(size_t)s.pages * s.heads_k + at];
 #pragma unroll
         for (int i = 0; i < kAsksK; ++i) {
             const uint32_t j = 64u * i + lane;
-            kr[i] = make_uint2(0, 0);
-            if (kWhole || j < 16u * pieces) kr[i] = reinterpret_cast<const uint2*>(k)[j];
+            w.k[i] = make_uint2(0, 0);
+            if (kWhole || j < 16u * pieces) w.k[i] = reinterpret_cast<const uint2*>(k)[j];
         }
 #pragma unroll
         for (int i = 0; i < kAsksV; ++i) {
             const uint32_t c = 64u * i + lane;
-            vr[i] = make_uint4(0, 0, 0, 0);
-            if (c < dim) vr[i] = *reinterpret_cast<const uint4*>(v + ((size_t)c << bits));
+            w.v[i] = make_uint4(0, 0, 0, 0);
+            if (c < dim) w.v[i] = *reinterpret_cast<const uint4*>(v + ((size_t)c << bits));
         }
     };
-    auto put = [&](uint32_t step, uint32_t buffer) FB4_INLINE {
-        const float fk = __builtin_bit_cast(float, k_byte << 23), fv = __builtin_bit_cast(float, v_byte << 23);
+    auto put = [&](Asked& w, uint32_t step, uint32_t buffer) FB4_INLINE {
+        const float fk = __builtin_bit_cast(float, w.k_byte << 23), fv = __builtin_bit_cast(float, w.v_byte << 23);
         uint8_t* to_k = lds + buffer;
         uint8_t* to_v = lds + buffer + kKeys + 2u * mine;
 #pragma unroll
@@ -609,20 +633,20 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
             const uint32_t j = 64u * i + lane, key = kWhole ? j / (4u * kD32) : j / pieces, c = j - key * (kWhole ? 4u * kD32 : pieces);
             // key 4 t + x of sixteenth w: row 4 w + x of tile t
             if (kWhole || j < 16u * pieces)
-                *reinterpret_cast<cache_bf16x8*>(to_k + ((key & ~3u) * 4u + 4u * wave + (key & 3u)) * kPitchK + 16u * c) = cache_decode(kr[i].x, kr[i].y, fk);
+                *reinterpret_cast<cache_bf16x8*>(to_k + ((key & ~3u) * 4u + 4u * wave + (key & 3u)) * kPitchK + 16u * c) = cache_decode(w.k[i].x, w.k[i].y, fk);
         }
         // a page that is not there, what lies behind the end: zeros; and no NaN that a query does not see
         const uint32_t key = step * kCacheStep + mine;
-        uint32_t note = there ? 0u : kNone;
-        if (!there || key + 16u > least_of_all) {
-            const uint32_t n = there && rows.len > key ? min(rows.len - key, 16u) : 0u;
+        uint32_t note = w.there ? 0u : kNone;
+        if (!w.there || key + 16u > least_of_all) {
+            const uint32_t n = w.there && rows.len > key ? min(rows.len - key, 16u) : 0u;
             uint32_t some = 0;
 #pragma unroll
             for (int i = 0; i < kAsksV; ++i) {
-                vr[i] = first_bytes(vr[i], n);
-                const uint4 bad = nans_of(vr[i]);
+                w.v[i] = first_bytes(w.v[i], n);
+                const uint4 bad = nans_of(w.v[i]);
                 some |= bad.x | bad.y | bad.z | bad.w;
-                vr[i] = without(vr[i], bad);
+                w.v[i] = without(w.v[i], bad);
             }
             if (__any(some != 0u)) note |= kNan;
         }
@@ -631,8 +655,8 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
             const uint32_t c = 64u * i + lane;
             if (c < 32u * kD32) {   // (channels past the row: zeros)
                 cache_bf16x8* at = reinterpret_cast<cache_bf16x8*>(to_v + c * kPitchV);
-                at[0] = cache_decode(vr[i].x, vr[i].y, fv);
-                at[1] = cache_decode(vr[i].z, vr[i].w, fv);
+                at[0] = cache_decode(w.v[i].x, w.v[i].y, fv);
+                at[1] = cache_decode(w.v[i].z, w.v[i].w, fv);
             }
         }
         if (lane == 0) notes[buffer != 0u][wave] = note;
@@ -655,14 +679,17 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
         __syncthreads();
     }
     if (from < to) {
-        ask(from, page_of(from * kCacheStep + mine));
-        page = page_of((from + 1u) * kCacheStep + mine);
-        put(from, 0);
-        if (from + 1u < to) ask(from + 1u, page);
-        page = page_of((from + 2u) * kCacheStep + mine);
+        auto at = [&](uint32_t step) FB4_INLINE { return page_of(step * kCacheStep + mine); };
+        ask(even, from, at(from));
+        ask(odd, from + 1u, at(from + 1u));
+        page = at(from + 2u);
+        put(even, from, 0);
+        ask(even, from + 2u, page);
+        page = at(from + 3u);
     }
-    uint32_t buffer = 0, seen_notes = 0;
-    for (uint32_t step = from; step < to; ++step) {
+    uint32_t seen_notes = 0;
+    // step: its operands are in `buffer`; those of the next, in w, go to the other, and those of the one two behind that are asked for
+    auto run_step = [&](uint32_t step, uint32_t buffer, Asked& w) FB4_INLINE {
         __syncthreads();   // this step's operands are there; everyone is done with the other buffer
         const uint8_t* keys = lds + buffer + k_at;
         const uint8_t* vals = lds + buffer + v_at;
@@ -708,14 +735,17 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
             }
             seen_notes |= note;
         }
-        buffer = kBuffer - buffer;
         if (step + 1u < to) {
-            put(step + 1u, buffer);
-            if (step + 2u < to) {
-                ask(step + 2u, page);
-                page = page_of((step + 3u) * kCacheStep + mine);
-            }
+            put(w, step + 1u, kBuffer - buffer);
+            ask(w, step + 3u, page);
+            page = page_of((step + 4u) * kCacheStep + mine);
         }
+    };
+    for (uint32_t step = from; step < to;) {
+        run_step(step, 0, odd);
+        if (++step >= to) break;
+        run_step(step, kBuffer, even);
+        ++step;
     }
     if (__any(seen_notes & kNan)) {
         for (uint32_t step = max(from, least_of_all / kCacheStep); step < to; ++step) {
@@ -773,7 +803,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const float* workspace,
     const uint32_t share = scalar(share_of(starts, lens, group, tile_rows, s));
     uint32_t base = 0;
     walk_parts(starts, lens, group, tile_rows, share, b, base, s);
-    const uint32_t at = (token - rows.first) * group + (head - hk * group), tile = at / tile_rows, parts = parts_of(rows.len, share);
+    const uint32_t at = (token - rows.first) * group + (head - hk * group), tile = at / tile_rows, parts = parts_of(rows.len, share, tile_rows);
     const uint32_t first = (scalar(base) + tile * parts) * s.heads_k + hk;   // of the parts' positions
     const uint32_t n = min(parts, first < n_positions ? (n_positions - first + s.heads_k - 1u) / s.heads_k : 0u);
     const size_t step = (size_t)s.heads_k * tile_rows, from = (size_t)first * tile_rows + (at - tile * tile_rows);

@@ -34,8 +34,9 @@ struct CachePlan {
     int rows16;             // rows of a tile / 16: 8 for the kernel of many queries
     bool split;
     int64_t tiles, positions;
+    int target;             // workgroups that parts make, about
 };
-constexpr int kCacheTarget = 768;
+constexpr int kCacheFew = 768, kCacheTarget = 768, kTilesTarget = 1536;
 
 // Sizes that are served, the tiles' size, and whether the keys are shared among workgroups.
 int plan_attention(int64_t tokens, int heads, int heads_k, int64_t dim, int page, int64_t max_pages, int64_t batch, CachePlan* p)
@@ -48,8 +49,9 @@ int plan_attention(int64_t tokens, int heads, int heads_k, int64_t dim, int page
     const int64_t each = batch ? rows / batch : 0;
     p->rows16 = each > 40 || (tokens - batch) * (heads / heads_k) >= 1024 ? 8 : each > 16 ? 2 : 1;
     p->tiles = rows / (16 * p->rows16) + batch;
-    p->split = p->tiles * heads_k < kCacheTarget && (max_pages << bits) > (int64_t)kCacheLeastShare * kCacheStep;
-    p->positions = p->tiles * heads_k + (p->split ? kCacheTarget : 0);
+    p->target = p->rows16 == 8 ? kTilesTarget : kCacheTarget;
+    p->split = p->tiles * heads_k < kCacheFew && (max_pages << bits) > (int64_t)kCacheLeastShare * kCacheStep;
+    p->positions = p->tiles * heads_k + (p->split ? p->target : 0);
     if (p->positions > (1 << 24) - 1) return FB4_ERR_UNSUPPORTED;
     return FB4_OK;
 }
@@ -175,7 +177,7 @@ int fb4_cache_attention(const void* q, const int64_t* q_strides, int64_t tokens,
         return FB4_ERR_UNSUPPORTED;
     // (no pages: no sequence has a key)
     const CacheShape s = {(uint32_t)tokens, pages ? (uint32_t)max_pages : 0u, (uint32_t)pages, (uint16_t)batch, (uint16_t)heads, (uint16_t)heads_k,
-                          (uint16_t)kCacheTarget, (uint8_t)page_bits_of(page), (uint8_t)(dim / 8), (uint8_t)causal, (uint8_t)p.rows16, scale};
+                          (uint16_t)p.target, (uint8_t)page_bits_of(page), (uint8_t)(dim / 8), (uint8_t)causal, (uint8_t)p.rows16, scale};
     hipStream_t st = static_cast<hipStream_t>(stream);
     float* parts = static_cast<float*>(workspace);
     float* states = p.split ? parts + (size_t)p.positions * (16 * p.rows16) * dim : nullptr;
