@@ -67,6 +67,7 @@ __device__ __forceinline__ uint32_t steps_of(uint32_t len) { return (len + kCach
 __device__ __forceinline__ uint32_t sequence_of(const int32_t* starts, uint32_t slot, uint32_t group, uint32_t tile_rows, const CacheShape& s)
 {
     const uint32_t lane = threadIdx.x & 63u, stride = (s.batch + 63u) / 64u;
+    if (s.batch == 1u) return 0;
     uint32_t b = lane * stride;
     uint64_t yes = __ballot(b < s.batch && place_of(start_of(starts, b < s.batch ? b : 0u, s.tokens), b, group, tile_rows) <= slot);
     const uint32_t base = (uint32_t)(63 - __builtin_clzll(yes | 1ull)) * stride;
@@ -350,8 +351,8 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
     };
     auto page_of = [&](uint32_t key) FB4_INLINE {
         const uint32_t i = key >> bits;
-        const int32_t p = i < held ? table[i] : -1;
-        return (uint32_t)p < s.pages ? p : -1;
+        const int32_t p = s.max_pages ? table[min(i, s.max_pages - 1u)] : -1;   // (not after its length has come)
+        return i < held && (uint32_t)p < s.pages ? p : -1;
     };
     auto find = [&](uint32_t step) FB4_INLINE { return Where{page_of(step * kCacheStep + 16u * (r >> 2)), page_of(step * kCacheStep + 16u * g)}; };
     uint4 kr[4][(kD32 + 1) / 2], vr[2 * kD32];   // four tiles of keys; 16 channels each
@@ -591,8 +592,8 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
     const uint8_t* values = cache + (size_t)s.pages * s.heads_k * page_bytes;
     auto page_of = [&](uint32_t key) FB4_INLINE {   // -1: none
         const uint32_t i = key >> bits;
-        const int32_t p = i < held ? table[i] : -1;
-        return (uint32_t)p < s.pages ? p : -1;
+        const int32_t p = s.max_pages ? table[min(i, s.max_pages - 1u)] : -1;   // (not after its length has come)
+        return i < held && (uint32_t)p < s.pages ? p : -1;
     };
     // ---- this wavefront's sixteenth of a step, into registers and from there into LDS
     const uint32_t mine = 16u * wave;
@@ -785,8 +786,9 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
     }
 }
 
-// The parts of a row meet.  kWaves wavefronts to a row: four where rows are few and parts many.  Half a wavefront takes a part, four channels a
-// lane.
+// The parts of a row meet.  kWaves = 4: four wavefronts to a row, where rows are few and parts many; 1: kJoinRows rows to a wavefront, one after the
+// other, so that finding their parts, a chain of reads, comes once for them.  Half a wavefront takes a part, four channels a lane.
+constexpr uint32_t kJoinRows = 4;
 template <int kWaves>
 __global__ __launch_bounds__(256) void cache_join_kernel(const float* workspace, const float2* states, const int32_t* lens, const int32_t* starts, uint16_t* out,
                                                          float* lse, uint32_t n_positions, CacheStrides so, CacheShape s)
@@ -794,57 +796,81 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const float* workspace,
     __shared__ cache_f32x4 meet[4][32];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     auto scalar = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
-    const uint32_t group = scalar((uint32_t)s.heads / s.heads_k), tile_rows = 16u * s.rows16, dim = s.dim8 * 8u;
-    const uint32_t row = kWaves == 4 ? blockIdx.x : blockIdx.x * 4u + wave;
-    const uint32_t token = scalar(row / s.heads), head = row - token * s.heads, hk = scalar(head / group);
-    const uint32_t b = scalar(sequence_of(starts, token, 0u, 1u, s));
-    const CacheRows rows = rows_of(starts, lens, b, s);
-    if (token < rows.first || token - rows.first >= rows.n) return;   // (a whole workgroup, or a wavefront by itself)
+    const uint32_t group = scalar((uint32_t)s.heads / s.heads_k), tile_rows = 16u * s.rows16, dim = s.dim8 * 8u, n_rows = s.tokens * s.heads;
+    const uint32_t first_row = kWaves == 4 ? blockIdx.x : (blockIdx.x * 4u + wave) * kJoinRows;
     const uint32_t share = scalar(share_of(starts, lens, group, tile_rows, s));
-    uint32_t base = 0;
-    walk_parts(starts, lens, group, tile_rows, share, b, base, s);
-    const uint32_t at = (token - rows.first) * group + (head - hk * group), tile = at / tile_rows, parts = parts_of(rows.len, share, tile_rows);
-    const uint32_t first = (scalar(base) + tile * parts) * s.heads_k + hk;   // of the parts' positions
-    const uint32_t n = min(parts, first < n_positions ? (n_positions - first + s.heads_k - 1u) / s.heads_k : 0u);
-    const size_t step = (size_t)s.heads_k * tile_rows, from = (size_t)first * tile_rows + (at - tile * tile_rows);
     const float factor = s.scale * kCacheLog2E;
-    float most = -__builtin_inff(), sum = 0.0f;
-    for (uint32_t p = lane; p < n; p += 64u) most = fmaxf(most, states[from + p * step].x);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
-    const float reference = most == -__builtin_inff() ? 0.0f : most;
-    for (uint32_t p = lane; p < n; p += 64u) {
-        const float2 st = states[from + p * step];
-        sum = fmaf(st.y, __builtin_amdgcn_exp2f((st.x - reference) * factor), sum);
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
     const uint32_t c = 4u * (lane & 31u);
-    cache_f32x4 o = {0, 0, 0, 0};
-    if (c < dim) {
-#pragma unroll 4
-        for (uint32_t p = (kWaves == 4 ? 2u * wave : 0u) + (lane >> 5); p < n; p += 2u * kWaves) {
-            const float w = __builtin_amdgcn_exp2f((states[from + p * step].x - reference) * factor);
-            const cache_f32x4 x = *reinterpret_cast<const cache_f32x4*>(workspace + (from + p * step) * dim + c);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[j] = fmaf(x[j], w, o[j]);
+    CacheRows rows = {0, 0, 0};
+    uint32_t base = 0, parts = 1;
+    for (uint32_t row = first_row; row < min(first_row + (kWaves == 4 ? 1u : kJoinRows), n_rows); ++row) {
+        const uint32_t token = scalar(row / s.heads), head = row - token * s.heads, hk = scalar(head / group);
+        if (token < rows.first || token - rows.first >= rows.n) {   // (the first row's sequence, and another one's later)
+            const uint32_t b = scalar(sequence_of(starts, token, 0u, 1u, s));
+            rows = rows_of(starts, lens, b, s);
+            if (token < rows.first || token - rows.first >= rows.n) continue;   // (of none; with four wavefronts the whole workgroup)
+            base = 0;
+            walk_parts(starts, lens, group, tile_rows, share, b, base, s);
+            base = scalar(base);
+            parts = scalar(parts_of(rows.len, share, tile_rows));
         }
-    }
+        const uint32_t at = (token - rows.first) * group + (head - hk * group), tile = at / tile_rows;
+        const uint32_t first = (base + tile * parts) * s.heads_k + hk;   // of the parts' positions
+        const uint32_t n = min(parts, first < n_positions ? (n_positions - first + s.heads_k - 1u) / s.heads_k : 0u);
+        const size_t step = (size_t)s.heads_k * tile_rows, from = (size_t)first * tile_rows + (at - tile * tile_rows);
+        // (the first parts' rows are asked for before their maxima are known)
+        const uint32_t p0 = (kWaves == 4 ? 2u * wave : 0u) + (lane >> 5);
+        auto part = [&](uint32_t p) { return *reinterpret_cast<const cache_f32x4*>(workspace + (from + p * step) * dim + c); };
+        cache_f32x4 x[4], o = {0, 0, 0, 0};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] += __shfl_xor(o[j], 32);
-    if (kWaves == 4) {
-        if (lane < 32u) meet[wave][lane] = o;
-        __syncthreads();
-        if (wave > 0 || lane >= 32u) return;
-        for (int i = 1; i < 4; ++i) o += meet[i][lane];
+        for (uint32_t i = 0; i < 4; ++i) {
+            x[i] = cache_f32x4{0, 0, 0, 0};
+            if (c < dim && p0 + 2u * kWaves * i < n) x[i] = part(p0 + 2u * kWaves * i);
+        }
+        float most = -__builtin_inff(), sum = 0.0f;
+        float2 mine = make_float2(-__builtin_inff(), 0.0f);
+        if (lane < n) mine = states[from + lane * step];
+        for (uint32_t p = lane; p < n; p += 64u) most = fmaxf(most, p < 64u ? mine.x : states[from + p * step].x);
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+        const float reference = most == -__builtin_inff() ? 0.0f : most;
+        for (uint32_t p = lane; p < n; p += 64u) {
+            const float2 st = p < 64u ? mine : states[from + p * step];
+            sum = fmaf(st.y, __builtin_amdgcn_exp2f((st.x - reference) * factor), sum);
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+        const float weight = __builtin_amdgcn_exp2f((mine.x - reference) * factor);
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {   // (rows of zeros where there is none)
+            const float w = __shfl(weight, p0 + 2u * kWaves * i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = fmaf(x[i][j], w, o[j]);
+        }
+        if (c < dim) {
+#pragma unroll 4
+            for (uint32_t p = p0 + 8u * kWaves; p < n; p += 2u * kWaves) {
+                const float w = __builtin_amdgcn_exp2f((states[from + p * step].x - reference) * factor);
+                const cache_f32x4 y = part(p);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[j] = fmaf(y[j], w, o[j]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] += __shfl_xor(o[j], 32);
+        if (kWaves == 4) {
+            if (lane < 32u) meet[wave][lane] = o;
+            __syncthreads();
+            if (wave > 0) return;
+            for (int i = 1; i < 4; ++i) o += meet[i][lane & 31u];
+        }
+        const float inverse = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
+        if (c < dim && lane < 32u) {
+            uint16_t* place = out + ((size_t)head * so.head + (size_t)token * so.token) * 8u + c;
+            *reinterpret_cast<uint2*>(place) = rounded(o, inverse);
+        }
+        if (lse && lane == 0) lse[(size_t)token * s.heads + head] = sum == 0.0f ? -__builtin_inff() : fmaf(reference, s.scale, kCacheLn2 * __builtin_amdgcn_logf(sum));
     }
-    if (lane >= 32u) return;
-    const float inverse = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
-    if (c < dim) {
-        uint16_t* place = out + ((size_t)head * so.head + (size_t)token * so.token) * 8u + c;
-        *reinterpret_cast<uint2*>(place) = rounded(o, inverse);
-    }
-    if (lse && lane == 0) lse[(size_t)token * s.heads + head] = sum == 0.0f ? -__builtin_inff() : fmaf(reference, s.scale, kCacheLn2 * __builtin_amdgcn_logf(sum));
 }
 
 #undef FB4_INLINE

@@ -94,8 +94,10 @@ __global__ __launch_bounds__(kStoreThreads) void cache_store_kernel(const uint16
         const uint32_t p = (uint32_t)__builtin_amdgcn_readfirstlane((int)page_at(t0));
         const size_t at_scale = ((size_t)which * s.pages + p) * s.heads_k + head;
         const uint32_t before = min((uint32_t)scales[at_scale], kStoreHighest);
-        // ---- the places' tokens, by the first wavefront
-        if (tid < 64u) {
+        // ---- the places' tokens, by the first wavefront; a token by itself is everyone's
+        const bool alone = t0 + 1u >= s.tokens || page_at(t0 + 1u) != p;
+        const uint32_t place = (uint32_t)slots[t0] & (page - 1u);
+        if (!alone && tid < 64u) {
             owner[tid] = owner[64u + tid] = -1;
             for (uint32_t at = t0; at < s.tokens; at += 64u) {
                 const uint32_t t = min(at + lane, s.tokens - 1u), slot = (uint32_t)slots[t];
@@ -105,14 +107,19 @@ __global__ __launch_bounds__(kStoreThreads) void cache_store_kernel(const uint16
                 if (run < 64u) break;
             }
         }
-        __syncthreads();
+        if (!alone) __syncthreads();
         // ---- rows, and the largest magnitude
         uint4 w[kRounds][4];
         uint32_t have[kRounds], most = 0;
 #pragma unroll
         for (int i = 0; i < kRounds; ++i) {
-            const int4 from = *reinterpret_cast<const int4*>(owner + 4u * quad[i]);
-            const int32_t t[4] = {from.x, from.y, from.z, from.w};
+            int4 from = make_int4(-1, -1, -1, -1);
+            if (!alone) from = *reinterpret_cast<const int4*>(owner + 4u * quad[i]);
+            int32_t t[4] = {from.x, from.y, from.z, from.w};
+            if (alone && quad[i] == place / 4u) {
+#pragma unroll
+                for (uint32_t a = 0; a < 4; ++a) t[a] = (place & 3u) == a ? (int32_t)t0 : -1;
+            }
             have[i] = 0;
 #pragma unroll
             for (int a = 0; a < 4; ++a) {
@@ -138,7 +145,7 @@ __global__ __launch_bounds__(kStoreThreads) void cache_store_kernel(const uint16
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, d));
         if ((tid & 63u) == 0) largest[tid >> 6] = most;
-        const bool begun = owner[0] >= 0;
+        const bool begun = alone ? place == 0u : owner[0] >= 0;
         __syncthreads();
         most = max(max(largest[0], largest[1]), max(largest[2], largest[3]));
         // (biased exponent, one more from 1.75 + 2^-7 on; less 8)

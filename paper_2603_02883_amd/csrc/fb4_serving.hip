@@ -210,7 +210,7 @@ int fb4_cache_attention(const void* q, const int64_t* q_strides, int64_t tokens,
     if (p.split) {
         const int64_t rows = tokens * heads;   // (below the target's tiles of 64 rows and the batch's)
         const bool few = rows <= 4096;
-        launch(few ? cache_join_kernel<4> : cache_join_kernel<1>, dim3((unsigned)(few ? rows : (rows + 3) / 4)), dim3(256), 0, st, parts,
+        launch(few ? cache_join_kernel<4> : cache_join_kernel<1>, dim3((unsigned)(few ? rows : (rows + 4 * kJoinRows - 1) / (4 * kJoinRows))), dim3(256), 0, st, parts,
                reinterpret_cast<const float2*>(states), lens, starts, static_cast<uint16_t*>(out), lse, (uint32_t)p.positions, so, s);
     }
     return hipGetLastError() == hipSuccess ? FB4_OK : FB4_ERR_HIP;
