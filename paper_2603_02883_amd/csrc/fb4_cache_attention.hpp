@@ -159,13 +159,14 @@ __device__ __forceinline__ uint32_t walk_parts(const int32_t* starts, const int3
 // ------------------------------------------------------------------------------------------------ a step's weights, and bytes
 // What a query's weights are relative to: the largest product so far (-Inf: none), and its rounded product with the factor c = scale log2 e
 // (0: none).  Weights are exp2(S c - off), by one fused multiply-add whose product is exact, so that the rounding of `off` is one factor in all
-// weights and in their sum.  Beyond |off| = 2^20 that factor could itself be no small number, and the wavefront goes on with exp2((S - most) c).
+// weights and in their sum.  Beyond |off| = 2^20 that factor could itself be no small number, and the 16 queries go on with exp2((S - most) c).
 struct CacheState {
     float most, off, sum;
+    bool large;   // (of all 16)
 };
 // Moves it, and what is relative to it, when a weight would pass 2^8.
 template <int kD16>
-__device__ __forceinline__ void cache_reference(const cache_f32x4 (&sc)[4], CacheState& s, bool& large, cache_f32x4 (&o)[kD16], float factor)
+__device__ __forceinline__ void cache_reference(const cache_f32x4 (&sc)[4], CacheState& s, cache_f32x4 (&o)[kD16], float factor)
 {
 #pragma clang fp contract(off)   // (a rounded product is meant)
     float larger = -__builtin_inff();
@@ -180,10 +181,10 @@ __device__ __forceinline__ void cache_reference(const cache_f32x4 (&sc)[4], Cach
         larger = fmaxf(larger, __shfl_xor(larger, 16));
         larger = fminf(fmaxf(larger, __shfl_xor(larger, 32)), 0x1.fffffep127f);
         const float fresh = larger == -__builtin_inff() ? 0.0f : larger * factor;
-        const bool was_large = large;
-        large = large || __any(fabsf(fresh) > 0x1p20f);
+        const bool was_large = s.large;
+        s.large = s.large || __any(fabsf(fresh) > 0x1p20f);
         // from what the weights so far are relative to: the rounded product, or (large) the exact one
-        const float moved = was_large ? (s.most - larger) * factor : large ? fmaf(-larger, factor, s.off) : s.off - fresh;
+        const float moved = was_large ? (s.most - larger) * factor : s.large ? fmaf(-larger, factor, s.off) : s.off - fresh;
         const float shrink = s.most == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(moved);
         s.most = larger;
         s.off = fresh;
@@ -193,10 +194,10 @@ __device__ __forceinline__ void cache_reference(const cache_f32x4 (&sc)[4], Cach
     }
 }
 // Weights of four tiles of products (16 keys of this lane's query) as the second product's operands.
-__device__ __forceinline__ void cache_powers(const cache_f32x4 (&sc)[4], CacheState& s, bool large, cache_bf16x8 (&p)[2], float factor)
+__device__ __forceinline__ void cache_powers(const cache_f32x4 (&sc)[4], CacheState& s, cache_bf16x8 (&p)[2], float factor)
 {
     float w[16];
-    if (large) {
+    if (s.large) {
         const float base = s.most == -__builtin_inff() ? 0.0f : s.most;
 #pragma unroll
         for (int i = 0; i < 16; ++i) w[i] = (sc[i / 4][i % 4] - base) * factor;
@@ -219,11 +220,11 @@ __device__ __forceinline__ void cache_powers(const cache_f32x4 (&sc)[4], CacheSt
 }
 // At the end: relative to the exact product of maximum and factor, whose difference from another wavefront's or part's is then one of maxima.
 template <int kD16>
-__device__ __forceinline__ void cache_exact(CacheState& s, bool large, cache_f32x4 (&o)[kD16], float factor)
+__device__ __forceinline__ void cache_exact(CacheState& s, cache_f32x4 (&o)[kD16], float factor)
 {
     s.sum += __shfl_xor(s.sum, 16);
     s.sum += __shfl_xor(s.sum, 32);
-    const float f = large || s.most == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(fmaf(-s.most, factor, s.off));
+    const float f = s.large || s.most == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(fmaf(-s.most, factor, s.off));
     s.sum *= f;
 #pragma unroll
     for (int d = 0; d < kD16; ++d) o[d] *= f;
@@ -393,10 +394,9 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
     const float factor = s.scale * kCacheLog2E;
     cache_f32x4 o[kSets][2 * kD32];
     CacheState state[kSets];
-    bool large = false;   // (of the wavefront)
 #pragma unroll
     for (int u = 0; u < kSets; ++u) {
-        state[u] = CacheState{-__builtin_inff(), 0.0f, 0.0f};
+        state[u] = CacheState{-__builtin_inff(), 0.0f, 0.0f, false};
 #pragma unroll
         for (int d = 0; d < 2 * kD32; ++d) o[u][d] = cache_f32x4{0, 0, 0, 0};
     }
@@ -444,9 +444,9 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
         // ---- weights
         cache_bf16x8 p[kSets][2];
 #pragma unroll
-        for (int u = 0; u < kSets; ++u) cache_reference(sc[u], state[u], large, o[u], factor);
+        for (int u = 0; u < kSets; ++u) cache_reference(sc[u], state[u], o[u], factor);
 #pragma unroll
-        for (int u = 0; u < kSets; ++u) cache_powers(sc[u], state[u], large, p[u], factor);
+        for (int u = 0; u < kSets; ++u) cache_powers(sc[u], state[u], p[u], factor);
         // ---- O^T
         if (step * kCacheStep + kCacheStep > least) {
             const uint32_t n = rows.len > key ? min(rows.len - key, 16u) : 0u;   // (behind a sequence's end a page may hold anything)
@@ -481,7 +481,7 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
     // ---- the wavefronts meet
 #pragma unroll
     for (int u = 0; u < kSets; ++u) {
-        cache_exact(state[u], large, o[u], factor);
+        cache_exact(state[u], o[u], factor);
 #pragma unroll
         for (int d = 0; d < 2 * kD32; ++d) *reinterpret_cast<cache_f32x4*>(&meet[wave][r][16 * d + 4 * g]) = o[u][d];
         if (g == 0) states[wave][r] = make_float2(state[u].most, state[u].sum);
@@ -665,10 +665,9 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
     const float factor = s.scale * kCacheLog2E;
     cache_f32x4 o[kSets][2 * kD32];
     CacheState state[kSets];
-    bool large = false;   // (of the wavefront)
 #pragma unroll
     for (int u = 0; u < kSets; ++u) {
-        state[u] = CacheState{-__builtin_inff(), 0.0f, 0.0f};
+        state[u] = CacheState{-__builtin_inff(), 0.0f, 0.0f, false};
 #pragma unroll
         for (int d = 0; d < 2 * kD32; ++d) o[u][d] = cache_f32x4{0, 0, 0, 0};
     }
@@ -722,9 +721,9 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
             }
             cache_bf16x8 p[kSets][2];
 #pragma unroll
-            for (int u = 0; u < kSets; ++u) cache_reference(sc[u], state[u], large, o[u], factor);
+            for (int u = 0; u < kSets; ++u) cache_reference(sc[u], state[u], o[u], factor);
 #pragma unroll
-            for (int u = 0; u < kSets; ++u) cache_powers(sc[u], state[u], large, p[u], factor);
+            for (int u = 0; u < kSets; ++u) cache_powers(sc[u], state[u], p[u], factor);
 #pragma unroll
             for (int d = 0; d < 2 * kD32; ++d) {
 #pragma unroll
@@ -762,7 +761,7 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
     }
 #pragma unroll
     for (int u = 0; u < kSets; ++u) {
-        cache_exact(state[u], large, o[u], factor);
+        cache_exact(state[u], o[u], factor);
         const uint32_t row = first_row + 16u * u + r;
         if (row >= n_rows) continue;
         const uint32_t at = tile * kTileRows + row, token = at / group, head = hk * group + (at - token * group);

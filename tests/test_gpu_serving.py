@@ -778,3 +778,92 @@ def test_attention_scores_that_rise_by_far(F, n, long, first, later, scale):
     q = torch.zeros(4, n, 16, device="cuda", dtype=torch.bfloat16)
     q[..., 0] = (torch.arange(4 * n, device="cuda").view(4, n) % 5 - 2).bfloat16()
     check_attention(F, c, q, [n], True, scale=scale)
+
+
+@pytest.mark.parametrize("n,group", [(32, 1), (100, 1), (10, 3)])
+def test_attention_rows_of_far_larger_scores_beside_others(F, n, group):
+    """Sixteen rows' scores pass 2^20 powers of two half way; their neighbours' weights stay what they are, with a maximum whose product
+    with the scale does not fit fp32."""
+    long, dim = 1400, 16
+    c = Paged(F, 37, [long], 1, dim, 16, scale_spread=1)
+    held = c.tables[0, :-(-long // 16)].long()
+    keys = torch.zeros(held.numel() * 16, dim, device="cuda")
+    at = torch.arange(keys.shape[0], device="cuda")
+    keys[:, 0] = torch.where(at < long // 2, 2.0 ** -5, 448.0)
+    keys[:, 1] = 416.0
+    c.cache[0, held] = keys.to(torch.float8_e4m3fn).view(torch.uint8).view(-1, 1, 16 * dim)
+    c.scales[0] = 127
+    q = torch.zeros(group, n, dim, device="cuda", dtype=torch.bfloat16)
+    # (token by token, the heads of a key head side by side: sixteen rows after sixteen)
+    second = (torch.arange(n, device="cuda") * group + torch.arange(group, device="cuda").unsqueeze(1)) // 16 % 2 == 1
+    q[..., 0], q[..., 1] = torch.where(second, 0.0, 4096.0).bfloat16(), torch.where(second, 1237.0, 0.0).bfloat16()
+    check_attention(F, c, q, [n], True, scale=0.7)
+    out, lse = check_attention(F, c, q, [n], False, scale=1.0)
+    q[~second] = 0
+    alone, lse_alone = check_attention(F, c, q, [n], False, scale=1.0)
+    assert torch.equal(out[second.T], alone[second.T]) and torch.equal(lse[second.T], lse_alone[second.T])
+
+
+@pytest.mark.parametrize("long,n", [(150, 3), (150, 8), (2000, 3), (2000, 20)])
+def test_attention_nan_values_in_tiles_of_few_rows(F, long, n):
+    """As above for tiles of 16 and 32 rows: a NaN among the last keys, seen by some of the queries."""
+    for place in (long - 2, long - n, long - n - 1):
+        c = Paged(F, 41, [long], 2, 64, 32)
+        c.cache[1, int(c.tables[0, place // 32])].view(2, 64, 32)[1, 5, place % 32] = 0x7F
+        q = randn(gen(42), 4, n, 64).bfloat16()
+        check_nan_rows(F, c, q, n, long, place, 1)
+
+
+def test_attention_pages_that_are_none_beside_nan(F):
+    """A missing page's keys are skipped; a NaN in the same 64 keys is seen by those who see its key."""
+    for n in (3, 40):
+        c = Paged(F, 43, [600], 1, 64, 16)
+        c.tables[0, 5] = -1
+        c.cache[1, int(c.tables[0, 6])].view(64, 16)[7, 3] = 0xFF
+        q = randn(gen(44), 2, n, 64).bfloat16()
+        check_attention(F, c, q, [n], True)
+        out = F.fb4_cache_attention(q, c.cache, c.scales, c.tables, c.lens, ints([0, n]), 16)
+        assert out[:, :, 7].isnan().all() and out.isnan().sum() == 2 * n
+
+
+def test_prompts_and_single_tokens_in_one_call(F):
+    """What a server sends: sequences at their prompts beside others a token further, some idle, rows left over."""
+    lens = [900, 1, 4000, 300, 77, 0, 2500, 640]
+    counts = [900, 1, 1, 120, 1, 0, 333, 1]
+    for heads, heads_k, dim, page in ((24, 8, 128, 64), (16, 16, 72, 16), (4, 2, 40, 128)):
+        c = Paged(F, 45, lens, heads_k, dim, page)
+        q = randn(gen(46), heads, sum(counts) + 9, dim).bfloat16()
+        check_attention(F, c, q, counts, True, first=4)
+        check_attention(F, c, q, counts, False, first=4)
+
+
+def test_plans_without_positions_and_many_sequences(F):
+    r = random.Random(3)
+    lens = [r.randint(0, 200) for _ in range(1500)]
+    adds = [r.choice([1, 0, 17, 40, -3, -500]) for _ in range(1500)]
+    ids = list(range(1500 * 16))
+    tables = [[ids.pop() if p * 16 < lens[b] else -1 for p in range(16)] for b in range(1500)]
+    want = check_plan(F, lens, adds, tables, ids, len(ids), 16, sum(max(a, 0) for a in adds))
+    t = [ints(x) for x in (lens, adds, tables, ids, [len(ids)])]
+    tokens = len(want["slots"])
+    out = [torch.empty(n, dtype=torch.int32, device="cuda") for n in (1500, 1, 1501, tokens)]
+    import ctypes
+    P = lambda x: ctypes.c_void_p(x.data_ptr())
+    rc = F.binding.lib().fb4_cache_plan(P(t[0]), P(t[1]), 1500, 16, P(t[2]), 16, P(t[3]), len(ids), P(t[4]), P(out[0]), P(out[1]), P(out[2]), P(out[3]), None, tokens,
+                                        torch.cuda.current_stream().cuda_stream)
+    assert rc == F.OK and [x.cpu().tolist() for x in out] == [want["lens"], want["count"], want["starts"], want["slots"]]
+
+
+def test_two_calls_at_once_on_two_streams(F):
+    """Each with its own workspace: the results are those of one after the other."""
+    c, d = Paged(F, 47, [5000, 300], 2, 64, 64), Paged(F, 48, [7000, 3000], 2, 64, 64)
+    q = randn(gen(49), 4, 2, 64).bfloat16()
+    starts = ints([0, 1, 2])
+    want = [F.fb4_cache_attention(q, x.cache, x.scales, x.tables, x.lens, starts, 64) for x in (c, d)]
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(20):
+        got += [F.fb4_cache_attention(q, x.cache, x.scales, x.tables, x.lens, starts, 64, stream=s) for x, s in ((c, a), (d, b))]
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want[i % 2]) for i, g in enumerate(got))
