@@ -33,10 +33,11 @@ struct CacheStrides {
 };
 struct CacheShape {
     uint32_t tokens, max_pages, pages;
-    uint16_t batch, heads, heads_k, target;   // target: workgroups that the keys are shared among, where parts are made
-    uint8_t page_bits, dim8;                  // dim / 8
-    uint8_t causal, rows16;                   // rows of a tile / 16
+    uint16_t batch, heads, heads_k;
+    uint8_t page_bits, row;   // row: dim / 8, and 128 if causal
     float scale;
+    __host__ __device__ uint32_t dim8() const { return row & 127u; }
+    __host__ __device__ bool causal() const { return row > 127u; }
 };
 
 #define FB4_INLINE __attribute__((always_inline))
@@ -78,11 +79,26 @@ __device__ __forceinline__ uint32_t sequence_of(const int32_t* starts, uint32_t 
 }
 
 // Parts: where tiles are few, the keys of each are shared by several workgroups, of about `share` steps each -- the same for all, so that
-// sequences of unlike lengths get parts by their lengths.  Tiles of few rows: all tiles' steps over s.target workgroups.  Tiles of 128, of which
-// 512 run at a time and take as long one by one: p parts to a tile take ceil(tiles p / 512) rounds of 1 / p of the steps and about six more for
-// their beginning and end; the best p, with at most s.target workgroups.  (Two clips' frame of 1350 queries over 22950 keys, 336 tiles, us: one part 715,
-// two 671, three 505, four 552 to 600; one clip's: two 386, five 315, eight 297.)
-constexpr uint32_t kCacheLeastShare = 2 * kCacheWaves;
+// sequences of unlike lengths get parts by their lengths.  Tiles of few rows: all tiles' steps over kCacheTarget workgroups (512, 768 and
+// 1024, a token each, us: 32 sequences of 8192 keys at most 99, 88, 96; 16: 52, 47, 48; one of 65536: 30.5, 38, 36).  Tiles of 128: the best number of parts by the times below.  A tile of one part writes its rows itself.
+constexpr uint32_t kCacheLeastShare = 2 * kCacheWaves, kCacheTarget = 768, kTilesTarget = 1536;
+// Parts of each of n tiles of `steps` steps.  512 tiles run at a time, two to a compute unit, and steps take 1.2 times as long then as one by one
+// (1.65 and 2 us of 128 channels); a tile's beginning and end take as long as six; parts, their joining twelve and one more per 256 parts.
+// (24 heads of 128 channels, 128 tokens over 1024 keys: one part 34.9, two 36.8; over 2048: 63.5, four 39.0.  16 heads of 72 channels, 1350 tokens
+// over 2048: one 55, two 61; over 4096: 104, 85; 3500 tokens over 12000: one 373, two 408; 5000: 648, 552.)
+__host__ __device__ inline uint32_t tile_parts(uint32_t n, float steps)
+{
+    float least = 0.0f;
+    uint32_t best = 1;
+    for (uint32_t p = 1; p <= 16u && (p == 1u || (n * p <= kTilesTarget && steps >= (float)(p * kCacheLeastShare))); ++p) {
+        const float cost = (float)((n * p + 511u) / 512u) * (steps / (float)p + 6.0f) * (n * p > 256u ? 1.2f : 1.0f) + (p > 1u ? 12.0f + (float)(n * p) / 256.0f : 0.0f);
+        if (p == 1u || cost < least) {
+            best = p;
+            least = cost;
+        }
+    }
+    return best;
+}
 __device__ __forceinline__ uint32_t share_of(const int32_t* starts, const int32_t* lens, uint32_t group, uint32_t tile_rows, const CacheShape& s)
 {
     uint64_t sum = 0;
@@ -99,21 +115,10 @@ __device__ __forceinline__ uint32_t share_of(const int32_t* starts, const int32_
         tiles += __shfl_xor(tiles, d);
     }
     if (tile_rows < kTileRows) {
-        sum *= s.heads_k;
-        return (uint32_t)max((sum + s.target - 1u) / s.target, (uint64_t)kCacheLeastShare);
+        return (uint32_t)max((sum * s.heads_k + kCacheTarget - 1u) / kCacheTarget, (uint64_t)kCacheLeastShare);
     }
-    const uint32_t n = max(tiles, 1u) * s.heads_k;
     const float steps = (float)sum / (float)max(tiles, 1u);
-    float least = 0.0f;
-    uint32_t best = 1;
-    for (uint32_t p = 1; p <= 16u && (p == 1u || (n * p <= s.target && steps >= (float)(p * kCacheLeastShare))); ++p) {
-        const float cost = (float)((n * p + 511u) / 512u) * (steps / (float)p + 6.0f);
-        if (p == 1u || cost < least) {
-            best = p;
-            least = cost;
-        }
-    }
-    return max((uint32_t)ceilf(steps / (float)best), kCacheLeastShare);
+    return max((uint32_t)ceilf(steps / (float)tile_parts(max(tiles, 1u) * s.heads_k, steps)), kCacheLeastShare);
 }
 // (of 128 rows to the nearest number: one more than meant is a round more)
 __device__ __forceinline__ uint32_t parts_of(uint32_t len, uint32_t share, uint32_t tile_rows)
@@ -284,16 +289,20 @@ __device__ __forceinline__ uint2 rounded(cache_f32x4 x, float f)
     return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
 }
 
+// The workspace's rows' {maximum, sum}, behind all its rows.
+__device__ __forceinline__ float2* states_of(float* workspace, uint32_t rows, uint32_t dim) { return reinterpret_cast<float2*>(workspace + (size_t)gridDim.x * rows * dim); }
+
 // ------------------------------------------------------------------------------------------------ attention
 // kD32: channels / 32, rounded up; kWhole: a row is kD32 whole steps and 16-byte pieces.  kSplit: parts, into the workspace: floats
 // [position][16 kSets][dim], then {maximum, sum} of every row; position = (parts in front) * heads_k + key head.
 //
-template <int kD32, int kSets, bool kWhole, bool kSplit>
-__global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* scales, const int32_t* tables,
-                                                                          const int32_t* lens, const int32_t* starts, uint16_t* out, float* lse, CacheStrides sq,
-                                                                          CacheStrides so, CacheShape s)
+template <int kD32, bool kWhole, bool kSplit>
+__global__ __launch_bounds__(64 * kCacheWaves) __attribute__((amdgpu_waves_per_eu(2))) void cache_attention_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* scales, const int32_t* tables,
+                                                                          const int32_t* lens, const int32_t* starts, uint16_t* out, float* lse, float* workspace,
+                                                                          CacheStrides sq, CacheStrides so, CacheShape s)
 {
-    constexpr uint32_t kRows = 16 * kSets, kPitch = 32 * kD32 + 4;
+    constexpr int kSets = 1;
+    constexpr uint32_t kRows = 16, kPitch = 32 * kD32 + 4;
     __shared__ __align__(16) float meet[kCacheWaves][16][kPitch];
     __shared__ float2 states[kCacheWaves][16];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -320,12 +329,12 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
     }
     const uint32_t n_rows = min(rows.n * group - tile * kRows, kRows);
     // ---- this lane's queries (behind the last that one again), and the keys before which each ends
-    const uint32_t pieces = s.dim8, dim = pieces * 8u;
+    const uint32_t pieces = s.dim8(), dim = pieces * 8u;
     cache_bf16x8 qf[kSets][kD32];
     uint32_t limit[kSets];
     auto limit_of = [&](uint32_t row) FB4_INLINE {
         const uint32_t token = (tile * kRows + row) / group;
-        return s.causal ? (uint32_t)max((int64_t)rows.len - (int64_t)rows.n + (int64_t)token + 1, (int64_t)0) : rows.len;
+        return s.causal() ? (uint32_t)max((int64_t)rows.len - (int64_t)rows.n + (int64_t)token + 1, (int64_t)0) : rows.len;
     };
 #pragma unroll
     for (int u = 0; u < kSets; ++u) {
@@ -507,15 +516,15 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
 #pragma unroll
                     for (int j = 0; j < 4; ++j) x[j] = fmaf(y[j], w[i], x[j]);
                 }
-                if (kSplit) {
-                    *reinterpret_cast<cache_f32x4*>(reinterpret_cast<float*>(out) + ((size_t)blockIdx.x * kRows + at_row) * dim + c) = x;
+                if (kSplit && parts > 1u) {
+                    *reinterpret_cast<cache_f32x4*>(workspace + ((size_t)blockIdx.x * kRows + at_row) * dim + c) = x;
                 } else {
                     uint16_t* place = out + ((size_t)head * so.head + (size_t)(rows.first + token) * so.token) * 8u + c;
                     *reinterpret_cast<uint2*>(place) = rounded(x, inverse);
                 }
             }
             if ((threadIdx.x & 15u) == 0) {
-                if (kSplit) reinterpret_cast<float2*>(lse)[(size_t)blockIdx.x * kRows + at_row] = make_float2(most, total);
+                if (kSplit && parts > 1u) states_of(workspace, kRows, dim)[(size_t)blockIdx.x * kRows + at_row] = make_float2(most, total);
                 else if (lse) lse[(size_t)(rows.first + token) * s.heads + head] = total == 0.0f ? -__builtin_inff() : fmaf(base, s.scale, kCacheLn2 * __builtin_amdgcn_logf(total));
             }
         }
@@ -531,7 +540,7 @@ __global__ __launch_bounds__(64 * kCacheWaves) void cache_attention_kernel(const
 template <int kD32, bool kWhole, bool kSplit>
 __global__ __launch_bounds__(64 * kCacheWaves) __attribute__((amdgpu_waves_per_eu(2)))
 void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* scales, const int32_t* tables, const int32_t* lens, const int32_t* starts, uint16_t* out,
-                        float* lse, CacheStrides sq, CacheStrides so, CacheShape s)
+                        float* lse, float* workspace, CacheStrides sq, CacheStrides so, CacheShape s)
 {
     constexpr int kSets = 2;
     constexpr uint32_t kPitchK = 64 * kD32 + 16, kPitchV = 2 * kCacheStep + 16;
@@ -564,12 +573,12 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
     }
     rows.first = scalar(rows.first), rows.n = scalar(rows.n), rows.len = scalar(rows.len), tile = scalar(tile), part = scalar(part), parts = scalar(parts);
     const uint32_t n_rows = min(rows.n * group - tile * kTileRows, kTileRows), first_row = wave * 32u;
-    const uint32_t pieces = s.dim8, dim = pieces * 8u;
+    const uint32_t pieces = s.dim8(), dim = pieces * 8u;
     cache_bf16x8 qf[kSets][kD32];
     uint32_t limit[kSets];
     auto limit_of = [&](uint32_t row) FB4_INLINE {
         const uint32_t token = (tile * kTileRows + row) / group;
-        return s.causal ? (uint32_t)max((int64_t)rows.len - (int64_t)rows.n + (int64_t)token + 1, (int64_t)0) : rows.len;
+        return s.causal() ? (uint32_t)max((int64_t)rows.len - (int64_t)rows.n + (int64_t)token + 1, (int64_t)0) : rows.len;
     };
 #pragma unroll
     for (int u = 0; u < kSets; ++u) {
@@ -770,8 +779,8 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
         for (int d = 0; d < 2 * kD32; ++d) {
             const uint32_t c = 16u * d + 4u * g;
             if (!kWhole && c >= dim) continue;
-            if (kSplit) {
-                *reinterpret_cast<cache_f32x4*>(reinterpret_cast<float*>(out) + ((size_t)blockIdx.x * kTileRows + row) * dim + c) = o[u][d];
+            if (kSplit && parts > 1u) {
+                *reinterpret_cast<cache_f32x4*>(workspace + ((size_t)blockIdx.x * kTileRows + row) * dim + c) = o[u][d];
             } else {
                 uint16_t* place = out + ((size_t)head * so.head + (size_t)(rows.first + token) * so.token) * 8u + c;
                 *reinterpret_cast<uint2*>(place) = rounded(o[u][d], inverse);
@@ -779,7 +788,7 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
         }
         if (g == 0) {
             const float base = state[u].most == -__builtin_inff() ? 0.0f : state[u].most;
-            if (kSplit) reinterpret_cast<float2*>(lse)[(size_t)blockIdx.x * kTileRows + row] = make_float2(state[u].most, total);
+            if (kSplit && parts > 1u) states_of(workspace, kTileRows, dim)[(size_t)blockIdx.x * kTileRows + row] = make_float2(state[u].most, total);
             else if (lse) lse[(size_t)(rows.first + token) * s.heads + head] = total == 0.0f ? -__builtin_inff() : fmaf(base, s.scale, kCacheLn2 * __builtin_amdgcn_logf(total));
         }
     }
@@ -787,38 +796,39 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
 
 // The parts of a row meet.  kWaves = 4: four wavefronts to a row, where rows are few and parts many; 1: kJoinRows rows to a wavefront, one after the
 // other, so that finding their parts, a chain of reads, comes once for them.  Half a wavefront takes a part, four channels a lane.
-constexpr uint32_t kJoinRows = 4;
+constexpr uint32_t kJoinRows = 4, kJoinWaves = 4, kJoinFew = 1024;
 template <int kWaves>
-__global__ __launch_bounds__(256) void cache_join_kernel(const float* workspace, const float2* states, const int32_t* lens, const int32_t* starts, uint16_t* out,
-                                                         float* lse, uint32_t n_positions, CacheStrides so, CacheShape s)
+__global__ __launch_bounds__(64 * (kWaves > 4 ? kWaves : 4)) void cache_join_kernel(const float* workspace, const float2* states, const int32_t* lens, const int32_t* starts, uint16_t* out,
+                                                         float* lse, uint32_t n_positions, uint32_t tile_rows, CacheStrides so, CacheShape s)
 {
-    __shared__ cache_f32x4 meet[4][32];
+    __shared__ cache_f32x4 meet[kWaves][32];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     auto scalar = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
-    const uint32_t group = scalar((uint32_t)s.heads / s.heads_k), tile_rows = 16u * s.rows16, dim = s.dim8 * 8u, n_rows = s.tokens * s.heads;
-    const uint32_t first_row = kWaves == 4 ? blockIdx.x : (blockIdx.x * 4u + wave) * kJoinRows;
+    const uint32_t group = scalar((uint32_t)s.heads / s.heads_k), dim = s.dim8() * 8u, n_rows = s.tokens * s.heads;
+    const uint32_t first_row = kWaves > 1 ? blockIdx.x : (blockIdx.x * 4u + wave) * kJoinRows;
     const uint32_t share = scalar(share_of(starts, lens, group, tile_rows, s));
     const float factor = s.scale * kCacheLog2E;
     const uint32_t c = 4u * (lane & 31u);
     CacheRows rows = {0, 0, 0};
     uint32_t base = 0, parts = 1;
-    for (uint32_t row = first_row; row < min(first_row + (kWaves == 4 ? 1u : kJoinRows), n_rows); ++row) {
+    for (uint32_t row = first_row; row < min(first_row + (kWaves > 1 ? 1u : kJoinRows), n_rows); ++row) {
         const uint32_t token = scalar(row / s.heads), head = row - token * s.heads, hk = scalar(head / group);
         if (token < rows.first || token - rows.first >= rows.n) {   // (the first row's sequence, and another one's later)
             const uint32_t b = scalar(sequence_of(starts, token, 0u, 1u, s));
             rows = rows_of(starts, lens, b, s);
-            if (token < rows.first || token - rows.first >= rows.n) continue;   // (of none; with four wavefronts the whole workgroup)
+            if (token < rows.first || token - rows.first >= rows.n) continue;   // (of none; with several wavefronts the whole workgroup)
             base = 0;
             walk_parts(starts, lens, group, tile_rows, share, b, base, s);
             base = scalar(base);
             parts = scalar(parts_of(rows.len, share, tile_rows));
         }
+        if (parts == 1u) continue;   // (written already)
         const uint32_t at = (token - rows.first) * group + (head - hk * group), tile = at / tile_rows;
         const uint32_t first = (base + tile * parts) * s.heads_k + hk;   // of the parts' positions
         const uint32_t n = min(parts, first < n_positions ? (n_positions - first + s.heads_k - 1u) / s.heads_k : 0u);
         const size_t step = (size_t)s.heads_k * tile_rows, from = (size_t)first * tile_rows + (at - tile * tile_rows);
         // (the first parts' rows are asked for before their maxima are known)
-        const uint32_t p0 = (kWaves == 4 ? 2u * wave : 0u) + (lane >> 5);
+        const uint32_t p0 = (kWaves > 1 ? 2u * wave : 0u) + (lane >> 5);
         auto part = [&](uint32_t p) { return *reinterpret_cast<const cache_f32x4*>(workspace + (from + p * step) * dim + c); };
         cache_f32x4 x[4], o = {0, 0, 0, 0};
 #pragma unroll
@@ -857,11 +867,11 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const float* workspace,
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[j] += __shfl_xor(o[j], 32);
-        if (kWaves == 4) {
+        if (kWaves > 1) {
             if (lane < 32u) meet[wave][lane] = o;
             __syncthreads();
             if (wave > 0) return;
-            for (int i = 1; i < 4; ++i) o += meet[i][lane & 31u];
+            for (int i = 1; i < kWaves; ++i) o += meet[i][lane & 31u];
         }
         const float inverse = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
         if (c < dim && lane < 32u) {

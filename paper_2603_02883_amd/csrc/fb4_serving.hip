@@ -31,12 +31,13 @@ int strides_of(const int64_t* strides, T* out)
 }
 
 struct CachePlan {
-    int rows16;             // rows of a tile / 16: 8 for the kernel of many queries
+    uint32_t tile_rows;
     bool split;
-    int64_t tiles, positions;
-    int target;             // workgroups that parts make, about
+    int64_t positions;
 };
-constexpr int kCacheFew = 768, kCacheTarget = 768, kTilesTarget = 1536;
+// Tiles of few rows from which on a workgroup takes all keys of one, and keys up to which it does.  (A token each of sequences of up to 8192
+// keys, 24 heads over 8, us, whole and in parts: 40 sequences 112, 105; 48 121, 124; 64 149, 160.  One sequence: 1024 keys 12.0, 14.9; 1536 16.5, 14.9.)
+constexpr int kCacheFew = 384, kCacheShort = 1024;
 
 // Sizes that are served, the tiles' size, and whether the keys are shared among workgroups.
 int plan_attention(int64_t tokens, int heads, int heads_k, int64_t dim, int page, int64_t max_pages, int64_t batch, CachePlan* p)
@@ -46,12 +47,15 @@ int plan_attention(int64_t tokens, int heads, int heads_k, int64_t dim, int page
     if (bits < 0 || heads > 65535 || dim % 8 || dim > 128 || tokens > kMaxInt || max_pages > kMaxInt >> bits || batch > kCacheMaxBatch) return FB4_ERR_UNSUPPORTED;
     const int64_t rows = tokens * (heads / heads_k);
     if (rows > kMaxInt) return FB4_ERR_UNSUPPORTED;
-    const int64_t each = batch ? rows / batch : 0;
-    p->rows16 = each > 40 || (tokens - batch) * (heads / heads_k) >= 1024 ? 8 : each > 16 ? 2 : 1;
-    p->tiles = rows / (16 * p->rows16) + batch;
-    p->target = p->rows16 == 8 ? kTilesTarget : kCacheTarget;
-    p->split = p->tiles * heads_k < kCacheFew && (max_pages << bits) > (int64_t)kCacheLeastShare * kCacheStep;
-    p->positions = p->tiles * heads_k + (p->split ? p->target : 0);
+    // 16 rows to a workgroup, or 128: by the rows of a sequence on average, as both cost alike from 40 to 64 on -- 64 sequences of up to 4096 keys, 24
+    // heads over 8, us: 24 rows 121, 149; 39 145, 170; 48 173, 172; 66 209, 179; 192 458, 329; 8 sequences, 16 heads of 72 channels: 32 45, 52; 40 45, 46; 64
+    // 52, 48 -- and where the rows beyond a token each are a long prompt's, which 16 at a time take twice as long, among many sequences of few or none.
+    const bool many = rows > 40 * batch || rows >= 16384 + batch * (heads / heads_k);
+    p->tile_rows = many ? kTileRows : 16;
+    // (at least so many tiles have rows)
+    const int64_t tiles = std::max((rows + p->tile_rows - 1) / p->tile_rows, batch) * heads_k, keys = max_pages << bits;
+    p->split = many ? tiles <= (int64_t)kTilesTarget && tile_parts((uint32_t)tiles, (float)((keys + kCacheStep - 1) / kCacheStep)) > 1 : tiles < kCacheFew && keys > kCacheShort;
+    p->positions = (rows / p->tile_rows + batch) * heads_k + (p->split ? many ? kTilesTarget : kCacheTarget : 0);
     if (p->positions > (1 << 24) - 1) return FB4_ERR_UNSUPPORTED;
     return FB4_OK;
 }
@@ -75,9 +79,11 @@ int fb4_matvec(const fb4_luts* luts, const void* x, int64_t rows, int64_t x_row_
     if (int rc = check_device(luts)) return rc;
     const int sets = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     const int64_t chunks = cols / 32;
-    // Rows of the weights to a workgroup, 16 to a tile: as many as leave every compute unit a workgroup, since each reads all of x (16 rows,
-    // 16384 x 4096: 14.5 us with four tiles, 15.1 with two, 21 with one; 37 rows, 4610 x 1184: two 8.2, one 8.8; one row, 6912 x 1152: one 4.35, two 4.40)
-    const int tiles = sets == 4 ? (n >= 4096 ? 2 : 1) : n >= 16384 ? 4 : n >= 8192 ? 2 : 1;
+    // Rows of the weights to a workgroup, 16 to a tile: each reads all of x, so the more rows x has the fewer workgroups, down to one or two per
+    // compute unit.  (4096 channels, one, two and four tiles, us.  One row: 8192 rows of weights 6.9, 7.6, 11.5; 16384: 12.0, 11.0, 12.2; 49152 x
+    // 8192: 53.6, 47.3, 43.4.  Four: 12288: 10.4, 11.2, 12.0.  Eight: 5120: 8.7, 7.5, 11.3; 24576: 22.2, 17.7, 19.6.  Sixteen: 8192: 11.6, 9.6,
+    // 13.2; 12288: 16.1, 14.5, 13.4; 16384: 21.2, 15.0, 14.2.  Thirty-two: 12288: 27.0, 25.3, 18.3.  Sixty-four, one and two: 4096: 19.0, 21.6; 4610: 35.1, 21.8)
+    const int tiles = sets < 4 && n > (rows > 8 ? 8192 : 32768) ? 4 : n > (rows > 4 ? 4096 : 12288) ? 2 : 1;
     const int64_t steps = (chunks + 3) / 4;
     const int waves = (int)std::max<int64_t>(1, std::min<int64_t>(steps, 8));
     const bool direct = tiles == 1 && steps <= 2 * waves;
@@ -116,9 +122,9 @@ int fb4_cache_plan(const int32_t* lens, const int32_t* adds, int64_t batch, int 
                           static_cast<const void*>(starts), static_cast<const void*>(slots), static_cast<const void*>(positions)}) {
         if (!aligned(p, 4)) return FB4_ERR_UNSUPPORTED;
     }
-    // (few sequences and tokens: few wavefronts to wait for each other)
+    // (few sequences and tokens: few wavefronts to wait for each other; 256 sequences of a token 4.8 us and 5.0, 8 of 2048 at most 20 and 8.0)
     const int64_t most = std::max(batch, std::min<int64_t>(tokens / 4, kPlanMost));
-    const uint32_t threads = most <= 64 ? 64 : most <= 256 ? 256 : kPlanMost;
+    const uint32_t threads = most <= 256 ? 256 : kPlanMost;
     const PlanShape s = {(uint32_t)batch, (uint32_t)max_pages, (uint32_t)n_free, (uint32_t)tokens, (uint32_t)bits, threads};
     hipStream_t st = static_cast<hipStream_t>(stream);
     launch(batch > (int64_t)kPlanMost ? cache_plan_kernel<4> : cache_plan_kernel<1>, dim3(1), dim3(threads), 0, st, lens, adds, free_count, tables, free_pages, lens_out,
@@ -140,7 +146,8 @@ int fb4_cache_store(const void* k, const int64_t* k_strides, const void* v, cons
     if (int rc = strides_of(k_strides, &sk)) return rc;
     if (int rc = strides_of(v_strides, &sv)) return rc;
     if (!aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 4) || !aligned(cache, 16)) return FB4_ERR_UNSUPPORTED;
-    // Runs begin at any token; a workgroup per token while there are few, one per page's tokens where whole pages come.
+    // Tokens whose runs a workgroup takes, one run after the other: what the tokens are is on the device.  Sequences of a token each want few (1024: one
+    // 70.0 us, four 62.8, sixteen 73.2; 64: one 9.2, four 14.2), prompts a page's (16 of up to 1024 tokens: one 141, four 59, 64 22.7; of up to 4096: 579, 87).
     const int64_t span = std::max<int64_t>(1, std::min<int64_t>(page, tokens / 256));
     const int64_t groups = (tokens + span - 1) / span * heads_k * 2;
     if (groups > (1 << 24) - 1) return FB4_ERR_UNSUPPORTED;
@@ -154,7 +161,7 @@ size_t fb4_cache_attention_workspace(int64_t tokens, int heads, int heads_k, int
 {
     CachePlan p;
     if (plan_attention(tokens, heads, heads_k, dim, page, max_pages, batch, &p) != FB4_OK || !p.split || tokens == 0 || batch == 0) return 0;
-    return (size_t)p.positions * (size_t)(16 * p.rows16) * (size_t)(dim + 2) * sizeof(float);
+    return (size_t)p.positions * p.tile_rows * (size_t)(dim + 2) * sizeof(float);
 }
 
 int fb4_cache_attention(const void* q, const int64_t* q_strides, int64_t tokens, int heads, int heads_k, int64_t dim, const uint8_t* cache, const uint8_t* scales,
@@ -177,18 +184,16 @@ int fb4_cache_attention(const void* q, const int64_t* q_strides, int64_t tokens,
         return FB4_ERR_UNSUPPORTED;
     // (no pages: no sequence has a key)
     const CacheShape s = {(uint32_t)tokens, pages ? (uint32_t)max_pages : 0u, (uint32_t)pages, (uint16_t)batch, (uint16_t)heads, (uint16_t)heads_k,
-                          (uint16_t)p.target, (uint8_t)page_bits_of(page), (uint8_t)(dim / 8), (uint8_t)causal, (uint8_t)p.rows16, scale};
+                          (uint8_t)page_bits_of(page), (uint8_t)(dim / 8 + 128 * causal), scale};
     hipStream_t st = static_cast<hipStream_t>(stream);
     float* parts = static_cast<float*>(workspace);
-    float* states = p.split ? parts + (size_t)p.positions * (16 * p.rows16) * dim : nullptr;
     const dim3 grid((unsigned)p.positions);
-#define FB4_CACHE_KERNEL(kernel, split) launch(kernel, grid, dim3(64 * kCacheWaves), 0, st, static_cast<const uint16_t*>(q), cache, scales, tables, lens, starts, static_cast<uint16_t*>(split ? workspace : out), split ? states : lse, sq, so, s)
-#define FB4_CACHE_LAUNCH(d, u, w, split) FB4_CACHE_KERNEL((cache_attention_kernel<d, u, w, split>), split)
-#define FB4_CACHE_TILES(d, w, split) FB4_CACHE_KERNEL((cache_tiles_kernel<d, w, split>), split)
-#define FB4_CACHE_SETS(d, w, split)                     \
-    if (p.rows16 == 8) FB4_CACHE_TILES(d, w, split);     \
-    else if (p.rows16 == 2) FB4_CACHE_LAUNCH(d, 2, w, split); \
-    else FB4_CACHE_LAUNCH(d, 1, w, split)
+#define FB4_CACHE_KERNEL(kernel) launch(kernel, grid, dim3(64 * kCacheWaves), 0, st, static_cast<const uint16_t*>(q), cache, scales, tables, lens, starts, static_cast<uint16_t*>(out), lse, parts, sq, so, s)
+#define FB4_CACHE_LAUNCH(d, w, split) FB4_CACHE_KERNEL((cache_attention_kernel<d, w, split>))
+#define FB4_CACHE_TILES(d, w, split) FB4_CACHE_KERNEL((cache_tiles_kernel<d, w, split>))
+#define FB4_CACHE_SETS(d, w, split)                             \
+    if (p.tile_rows == kTileRows) FB4_CACHE_TILES(d, w, split); \
+    else FB4_CACHE_LAUNCH(d, w, split)
 #define FB4_CACHE_CASE(d)                               \
     case d:                                             \
         if (dim == 32 * d) {                            \
@@ -208,10 +213,11 @@ int fb4_cache_attention(const void* q, const int64_t* q_strides, int64_t tokens,
 #undef FB4_CACHE_LAUNCH
 #undef FB4_CACHE_KERNEL
     if (p.split) {
-        const int64_t rows = tokens * heads;   // (below the target's tiles of 64 rows and the batch's)
-        const bool few = rows <= 4096;
-        launch(few ? cache_join_kernel<4> : cache_join_kernel<1>, dim3((unsigned)(few ? rows : (rows + 4 * kJoinRows - 1) / (4 * kJoinRows))), dim3(256), 0, st, parts,
-               reinterpret_cast<const float2*>(states), lens, starts, static_cast<uint16_t*>(out), lse, (uint32_t)p.positions, so, s);
+        const int64_t rows = tokens * heads;   // (below the rows of kTilesTarget tiles)
+        const bool few = rows <= kJoinFew;
+        const float2* states = reinterpret_cast<const float2*>(parts + (size_t)p.positions * p.tile_rows * dim);
+        launch(few ? cache_join_kernel<kJoinWaves> : cache_join_kernel<1>, dim3((unsigned)(few ? rows : (rows + 4 * kJoinRows - 1) / (4 * kJoinRows))),
+               dim3(few ? 64 * kJoinWaves : 256), 0, st, parts, states, lens, starts, static_cast<uint16_t*>(out), lse, (uint32_t)p.positions, p.tile_rows, so, s);
     }
     return hipGetLastError() == hipSuccess ? FB4_OK : FB4_ERR_HIP;
 }
