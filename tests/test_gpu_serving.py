@@ -867,3 +867,17 @@ def test_two_calls_at_once_on_two_streams(F):
         got += [F.fb4_cache_attention(q, x.cache, x.scales, x.tables, x.lens, starts, 64, stream=s) for x, s in ((c, a), (d, b))]
     torch.cuda.synchronize()
     assert all(torch.equal(g, want[i % 2]) for i, g in enumerate(got))
+
+
+@pytest.mark.parametrize("dim", [72, 128])
+@pytest.mark.parametrize("counts", [[1, 1, 1, 1, 0], [6, 1, 6, 2, 3], [150, 150, 150, 150, 1], [1, 500, 40, 1, 0]])
+def test_attention_of_one_part_beside_several(F, counts, dim):
+    """Short and long sequences in a call: a tile of one part writes its rows itself, the others' parts meet.  Nothing of what the workspace held counts."""
+    lens = [200, 9000, 600, 3000, 7]
+    c = Paged(F, 51, lens, 2, dim, 64)
+    q = randn(gen(52), 6, sum(counts) + 5, dim).bfloat16()
+    for causal in (True, False):
+        size = F.binding.lib().fb4_cache_attention_workspace(q.shape[1], 6, 2, dim, 64, c.tables.shape[1], len(lens))
+        assert size > 0
+        work = torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda")
+        check_attention(F, c, q, counts, causal, first=2, workspace=work)
