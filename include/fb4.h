@@ -685,7 +685,8 @@ int fb4_cache_plan(const int32_t* lens, const int32_t* adds, int64_t batch, int 
  *   *_strides   host, (head, token) in elements, each a multiple of 8, at least
  *               0 and below 2^35 (FB4_ERR_UNSUPPORTED otherwise)
  *   dim         a multiple of 8, at most 128; heads_k 1..65535; at most
- *               2^31 - 1 tokens and slots (FB4_ERR_UNSUPPORTED otherwise)
+ *               2^31 - 1 tokens and slots, and fewer than 2^23 heads of pages'
+ *               worth of tokens (FB4_ERR_UNSUPPORTED otherwise)
  *   slots       device, int32 [tokens]; one outside 0 .. pages * page - 1 is
  *               not stored.  The tokens of a page stand side by side (as
  *               fb4_cache_plan leaves them); of several for one slot the last counts.  A
@@ -713,8 +714,9 @@ int fb4_cache_store(const void* k, const int64_t* k_strides, const void* v, cons
  *   starts      device, int32 [batch + 1], ascending: the queries of sequence b
  *               are the rows starts[b] .. starts[b + 1] - 1, clamped to 0 ..
  *               tokens (what fb4_cache_plan gives)
- *   batch       at most 4096; tokens * heads / heads_k below 2^31
- *               (FB4_ERR_UNSUPPORTED beyond)
+ *   batch       at most 4096; tokens * heads / heads_k below 2^31, and fewer
+ *               than 2^24 tiles of 16 rows of all key heads, or 128 rows of
+ *               more than 40 rows a sequence (FB4_ERR_UNSUPPORTED beyond)
  *   causal      0 or 1
  *   scale       as in fb4_block_attention
  *   out         device, bf16 [tokens][heads][dim] by out_strides (head, token), rows

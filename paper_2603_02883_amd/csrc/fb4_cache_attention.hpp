@@ -10,7 +10,10 @@
 // least 16 tokens, so each of these sixteenths lies in one page.
 //
 // Rows of a product's second operand are the queries of a key head: the n tokens of a sequence times the query heads that share it, token
-// by token, cut into tiles of 16 kSets.  A workgroup takes one tile, and its wavefronts every fourth step.
+// by token, cut into tiles of 16 (a workgroup's wavefronts take every fourth step of the keys) or of 128 (each wavefront 32 rows, all steps).
+//
+// Roundings to fewer bits than 32: the weights to bf16 as the second product's operand, half a bf16 step of each, beside which the output's own
+// is as large; keys and values are bf16 numbers as they are held.  Products, maxima, sums (of the unrounded weights) and parts are fp32.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -79,8 +82,9 @@ __device__ __forceinline__ uint32_t sequence_of(const int32_t* starts, uint32_t 
 }
 
 // Parts: where tiles are few, the keys of each are shared by several workgroups, of about `share` steps each -- the same for all, so that
-// sequences of unlike lengths get parts by their lengths.  Tiles of few rows: all tiles' steps over kCacheTarget workgroups (512, 768 and
-// 1024, a token each, us: 32 sequences of 8192 keys at most 99, 88, 96; 16: 52, 47, 48; one of 65536: 30.5, 38, 36).  Tiles of 128: the best number of parts by the times below.  A tile of one part writes its rows itself.
+// sequences of unlike lengths get parts by their lengths.  Tiles of few rows: all tiles' steps over kCacheTarget workgroups (512,
+// 768 and 1024, a token each, us: 32 sequences of up to 8192 keys 99, 88, 96; 16: 52, 47, 48; one of 65536: 30.5, 38, 36).  Tiles of 128: the
+// best number of parts by the times below.  A tile of one part writes its rows itself.
 constexpr uint32_t kCacheLeastShare = 2 * kCacheWaves, kCacheTarget = 768, kTilesTarget = 1536;
 // Parts of each of n tiles of `steps` steps.  512 tiles run at a time, two to a compute unit, and steps take 1.2 times as long then as one by one
 // (1.65 and 2 us of 128 channels); a tile's beginning and end take as long as six; parts, their joining twelve and one more per 256 parts.
@@ -294,8 +298,13 @@ __device__ __forceinline__ float2* states_of(float* workspace, uint32_t rows, ui
 
 // ------------------------------------------------------------------------------------------------ attention
 // kD32: channels / 32, rounded up; kWhole: a row is kD32 whole steps and 16-byte pieces.  kSplit: parts, into the workspace: floats
-// [position][16 kSets][dim], then {maximum, sum} of every row; position = (parts in front) * heads_k + key head.
+// [position][rows][dim], then {maximum, sum} of every row; position = (parts in front) * heads_k + key head.
 //
+// What bounds it: the reads of the cache.  A step's keys and values are asked for one step ahead into registers, so that two wavefronts per SIMD
+// (which amdgpu_waves_per_eu holds: three registers more had halved them, 32 sequences in parts 115 and 88 us) keep 8 x 16 KiB of a compute unit
+// on their way.  96 sequences of up to 8192 keys, a token each, 24 heads over 8 of 128 channels: 233 us, 5.1 TB/s; one of 333 keys: 8, its
+// chain of lengths, table, keys and values.  Two sets of 16 rows to a wavefront took 141 to 140 us where one takes 98 to 140 (64 sequences, 3 to 30
+// rows) and are not kept.
 template <int kD32, bool kWhole, bool kSplit>
 __global__ __launch_bounds__(64 * kCacheWaves) __attribute__((amdgpu_waves_per_eu(2))) void cache_attention_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* scales, const int32_t* tables,
                                                                           const int32_t* lens, const int32_t* starts, uint16_t* out, float* lse, float* workspace,
@@ -537,6 +546,13 @@ __global__ __launch_bounds__(64 * kCacheWaves) __attribute__((amdgpu_waves_per_e
 // for the w-th sixteenth of each two steps ahead and puts it down as bf16 one step ahead, so that the converter's half rate (7 cycles for two
 // elements) is paid once for 128 rows.  Rows of keys lie by tile and operand row, 16 bytes further apart than they are long, channels of
 // values likewise: the 16 rows that a read takes start in different banks.
+//
+// What bounds it: no one unit -- vector instructions 45 % of the cycles, matrix cores 38 %, LDS 48 % (a prompt of 16384 tokens, 24 heads over 8 of
+// 128 channels, 1649 GFLOP: 1760 to 1815 us, 0.91 to 0.94 PFLOP/s), and a wavefront's phases one after the other: without staging it takes 0.71 of the
+// time, without the exponentials 0.88, without the reads of keys 0.89, without the barrier 0.90.  Two clips' frame of 1350 queries over 22950 keys, 16
+// heads of 72 channels, 262 GFLOP: 490 us and 28 for joining (72 channels take the products of 96, and of 11 tiles the last is 70 rows).
+// Two wavefronts per SIMD with all their 228 registers are what the sizes allow; 64 rows to a wavefront at one per SIMD took 3379 us, eight
+// wavefronts to a workgroup 1767 and 597 for the frame, E4M3 in LDS decoded by every wavefront 2275, the next keys' products beside the weights 2500.
 template <int kD32, bool kWhole, bool kSplit>
 __global__ __launch_bounds__(64 * kCacheWaves) __attribute__((amdgpu_waves_per_eu(2)))
 void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* scales, const int32_t* tables, const int32_t* lens, const int32_t* starts, uint16_t* out,
@@ -794,8 +810,11 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
     }
 }
 
-// The parts of a row meet.  kWaves = 4: four wavefronts to a row, where rows are few and parts many; 1: kJoinRows rows to a wavefront, one after the
-// other, so that finding their parts, a chain of reads, comes once for them.  Half a wavefront takes a part, four channels a lane.
+// The parts of a row meet: sum of parts' sums and rows times exp2((their maximum - the largest) c), both in fp32.  kWaves = 4: four wavefronts to a row,
+// where rows are few and parts many; 1: kJoinRows rows to a wavefront, one after the other, so that finding their parts, a chain of reads, comes once for
+// them.  Half a wavefront takes a part, four channels a lane.  (The whole call, one row to a wavefront's turn and four wavefronts to a row, us: 24 rows over
+// 65536 keys 61, 37; 192 over 8192: 43, 34; 768: 91, 89; 4080: 49, 59; 32400: 175, 273.  Sixteen wavefronts to a row: 24 rows 15.9, four 15.0.)
+// What bounds it is that chain, about 10 us, then the parts' rows: 43200 rows of three parts of 72 channels 28 us.
 constexpr uint32_t kJoinRows = 4, kJoinWaves = 4, kJoinFew = 1024;
 template <int kWaves>
 __global__ __launch_bounds__(64 * (kWaves > 4 ? kWaves : 4)) void cache_join_kernel(const float* workspace, const float2* states, const int32_t* lens, const int32_t* starts, uint16_t* out,
