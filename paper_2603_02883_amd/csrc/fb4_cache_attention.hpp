@@ -542,13 +542,25 @@ __global__ __launch_bounds__(64 * kCacheWaves) __attribute__((amdgpu_waves_per_e
 }
 
 // ------------------------------------------------------------------------------------------------ attention of many queries
+// Where a row's piece lies in LDS.  A read of 16 bytes a lane takes the 64 banks in four turns of 16 lanes: of lane group g the rows 0 .. 3 and 12 ..
+// 15 with the rows 4 .. 11 of g + 1 (g even; and the other way round).  In each turn the pieces p of one half and p + slots / 4 of the other have
+// to lie in different banks: slots are exchanged by row, so that either half's are closed under that step.  (Rows 16 bytes further apart than they
+// are long instead, which does for 16 rows of one group: a prompt's LDS busy 49 % of the cycles against 35, 1760 us against 1748, four clips' frame 964
+// against 928, two clips' 490 against 496.)
+template <uint32_t kSlots>
+__device__ __forceinline__ uint32_t slot_of_piece(uint32_t piece, uint32_t row)
+{
+    constexpr uint32_t kLow = kSlots / 4, kShift = kSlots == 16 ? 0 : kSlots == 8 ? 1 : 2;
+    const uint32_t y = row >> kShift, x = y / kLow;   // x: row / 4
+    return piece ^ ((((x ^ x >> 1) & 1u) * 2u + (x >> 1)) * kLow + y % kLow);
+}
 // As above, for 128 rows to a workgroup, 32 to a wavefront.  A step's keys and values come into LDS once for all four, decoded: wavefront w asks
 // for the w-th sixteenth of each two steps ahead and puts it down as bf16 one step ahead, so that the converter's half rate (7 cycles for two
-// elements) is paid once for 128 rows.  Rows of keys lie by tile and operand row, 16 bytes further apart than they are long, channels of
-// values likewise: the 16 rows that a read takes start in different banks.
+// elements) is paid once for 128 rows.  Rows of keys lie by tile and operand row, rows of values by channel, in pieces of 16 bytes that slot_of_piece
+// places.
 //
-// What bounds it: no one unit -- vector instructions 45 % of the cycles, matrix cores 38 %, LDS 48 % (a prompt of 16384 tokens, 24 heads over 8 of
-// 128 channels, 1649 GFLOP: 1760 to 1815 us, 0.91 to 0.94 PFLOP/s), and a wavefront's phases one after the other: without staging it takes 0.71 of the
+// What bounds it: no one unit -- vector instructions 45 % of the cycles, matrix cores 38 %, LDS 35 % (a prompt of 16384 tokens, 24 heads over 8 of
+// 128 channels, 1649 GFLOP: 1750 to 1800 us, 0.92 to 0.94 PFLOP/s), and a wavefront's phases one after the other: without staging it takes 0.71 of the
 // time, without the exponentials 0.88, without the reads of keys 0.89, without the barrier 0.90.  Two clips' frame of 1350 queries over 22950 keys, 16
 // heads of 72 channels, 262 GFLOP: 490 us and 28 for joining (72 channels take the products of 96, and of 11 tiles the last is 70 rows).
 // Two wavefronts per SIMD with all their 228 registers are what the sizes allow; 64 rows to a wavefront at one per SIMD took 3379 us, eight
@@ -559,10 +571,10 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
                         float* lse, float* workspace, CacheStrides sq, CacheStrides so, CacheShape s)
 {
     constexpr int kSets = 2;
-    constexpr uint32_t kPitchK = 64 * kD32 + 16, kPitchV = 2 * kCacheStep + 16;
+    constexpr uint32_t kSlotsK = kD32 > 2 ? 16 : 4 * kD32, kSlotsV = kCacheStep / 8, kPitchK = 16 * kSlotsK, kPitchV = 16 * kSlotsV;
     constexpr uint32_t kKeys = kCacheStep * kPitchK, kBuffer = kKeys + 32 * kD32 * kPitchV;
     constexpr int kAsksK = kD32, kAsksV = (kD32 + 1) / 2;   // of 64 lanes: 8 bytes of a key each, 16 of a channel
-    __shared__ __align__(16) uint8_t lds[2 * kBuffer];
+    __shared__ __align__(256) uint8_t lds[2 * kBuffer];
     __shared__ uint32_t notes[2][4];                        // of a buffer's sixteenths: kNone, kNan
     constexpr uint32_t kNone = 1, kNan = 2;
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -653,13 +665,14 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
     auto put = [&](Asked& w, uint32_t step, uint32_t buffer) FB4_INLINE {
         const float fk = __builtin_bit_cast(float, w.k_byte << 23), fv = __builtin_bit_cast(float, w.v_byte << 23);
         uint8_t* to_k = lds + buffer;
-        uint8_t* to_v = lds + buffer + kKeys + 2u * mine;
+        uint8_t* to_v = lds + buffer + kKeys;
 #pragma unroll
         for (int i = 0; i < kAsksK; ++i) {
             const uint32_t j = 64u * i + lane, key = kWhole ? j / (4u * kD32) : j / pieces, c = j - key * (kWhole ? 4u * kD32 : pieces);
             // key 4 t + x of sixteenth w: row 4 w + x of tile t
+            const uint32_t row = 4u * wave + (key & 3u);
             if (kWhole || j < 16u * pieces)
-                *reinterpret_cast<cache_bf16x8*>(to_k + ((key & ~3u) * 4u + 4u * wave + (key & 3u)) * kPitchK + 16u * c) = cache_decode(w.k[i].x, w.k[i].y, fk);
+                *reinterpret_cast<cache_bf16x8*>(to_k + ((key & ~3u) * 4u + row) * kPitchK + 16u * slot_of_piece<kSlotsK>(kD32 == 3 ? c + c / 3u : c, row)) = cache_decode(w.k[i].x, w.k[i].y, fk);
         }
         // a page that is not there, what lies behind the end: zeros; and no NaN that a query does not see
         const uint32_t key = step * kCacheStep + mine;
@@ -680,9 +693,9 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
         for (int i = 0; i < kAsksV; ++i) {
             const uint32_t c = 64u * i + lane;
             if (c < 32u * kD32) {   // (channels past the row: zeros)
-                cache_bf16x8* at = reinterpret_cast<cache_bf16x8*>(to_v + c * kPitchV);
-                at[0] = cache_decode(w.v[i].x, w.v[i].y, fv);
-                at[1] = cache_decode(w.v[i].z, w.v[i].w, fv);
+                uint8_t* at = to_v + c * kPitchV;
+                *reinterpret_cast<cache_bf16x8*>(at + 16u * slot_of_piece<kSlotsV>(2u * wave, c & 15u)) = cache_decode(w.v[i].x, w.v[i].y, fv);
+                *reinterpret_cast<cache_bf16x8*>(at + 16u * slot_of_piece<kSlotsV>(2u * wave + 1u, c & 15u)) = cache_decode(w.v[i].z, w.v[i].w, fv);
             }
         }
         if (lane == 0) notes[buffer != 0u][wave] = note;
@@ -696,7 +709,11 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
 #pragma unroll
         for (int d = 0; d < 2 * kD32; ++d) o[u][d] = cache_f32x4{0, 0, 0, 0};
     }
-    const uint32_t k_at = r * kPitchK + 16u * kD32 * g, v_at = kKeys + r * kPitchV + 32u * g;
+    uint32_t k_at[kD32], v_at[2];
+#pragma unroll
+    for (uint32_t i = 0; i < kD32; ++i) k_at[i] = r * kPitchK + 16u * slot_of_piece<kSlotsK>((kD32 == 3 ? 4u : kD32) * g + i, r);
+#pragma unroll
+    for (uint32_t h = 0; h < 2; ++h) v_at[h] = kKeys + r * kPitchV + 16u * slot_of_piece<kSlotsV>(2u * g + h, r);
     const bool idle = first_row >= n_rows;
     int32_t page = -1;
     if (!kWhole) {   // channels past the row, of keys: zeros for good (the queries' are too, but 0 times what was here need not be)
@@ -716,8 +733,6 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
     // step: its operands are in `buffer`; those of the next, in w, go to the other, and those of the one two behind that are asked for
     auto run_step = [&](uint32_t step, uint32_t buffer, Asked& w) FB4_INLINE {
         __syncthreads();   // this step's operands are there; everyone is done with the other buffer
-        const uint8_t* keys = lds + buffer + k_at;
-        const uint8_t* vals = lds + buffer + v_at;
         if (!idle) {
             const uint32_t note = notes[buffer != 0u][g];
             cache_f32x4 sc[kSets][4];
@@ -727,7 +742,7 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
                 for (int u = 0; u < kSets; ++u) sc[u][t] = cache_f32x4{0, 0, 0, 0};
 #pragma unroll
                 for (int i = 0; i < kD32; ++i) {
-                    const cache_bf16x8 a = *reinterpret_cast<const cache_bf16x8*>(keys + 16u * t * kPitchK + 16u * i);
+                    const cache_bf16x8 a = *reinterpret_cast<const cache_bf16x8*>(lds + buffer + 16u * t * kPitchK + k_at[i]);
 #pragma unroll
                     for (int u = 0; u < kSets; ++u) sc[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[u][i], sc[u][t], 0, 0, 0);
                 }
@@ -753,7 +768,7 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
             for (int d = 0; d < 2 * kD32; ++d) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const cache_bf16x8 a = *reinterpret_cast<const cache_bf16x8*>(vals + 16u * d * kPitchV + 16u * h);
+                    const cache_bf16x8 a = *reinterpret_cast<const cache_bf16x8*>(lds + buffer + 16u * d * kPitchV + v_at[h]);
 #pragma unroll
                     for (int u = 0; u < kSets; ++u) o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[u][h], o[u][d], 0, 0, 0);
                 }
