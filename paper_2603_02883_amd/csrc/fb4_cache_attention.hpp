@@ -293,12 +293,16 @@ __device__ __forceinline__ uint2 rounded(cache_f32x4 x, float f)
     return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
 }
 
-// The workspace's rows' {maximum, sum}, behind all its rows.
-__device__ __forceinline__ float2* states_of(float* workspace, uint32_t rows, uint32_t dim) { return reinterpret_cast<float2*>(workspace + (size_t)gridDim.x * rows * dim); }
+// A position's rows in the workspace, and their {maximum, sum} behind them.
+__device__ __forceinline__ float* part_rows(float* workspace, uint32_t position, uint32_t rows, uint32_t dim) { return workspace + (size_t)position * rows * (dim + 2u); }
+__device__ __forceinline__ float2* part_states(float* workspace, uint32_t position, uint32_t rows, uint32_t dim)
+{
+    return reinterpret_cast<float2*>(part_rows(workspace, position, rows, dim) + rows * dim);
+}
 
 // ------------------------------------------------------------------------------------------------ attention
-// kD32: channels / 32, rounded up; kWhole: a row is kD32 whole steps and 16-byte pieces.  kSplit: parts, into the workspace: floats
-// [position][rows][dim], then {maximum, sum} of every row; position = (parts in front) * heads_k + key head.
+// kD32: channels / 32, rounded up; kWhole: a row is kD32 whole steps and 16-byte pieces.  kSplit: parts, into the workspace: by
+// position floats [rows][dim], then {maximum, sum} of every row; position = (parts in front) * heads_k + key head.
 //
 // What bounds it: the reads of the cache.  A step's keys and values are asked for one step ahead into registers, so that two wavefronts per SIMD
 // (which amdgpu_waves_per_eu holds: three registers more had halved them, 32 sequences in parts 115 and 88 us) keep 8 x 16 KiB of a compute unit
@@ -526,14 +530,14 @@ __global__ __launch_bounds__(64 * kCacheWaves) __attribute__((amdgpu_waves_per_e
                     for (int j = 0; j < 4; ++j) x[j] = fmaf(y[j], w[i], x[j]);
                 }
                 if (kSplit && parts > 1u) {
-                    *reinterpret_cast<cache_f32x4*>(workspace + ((size_t)blockIdx.x * kRows + at_row) * dim + c) = x;
+                    *reinterpret_cast<cache_f32x4*>(part_rows(workspace, blockIdx.x, kRows, dim) + at_row * dim + c) = x;
                 } else {
                     uint16_t* place = out + ((size_t)head * so.head + (size_t)(rows.first + token) * so.token) * 8u + c;
                     *reinterpret_cast<uint2*>(place) = rounded(x, inverse);
                 }
             }
             if ((threadIdx.x & 15u) == 0) {
-                if (kSplit && parts > 1u) states_of(workspace, kRows, dim)[(size_t)blockIdx.x * kRows + at_row] = make_float2(most, total);
+                if (kSplit && parts > 1u) part_states(workspace, blockIdx.x, kRows, dim)[at_row] = make_float2(most, total);
                 else if (lse) lse[(size_t)(rows.first + token) * s.heads + head] = total == 0.0f ? -__builtin_inff() : fmaf(base, s.scale, kCacheLn2 * __builtin_amdgcn_logf(total));
             }
         }
@@ -811,7 +815,7 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
             const uint32_t c = 16u * d + 4u * g;
             if (!kWhole && c >= dim) continue;
             if (kSplit && parts > 1u) {
-                *reinterpret_cast<cache_f32x4*>(workspace + ((size_t)blockIdx.x * kTileRows + row) * dim + c) = o[u][d];
+                *reinterpret_cast<cache_f32x4*>(part_rows(workspace, blockIdx.x, kTileRows, dim) + row * dim + c) = o[u][d];
             } else {
                 uint16_t* place = out + ((size_t)head * so.head + (size_t)(rows.first + token) * so.token) * 8u + c;
                 *reinterpret_cast<uint2*>(place) = rounded(o[u][d], inverse);
@@ -819,7 +823,7 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
         }
         if (g == 0) {
             const float base = state[u].most == -__builtin_inff() ? 0.0f : state[u].most;
-            if (kSplit && parts > 1u) states_of(workspace, kTileRows, dim)[(size_t)blockIdx.x * kTileRows + row] = make_float2(state[u].most, total);
+            if (kSplit && parts > 1u) part_states(workspace, blockIdx.x, kTileRows, dim)[row] = make_float2(state[u].most, total);
             else if (lse) lse[(size_t)(rows.first + token) * s.heads + head] = total == 0.0f ? -__builtin_inff() : fmaf(base, s.scale, kCacheLn2 * __builtin_amdgcn_logf(total));
         }
     }
@@ -832,7 +836,7 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
 // What bounds it is that chain, about 10 us, then the parts' rows: 43200 rows of three parts of 72 channels 28 us.
 constexpr uint32_t kJoinRows = 4, kJoinWaves = 4, kJoinFew = 1024;
 template <int kWaves>
-__global__ __launch_bounds__(64 * (kWaves > 4 ? kWaves : 4)) void cache_join_kernel(const float* workspace, const float2* states, const int32_t* lens, const int32_t* starts, uint16_t* out,
+__global__ __launch_bounds__(64 * (kWaves > 4 ? kWaves : 4)) void cache_join_kernel(float* workspace, const int32_t* lens, const int32_t* starts, uint16_t* out,
                                                          float* lse, uint32_t n_positions, uint32_t tile_rows, CacheStrides so, CacheShape s)
 {
     __shared__ cache_f32x4 meet[kWaves][32];
@@ -860,10 +864,14 @@ __global__ __launch_bounds__(64 * (kWaves > 4 ? kWaves : 4)) void cache_join_ker
         const uint32_t at = (token - rows.first) * group + (head - hk * group), tile = at / tile_rows;
         const uint32_t first = (base + tile * parts) * s.heads_k + hk;   // of the parts' positions
         const uint32_t n = min(parts, first < n_positions ? (n_positions - first + s.heads_k - 1u) / s.heads_k : 0u);
-        const size_t step = (size_t)s.heads_k * tile_rows, from = (size_t)first * tile_rows + (at - tile * tile_rows);
+        const uint32_t in_tile = at - tile * tile_rows;
+        const size_t step = (size_t)s.heads_k * tile_rows * (dim + 2u);   // floats from part to part
+        const float* from = part_rows(workspace, first, tile_rows, dim) + in_tile * dim + c;
+        const float* state = reinterpret_cast<const float*>(part_states(workspace, first, tile_rows, dim) + in_tile);
+        auto state_of = [&](uint32_t p) { return *reinterpret_cast<const float2*>(state + p * step); };
         // (the first parts' rows are asked for before their maxima are known)
         const uint32_t p0 = (kWaves > 1 ? 2u * wave : 0u) + (lane >> 5);
-        auto part = [&](uint32_t p) { return *reinterpret_cast<const cache_f32x4*>(workspace + (from + p * step) * dim + c); };
+        auto part = [&](uint32_t p) { return *reinterpret_cast<const cache_f32x4*>(from + p * step); };
         cache_f32x4 x[4], o = {0, 0, 0, 0};
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i) {
@@ -872,13 +880,13 @@ __global__ __launch_bounds__(64 * (kWaves > 4 ? kWaves : 4)) void cache_join_ker
         }
         float most = -__builtin_inff(), sum = 0.0f;
         float2 mine = make_float2(-__builtin_inff(), 0.0f);
-        if (lane < n) mine = states[from + lane * step];
-        for (uint32_t p = lane; p < n; p += 64u) most = fmaxf(most, p < 64u ? mine.x : states[from + p * step].x);
+        if (lane < n) mine = state_of(lane);
+        for (uint32_t p = lane; p < n; p += 64u) most = fmaxf(most, p < 64u ? mine.x : state_of(p).x);
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
         const float reference = most == -__builtin_inff() ? 0.0f : most;
         for (uint32_t p = lane; p < n; p += 64u) {
-            const float2 st = p < 64u ? mine : states[from + p * step];
+            const float2 st = p < 64u ? mine : state_of(p);
             sum = fmaf(st.y, __builtin_amdgcn_exp2f((st.x - reference) * factor), sum);
         }
 #pragma unroll
@@ -893,7 +901,7 @@ __global__ __launch_bounds__(64 * (kWaves > 4 ? kWaves : 4)) void cache_join_ker
         if (c < dim) {
 #pragma unroll 4
             for (uint32_t p = p0 + 8u * kWaves; p < n; p += 2u * kWaves) {
-                const float w = __builtin_amdgcn_exp2f((states[from + p * step].x - reference) * factor);
+                const float w = __builtin_amdgcn_exp2f((state_of(p).x - reference) * factor);
                 const cache_f32x4 y = part(p);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) o[j] = fmaf(y[j], w, o[j]);

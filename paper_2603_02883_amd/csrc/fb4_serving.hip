@@ -216,9 +216,8 @@ int fb4_cache_attention(const void* q, const int64_t* q_strides, int64_t tokens,
     if (p.split) {
         const int64_t rows = tokens * heads;   // (below the rows of kTilesTarget tiles)
         const bool few = rows <= kJoinFew;
-        const float2* states = reinterpret_cast<const float2*>(parts + (size_t)p.positions * p.tile_rows * dim);
         launch(few ? cache_join_kernel<kJoinWaves> : cache_join_kernel<1>, dim3((unsigned)(few ? rows : (rows + 4 * kJoinRows - 1) / (4 * kJoinRows))),
-               dim3(few ? 64 * kJoinWaves : 256), 0, st, parts, states, lens, starts, static_cast<uint16_t*>(out), lse, (uint32_t)p.positions, p.tile_rows, so, s);
+               dim3(few ? 64 * kJoinWaves : 256), 0, st, parts, lens, starts, static_cast<uint16_t*>(out), lse, (uint32_t)p.positions, p.tile_rows, so, s);
     }
     return hipGetLastError() == hipSuccess ? FB4_OK : FB4_ERR_HIP;
 }
