@@ -549,12 +549,14 @@ __global__ __launch_bounds__(64 * kCacheWaves) __attribute__((amdgpu_waves_per_e
 // Where a row's piece lies in LDS.  A read of 16 bytes a lane takes the 64 banks in four turns of 16 lanes: of lane group g the rows 0 .. 3 and 12 ..
 // 15 with the rows 4 .. 11 of g + 1 (g even; and the other way round).  In each turn the pieces p of one half and p + slots / 4 of the other have
 // to lie in different banks: slots are exchanged by row, so that either half's are closed under that step.  (Rows 16 bytes further apart than they
-// are long instead, which does for 16 rows of one group: a prompt's LDS busy 49 % of the cycles against 35, 1760 us against 1748, four clips' frame 964
-// against 928, two clips' 490 against 496.)
+// are long instead, which does for 16 rows of one group: of 128 channels a prompt's LDS busy 49 % of the cycles against 35, 1755 us against 1742, 64 channels,
+// 5 sequences of 900 queries 166 and 161.  Kept so, as 0 slots, for rows of 12 pieces, which would leave every fourth slot of 16 unused: frames of 72 channels, one
+// clip 297 and 311, two 490 and 500, four 984 and 950, 3500 tokens over 12000 373 and 378.)
 template <uint32_t kSlots>
 __device__ __forceinline__ uint32_t slot_of_piece(uint32_t piece, uint32_t row)
 {
-    constexpr uint32_t kLow = kSlots / 4, kShift = kSlots == 16 ? 0 : kSlots == 8 ? 1 : 2;
+    if (kSlots == 0) return piece;
+    constexpr uint32_t kLow = kSlots ? kSlots / 4 : 1, kShift = kSlots == 16 ? 0 : kSlots == 8 ? 1 : 2;
     const uint32_t y = row >> kShift, x = y / kLow;   // x: row / 4
     return piece ^ ((((x ^ x >> 1) & 1u) * 2u + (x >> 1)) * kLow + y % kLow);
 }
@@ -575,7 +577,9 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
                         float* lse, float* workspace, CacheStrides sq, CacheStrides so, CacheShape s)
 {
     constexpr int kSets = 2;
-    constexpr uint32_t kSlotsK = kD32 > 2 ? 16 : 4 * kD32, kSlotsV = kCacheStep / 8, kPitchK = 16 * kSlotsK, kPitchV = 16 * kSlotsV;
+    constexpr bool kApart = kD32 == 3;   // rows 16 bytes apart instead of exchanged pieces
+    constexpr uint32_t kSlotsK = kApart ? 0 : 4 * kD32, kSlotsV = kApart ? 0 : kCacheStep / 8;
+    constexpr uint32_t kPitchK = 64 * kD32 + 16 * kApart, kPitchV = 2 * kCacheStep + 16 * kApart;
     constexpr uint32_t kKeys = kCacheStep * kPitchK, kBuffer = kKeys + 32 * kD32 * kPitchV;
     constexpr int kAsksK = kD32, kAsksV = (kD32 + 1) / 2;   // of 64 lanes: 8 bytes of a key each, 16 of a channel
     __shared__ __align__(256) uint8_t lds[2 * kBuffer];
@@ -676,7 +680,7 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
             // key 4 t + x of sixteenth w: row 4 w + x of tile t
             const uint32_t row = 4u * wave + (key & 3u);
             if (kWhole || j < 16u * pieces)
-                *reinterpret_cast<cache_bf16x8*>(to_k + ((key & ~3u) * 4u + row) * kPitchK + 16u * slot_of_piece<kSlotsK>(kD32 == 3 ? c + c / 3u : c, row)) = cache_decode(w.k[i].x, w.k[i].y, fk);
+                *reinterpret_cast<cache_bf16x8*>(to_k + ((key & ~3u) * 4u + row) * kPitchK + 16u * slot_of_piece<kSlotsK>(c, row)) = cache_decode(w.k[i].x, w.k[i].y, fk);
         }
         // a page that is not there, what lies behind the end: zeros; and no NaN that a query does not see
         const uint32_t key = step * kCacheStep + mine;
@@ -715,7 +719,7 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
     }
     uint32_t k_at[kD32], v_at[2];
 #pragma unroll
-    for (uint32_t i = 0; i < kD32; ++i) k_at[i] = r * kPitchK + 16u * slot_of_piece<kSlotsK>((kD32 == 3 ? 4u : kD32) * g + i, r);
+    for (uint32_t i = 0; i < kD32; ++i) k_at[i] = r * kPitchK + 16u * slot_of_piece<kSlotsK>(kD32 * g + i, r);
 #pragma unroll
     for (uint32_t h = 0; h < 2; ++h) v_at[h] = kKeys + r * kPitchV + 16u * slot_of_piece<kSlotsV>(2u * g + h, r);
     const bool idle = first_row >= n_rows;
@@ -737,6 +741,8 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
     // step: its operands are in `buffer`; those of the next, in w, go to the other, and those of the one two behind that are asked for
     auto run_step = [&](uint32_t step, uint32_t buffer, Asked& w) FB4_INLINE {
         __syncthreads();   // this step's operands are there; everyone is done with the other buffer
+        const uint8_t* keys = lds + buffer + (kApart ? k_at[0] : 0u);
+        const uint8_t* vals = lds + buffer + (kApart ? v_at[0] : 0u);
         if (!idle) {
             const uint32_t note = notes[buffer != 0u][g];
             cache_f32x4 sc[kSets][4];
@@ -746,7 +752,7 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
                 for (int u = 0; u < kSets; ++u) sc[u][t] = cache_f32x4{0, 0, 0, 0};
 #pragma unroll
                 for (int i = 0; i < kD32; ++i) {
-                    const cache_bf16x8 a = *reinterpret_cast<const cache_bf16x8*>(lds + buffer + 16u * t * kPitchK + k_at[i]);
+                    const cache_bf16x8 a = *reinterpret_cast<const cache_bf16x8*>(keys + 16u * t * kPitchK + (kApart ? 16u * i : k_at[i]));
 #pragma unroll
                     for (int u = 0; u < kSets; ++u) sc[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[u][i], sc[u][t], 0, 0, 0);
                 }
@@ -772,7 +778,7 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
             for (int d = 0; d < 2 * kD32; ++d) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const cache_bf16x8 a = *reinterpret_cast<const cache_bf16x8*>(lds + buffer + 16u * d * kPitchV + v_at[h]);
+                    const cache_bf16x8 a = *reinterpret_cast<const cache_bf16x8*>(vals + 16u * d * kPitchV + (kApart ? 16u * h : v_at[h]));
 #pragma unroll
                     for (int u = 0; u < kSets; ++u) o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[u][h], o[u][d], 0, 0, 0);
                 }
