@@ -568,8 +568,8 @@ __device__ __forceinline__ uint32_t slot_of_piece(uint32_t piece, uint32_t row)
 // What bounds it: no one unit -- vector instructions 45 % of the cycles, matrix cores 38 %, LDS 35 % (a prompt of 16384 tokens, 24 heads over 8 of
 // 128 channels, 1649 GFLOP: 1750 to 1800 us, 0.92 to 0.94 PFLOP/s), and a wavefront's phases one after the other: without staging it takes 0.71 of the
 // time, without the exponentials 0.88, without the reads of keys 0.89, without the barrier 0.90.  Two clips' frame of 1350 queries over 22950 keys, 16
-// heads of 72 channels, 262 GFLOP: 490 us and 28 for joining (72 channels take the products of 96, and of 11 tiles the last is 70 rows).
-// Two wavefronts per SIMD with all their 228 registers are what the sizes allow; 64 rows to a wavefront at one per SIMD took 3379 us, eight
+// heads of 72 channels, 262 GFLOP: 484 to 502 us, 26 to 28 of it joining (72 channels take the products of 96, and of 11 tiles the last is 70 rows).
+// Two wavefronts per SIMD with 200 to 243 of their 256 registers are what the sizes allow; 64 rows to a wavefront at one per SIMD took 3379 us, eight
 // wavefronts to a workgroup 1767 and 597 for the frame, E4M3 in LDS decoded by every wavefront 2275, the next keys' products beside the weights 2500.
 template <int kD32, bool kWhole, bool kSplit>
 __global__ __launch_bounds__(64 * kCacheWaves) __attribute__((amdgpu_waves_per_eu(2)))

@@ -881,3 +881,23 @@ def test_attention_of_one_part_beside_several(F, counts, dim):
         assert size > 0
         work = torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda")
         check_attention(F, c, q, counts, causal, first=2, workspace=work)
+
+
+@pytest.mark.parametrize("block", [32, 16])
+@pytest.mark.parametrize("rows,n,cols", [(1, 33000, 64), (4, 12300, 160), (5, 4100, 96), (8, 32770, 32), (9, 8200, 352), (16, 8193, 1184), (32, 9000, 64), (64, 4097, 96)])
+def test_products_of_many_rows_of_weights(F, luts, rows, n, cols, block):
+    """Several tiles of the weights to a workgroup, by their number and that of the rows; the last ones ragged."""
+    g = gen(rows + n + cols + block)
+    codes, meta = weights(F, luts, g, n, cols, block)
+    x, bias = randn(g, rows, cols).bfloat16(), randn(g, n)
+    for dtype in (torch.bfloat16, torch.float32):
+        out = torch.full((rows, n), 7.0, dtype=dtype, device="cuda")
+        F.fb4_matvec(luts, x, codes, meta, block, bias, out=out)
+        check_product(F, luts, x, codes, meta, block, bias, out)
+
+
+def test_one_prompt_among_many_single_tokens(F):
+    lens = [9 + b % 50 for b in range(499)] + [6000]
+    c = Paged(F, 53, lens, 1, 64, 64)
+    q = randn(gen(54), 3, 499 + 6000, 64).bfloat16()
+    check_attention(F, c, q, [1] * 499 + [6000], True)
