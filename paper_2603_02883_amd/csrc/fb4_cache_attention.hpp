@@ -314,7 +314,7 @@ __global__ __launch_bounds__(64 * kCacheWaves) __attribute__((amdgpu_waves_per_e
                                                                           const int32_t* lens, const int32_t* starts, uint16_t* out, float* lse, float* workspace,
                                                                           CacheStrides sq, CacheStrides so, CacheShape s)
 {
-    constexpr int kSets = 1;
+    constexpr int kSets = 1;   // (of 16 rows, as the shared functions take them)
     constexpr uint32_t kRows = 16, kPitch = 32 * kD32 + 4;
     __shared__ __align__(16) float meet[kCacheWaves][16][kPitch];
     __shared__ float2 states[kCacheWaves][16];
@@ -842,7 +842,7 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
 // What bounds it is that chain, about 10 us, then the parts' rows: 43200 rows of three parts of 72 channels 28 us.
 constexpr uint32_t kJoinRows = 4, kJoinWaves = 4, kJoinFew = 1024;
 template <int kWaves>
-__global__ __launch_bounds__(64 * (kWaves > 4 ? kWaves : 4)) void cache_join_kernel(float* workspace, const int32_t* lens, const int32_t* starts, uint16_t* out,
+__global__ __launch_bounds__(256) void cache_join_kernel(float* workspace, const int32_t* lens, const int32_t* starts, uint16_t* out,
                                                          float* lse, uint32_t n_positions, uint32_t tile_rows, CacheStrides so, CacheShape s)
 {
     __shared__ cache_f32x4 meet[kWaves][32];

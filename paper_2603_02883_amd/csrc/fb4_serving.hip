@@ -217,7 +217,7 @@ int fb4_cache_attention(const void* q, const int64_t* q_strides, int64_t tokens,
         const int64_t rows = tokens * heads;   // (below the rows of kTilesTarget tiles)
         const bool few = rows <= kJoinFew;
         launch(few ? cache_join_kernel<kJoinWaves> : cache_join_kernel<1>, dim3((unsigned)(few ? rows : (rows + 4 * kJoinRows - 1) / (4 * kJoinRows))),
-               dim3(few ? 64 * kJoinWaves : 256), 0, st, parts, lens, starts, static_cast<uint16_t*>(out), lse, (uint32_t)p.positions, p.tile_rows, so, s);
+               dim3(256), 0, st, parts, lens, starts, static_cast<uint16_t*>(out), lse, (uint32_t)p.positions, p.tile_rows, so, s);
     }
     return hipGetLastError() == hipSuccess ? FB4_OK : FB4_ERR_HIP;
 }
