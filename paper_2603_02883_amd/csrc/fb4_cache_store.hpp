@@ -36,7 +36,7 @@ struct StoreShape {
     uint8_t page_bits, pieces;   // pieces: 16-byte ones of a row, dim / 8
 };
 
-// 2^-e of scale byte e + 127 (10 .. 247: a normal number either way)
+// 2^-e of scale byte e + 127, up to 253 (10 .. 247: a normal number either way), and 0 of 254
 __device__ __forceinline__ float inverse_scale(uint32_t byte) { return __builtin_bit_cast(float, (254u - byte) << 23); }
 
 // E4M3 of two bf16 in `w`, times `f`, in the low 16 bits; what is no number is NaN.
@@ -156,7 +156,8 @@ __global__ __launch_bounds__(kStoreThreads) void cache_store_kernel(const uint16
         uint32_t scale = max((most + 0x1Fu) >> 7, kStoreLowest + 8u) - 8u;
         const bool again = !begun && before < scale;   // what the page holds besides is rounded to the larger scale
         if (!begun) scale = max(scale, before);
-        const float f = inverse_scale(scale), f_old = again ? inverse_scale(scale - before + 127u) : 1.0f;
+        // (2^-126 times E4M3's largest is far below half of its least, as 0 times it is, where larger growths have no exponent left)
+        const float f = inverse_scale(scale), f_old = again ? inverse_scale(min(scale - before, 127u) + 127u) : 1.0f;
         uint8_t* to = cache + at_scale * page_bytes;
 #pragma unroll
         for (int i = 0; i < kRounds; ++i) {

@@ -901,3 +901,41 @@ def test_one_prompt_among_many_single_tokens(F):
     c = Paged(F, 53, lens, 1, 64, 64)
     q = randn(gen(54), 3, 499 + 6000, 64).bfloat16()
     check_attention(F, c, q, [1] * 499 + [6000], True)
+
+
+# (growths of the scale's byte on which its inverse is a normal number, 0, and past all exponents)
+@pytest.mark.parametrize("old", [0, 10, 19, 110])
+def test_stores_whose_scale_grows_by_far(F, old):
+    """What a page holds is rounded to a scale that is larger by up to 2^247: beyond 2^18 everything is below half of E4M3's least number."""
+    page, dim, heads = 16, 16, 2
+    growths = [n for n in (1, 5, 17, 18, 19, 100, 126, 127, 128, 129, 130, 200, 237, 247) if 10 <= old + n <= 247]
+    for tokens in (1, 6):
+        g = gen(old + tokens)
+        cache, scales = new_cache(g, len(growths), heads, dim, page)
+        cache[:, :, 0] = 0                          # a head of zeros, one of anything, a NaN in it
+        cache[:, :, 1, 15 * 16 + 15] = 0x7F
+        scales[:] = old
+        x = torch.zeros(heads, len(growths) * tokens, dim)
+        for i, n in enumerate(growths):             # 160 and -240 times the new scale
+            x[:, i * tokens:(i + 1) * tokens] = 1.25 * 2.0 ** (old + n - 120)
+            x[:, (i + 1) * tokens - 1, 3] *= -1.5
+        x = x.bfloat16().cuda()
+        at = [i * page + 3 + t for i in range(len(growths)) for t in range(tokens)]
+        check_store(F, x, x.flip(2), at, cache, scales, page)
+        assert (scales.cpu() == torch.tensor([old + n for n in growths]).view(1, -1, 1)).all()
+
+
+@pytest.mark.parametrize("begin", [0.0, 2.0 ** -100])
+def test_stores_of_large_tokens_behind_small_ones(F, begin):
+    """A page that a token of zeros (or next to nothing) begins, and one from 5e5 to 3e38 behind it, singly and as runs."""
+    page, dim, heads, sizes = 32, 24, 2, (4.6e5, 5e5, 9e5, 1e6, 2.0 ** 60, 3e38)
+    for tokens in (1, 5):
+        cache, scales = torch.zeros(2, len(sizes), heads, page * dim, dtype=torch.uint8, device="cuda"), torch.zeros(2, len(sizes), heads, dtype=torch.uint8, device="cuda")
+        first = torch.full((heads, len(sizes), dim), begin).bfloat16().cuda()
+        first[:, :, 5] *= -1
+        check_store(F, first, first, [p * page for p in range(len(sizes))], cache, scales, page)
+        x = randn(gen(60), heads, len(sizes) * tokens, dim)
+        x = x / x.abs().amax((0, 2), keepdim=True) * torch.tensor(sizes, device="cuda").repeat_interleave(tokens).view(1, -1, 1)
+        at = [p * page + 1 + t for p in range(len(sizes)) for t in range(tokens)]
+        check_store(F, x.bfloat16(), x.flip(2).bfloat16(), at, cache, scales, page)
+        assert np.isfinite(values_of(cache)).all()
