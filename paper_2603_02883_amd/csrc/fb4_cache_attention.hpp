@@ -860,7 +860,10 @@ __global__ __launch_bounds__(256) void cache_join_kernel(float* workspace, const
         if (token < rows.first || token - rows.first >= rows.n) {   // (the first row's sequence, and another one's later)
             const uint32_t b = scalar(sequence_of(starts, token, 0u, 1u, s));
             rows = rows_of(starts, lens, b, s);
-            if (token < rows.first || token - rows.first >= rows.n) continue;   // (of none; with several wavefronts the whole workgroup)
+            if (token < rows.first || token - rows.first >= rows.n) {   // (of none; with several wavefronts the whole workgroup)
+                rows.n = 0;   // (the sequence found may be the next row's, whose parts are not known yet)
+                continue;
+            }
             base = 0;
             walk_parts(starts, lens, group, tile_rows, share, b, base, s);
             base = scalar(base);

@@ -939,3 +939,22 @@ def test_stores_of_large_tokens_behind_small_ones(F, begin):
         at = [p * page + 1 + t for p in range(len(sizes)) for t in range(tokens)]
         check_store(F, x.bfloat16(), x.flip(2).bfloat16(), at, cache, scales, page)
         assert np.isfinite(values_of(cache)).all()
+
+
+@pytest.mark.parametrize("tile", [16, 128])
+@pytest.mark.parametrize("heads,heads_k", [(1, 1), (3, 1), (6, 2), (2, 2)])
+@pytest.mark.parametrize("first", [1, 3])
+def test_attention_in_parts_behind_rows_of_no_sequence(F, heads, heads_k, first, tile):
+    """A wavefront that joins rows has some of no sequence and then some of the first one, whose keys are in several parts."""
+    if tile == 16:   # (at most 40 rows to a sequence)
+        lens = [5000] + [300 + 7 * b for b in range(43)]
+        counts = [30 * heads_k // heads] + [25 * heads_k // heads] * 43
+    else:
+        lens, counts = [9000, 700], [900, 300]
+    c = Paged(F, 61, lens, heads_k, 64, 64)
+    tokens = first + sum(counts) + 2
+    assert tokens * heads > 1024 and heads * first % 4
+    assert F.binding.lib().fb4_cache_attention_workspace(tokens, heads, heads_k, 64, 64, c.tables.shape[1], len(lens)) > 0
+    q = randn(gen(62), heads, tokens, 64).bfloat16()
+    for causal in (True, False):
+        check_attention(F, c, q, counts, causal, first=first)
