@@ -635,9 +635,10 @@ int fb4_matvec(const fb4_luts* luts, const void* x, int64_t rows, int64_t x_row_
  *   cache       uint8 [2][pages][heads_k][page * dim], 16-byte aligned: OCP FP8
  *               E4M3 elements; per page and head the keys [page][dim], the
  *               values [dim][page]
- *   scales      uint8 [2][pages][heads_k], E8M0 (value 2^(s - 127)): one for a
- *               page's keys and one for its values of every head; element times scale is
- *               always a bf16 number
+ *   scales      uint8 [2][pages][heads_k], E8M0 (value 2^(s - 127)), at most 247:
+ *               one for a page's keys and one for its values of every head; element
+ *               times scale is a bf16 number, or Inf where it reaches 2^128 (magnitudes
+ *               from 1.9375 * 2^127 on are stored so)
  * fb4_cache_plan: the pages and slots of new tokens, from the sequences'
  * lengths, on the GPU.  In the order of the sequences:
  *   adds[b] < 0   the sequence loses its last -adds[b] tokens (all, if it has
@@ -728,7 +729,8 @@ int fb4_cache_store(const void* k, const int64_t* k_strides, const void* v, cons
  *               otherwise; 0 for a negative or unserved size); may be NULL where that is 0; free
  *               again when the call's work on the stream is done
  * A query without a key, infinite and NaN scores: as in fb4_block_attention.  A
- * value behind a query's last key never touches its result, NaN or not.  Rows of no sequence keep what
+ * value behind a query's last key never touches its result, NaN, Inf or not; one that it
+ * sees makes its channel Inf or NaN then.  Rows of no sequence keep what
  * they held, in out and in lse.  A row's sums are formed in an order that depends on
  * the call's sizes and all sequences' lengths (the same call always gives the
  * same results); the launch does not depend on what lens, starts and tables hold, so a

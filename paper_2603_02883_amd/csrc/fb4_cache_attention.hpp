@@ -253,10 +253,12 @@ __device__ __forceinline__ uint4 first_bytes(uint4 w, uint32_t n)
     auto mask = [&](uint32_t i) { return n >= 4u * i + 4u ? 0xFFFFFFFFu : n <= 4u * i ? 0u : (1u << (8u * (n - 4u * i))) - 1u; };
     return make_uint4(w.x & mask(0), w.y & mask(1), w.z & mask(2), w.w & mask(3));
 }
-// Bytes that are NaN, as 1 each (0x7F is E4M3's NaN; one more carries into the sign and no further).
-__device__ __forceinline__ uint4 nans_of(uint4 w)
+// Bytes that are no finite bf16 with their page's scale, as 1 each: what is added to a magnitude for that to carry into the sign, and no further.
+// 0x7F is E4M3's NaN; with the largest scale, 2^120 (byte 247), 0x78 is 2^128.
+__device__ __forceinline__ uint32_t past_numbers(uint32_t scale_byte) { return scale_byte < 247u ? 0x01010101u : 0x08080808u; }
+__device__ __forceinline__ uint4 nans_of(uint4 w, uint32_t past)
 {
-    auto some = [](uint32_t x) { return (((x & 0x7F7F7F7Fu) + 0x01010101u) >> 7) & 0x01010101u; };
+    auto some = [past](uint32_t x) { return (((x & 0x7F7F7F7Fu) + past) >> 7) & 0x01010101u; };
     return make_uint4(some(w.x), some(w.y), some(w.z), some(w.w));
 }
 __device__ __forceinline__ uint4 without(uint4 w, uint4 nans) { return make_uint4(w.x & ~(nans.x * 0xFFu), w.y & ~(nans.y * 0xFFu), w.z & ~(nans.z * 0xFFu), w.w & ~(nans.w * 0xFFu)); }
@@ -268,8 +270,8 @@ __device__ __forceinline__ cache_bf16x8 seen_keys(uint32_t key, uint32_t limit)
     for (uint32_t i = 0; i < 4; ++i) y[i] = (key + 2u * i < limit ? 0x3F80u : 0u) | (key + 2u * i + 1u < limit ? 0x3F800000u : 0u);
     return __builtin_bit_cast(cache_bf16x8, make_uint4(y[0], y[1], y[2], y[3]));
 }
-// What lies behind a query's last key has weight 0, but 0 times NaN is none.  So the keys that some query does not see come into the products without
-// NaN; where there was one, a walk over these keys at the end, with products of ones, says which accumulators it belongs to.
+// What lies behind a query's last key has weight 0, but 0 times NaN or Inf is no number.  So the keys that some query does not see come into the products
+// without them; where there was one, a walk over these keys at the end, with products of ones, says which accumulators become NaN.
 template <int kD16, int kSets, typename Pieces>
 __device__ __forceinline__ void mark_nans(cache_f32x4 (&o)[kSets][kD16], Pieces pieces, uint32_t key, const uint32_t (&limit)[kSets])
 {
@@ -381,6 +383,7 @@ __global__ __launch_bounds__(64 * kCacheWaves) __attribute__((amdgpu_waves_per_e
     uint4 kr[4][(kD32 + 1) / 2], vr[2 * kD32];   // four tiles of keys; 16 channels each
     float k_scale = 0.0f, v_scale = 0.0f;
     auto scale_of = [&](uint32_t byte) FB4_INLINE { return __builtin_bit_cast(float, byte << 23); };
+    auto past_of = [&](float scale) FB4_INLINE { return past_numbers(__builtin_bit_cast(uint32_t, scale) >> 23); };
     auto fetch_k = [&](uint32_t step, int32_t p) FB4_INLINE {
         const size_t at = (size_t)max(p, 0) * s.heads_k + hk;   // (what no page has: another's, whose products are replaced)
         k_scale = scale_of(scales[at]);
@@ -472,10 +475,11 @@ __global__ __launch_bounds__(64 * kCacheWaves) __attribute__((amdgpu_waves_per_e
         // ---- O^T
         if (step * kCacheStep + kCacheStep > least) {
             const uint32_t n = rows.len > key ? min(rows.len - key, 16u) : 0u;   // (behind a sequence's end a page may hold anything)
+            const uint32_t past = past_of(v_scale);
 #pragma unroll
             for (int d = 0; d < 2 * kD32; ++d) {
                 vr[d] = first_bytes(vr[d], n);
-                const uint4 bad = nans_of(vr[d]);
+                const uint4 bad = nans_of(vr[d], past);
                 nans |= bad.x | bad.y | bad.z | bad.w;
                 vr[d] = without(vr[d], bad);
             }
@@ -497,7 +501,8 @@ __global__ __launch_bounds__(64 * kCacheWaves) __attribute__((amdgpu_waves_per_e
         for (step = first + (wave + kCacheWaves - (first - from) % kCacheWaves) % kCacheWaves; step < to; step += kCacheWaves) {
             const uint32_t key = step * kCacheStep + 16u * g, n = rows.len > key ? min(rows.len - key, 16u) : 0u;
             fetch_v(step, page_of(key));
-            mark_nans(o, [&](int d) FB4_INLINE { return nans_of(first_bytes(vr[d], n)); }, key, limit);
+            const uint32_t past = past_of(v_scale);
+            mark_nans(o, [&](int d) FB4_INLINE { return nans_of(first_bytes(vr[d], n), past); }, key, limit);
         }
     }
     // ---- the wavefronts meet
@@ -682,16 +687,17 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
             if (kWhole || j < 16u * pieces)
                 *reinterpret_cast<cache_bf16x8*>(to_k + ((key & ~3u) * 4u + row) * kPitchK + 16u * slot_of_piece<kSlotsK>(c, row)) = cache_decode(w.k[i].x, w.k[i].y, fk);
         }
-        // a page that is not there, what lies behind the end: zeros; and no NaN that a query does not see
+        // a page that is not there, what lies behind the end: zeros; and no NaN or Inf that a query does not see
         const uint32_t key = step * kCacheStep + mine;
         uint32_t note = w.there ? 0u : kNone;
         if (!w.there || key + 16u > least_of_all) {
             const uint32_t n = w.there && rows.len > key ? min(rows.len - key, 16u) : 0u;
+            const uint32_t past = past_numbers(w.v_byte);
             uint32_t some = 0;
 #pragma unroll
             for (int i = 0; i < kAsksV; ++i) {
                 w.v[i] = first_bytes(w.v[i], n);
-                const uint4 bad = nans_of(w.v[i]);
+                const uint4 bad = nans_of(w.v[i], past);
                 some |= bad.x | bad.y | bad.z | bad.w;
                 w.v[i] = without(w.v[i], bad);
             }
@@ -801,11 +807,12 @@ void cache_tiles_kernel(const uint16_t* q, const uint8_t* cache, const uint8_t* 
         for (uint32_t step = max(from, least_of_all / kCacheStep); step < to; ++step) {
             const uint32_t key = step * kCacheStep + 16u * g;
             const int32_t at = page_of(key);
-            const uint8_t* v = values + ((size_t)max(at, 0) * s.heads_k + hk) * page_bytes + (key & in_page);
-            const uint32_t n = at >= 0 && rows.len > key ? min(rows.len - key, 16u) : 0u;
+            const size_t place = (size_t)max(at, 0) * s.heads_k + hk;
+            const uint8_t* v = values + place * page_bytes + (key & in_page);
+            const uint32_t n = at >= 0 && rows.len > key ? min(rows.len - key, 16u) : 0u, past = past_numbers(scales[(size_t)s.pages * s.heads_k + place]);
             mark_nans(o, [&](int d) FB4_INLINE {
                 const uint32_t c = 16u * d + r;
-                return nans_of(c < dim ? first_bytes(*reinterpret_cast<const uint4*>(v + ((size_t)c << bits)), n) : make_uint4(0, 0, 0, 0));
+                return nans_of(c < dim ? first_bytes(*reinterpret_cast<const uint4*>(v + ((size_t)c << bits)), n) : make_uint4(0, 0, 0, 0), past);
             }, key, limit);
         }
     }

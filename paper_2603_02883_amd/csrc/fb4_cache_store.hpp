@@ -23,7 +23,7 @@
 namespace fb4 {
 
 constexpr uint32_t kStoreThreads = 256, kStoreMaxPage = 128;
-constexpr uint32_t kStoreLowest = 10, kStoreHighest = 247;   // scale bytes: every element is a normal bf16; the largest bf16 fits
+constexpr uint32_t kStoreLowest = 10, kStoreHighest = 247;   // scale bytes: every element is a normal bf16, or (256 with the highest) 2^128
 
 typedef float store_f32x2 __attribute__((ext_vector_type(2)));
 

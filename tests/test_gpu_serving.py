@@ -958,3 +958,46 @@ def test_attention_in_parts_behind_rows_of_no_sequence(F, heads, heads_k, first,
     q = randn(gen(62), heads, tokens, 64).bfloat16()
     for causal in (True, False):
         check_attention(F, c, q, counts, causal, first=first)
+
+
+@pytest.mark.parametrize("long,n", [(150, 3), (150, 40), (2000, 3), (2000, 40), (130, 9), (130, 70)])
+@pytest.mark.parametrize("dim", [64, 72])
+@pytest.mark.parametrize("element", [0x78, 0xF8, 0x7E])
+def test_attention_values_past_the_largest_number_stay_behind_a_querys_end(F, long, n, dim, element):
+    """An element that the largest scale takes to 2^128 and beyond is Inf as an operand, whose product with a weight of 0 is no number."""
+    for place in (long - 2, long - n, long - n - 1):
+        c = Paged(F, 63, [long], 2, dim, 32)
+        p = int(c.tables[0, place // 32])
+        held = c.cache[1, p].view(2, dim, 32)[1]
+        held[:, :] = 0
+        c.scales[1, p, 1] = 247
+        if long % 32 and p == int(c.tables[0, long // 32]):
+            held[:, long % 32:] = 0x7E           # (past all numbers as well, behind the sequence's end)
+        q = randn(gen(64), 4, n, dim).bfloat16()
+        call = lambda: F.fb4_cache_attention(q, c.cache, c.scales, c.tables, c.lens, ints([0, n]), c.page)
+        want = call()
+        assert want[:, :2].isfinite().all()
+        held[5, place % 32] = element
+        out = call()
+        sees = torch.arange(long - n, long, device="cuda") >= place
+        assert torch.equal(out[~sees], want[~sees]) and want[~sees].isfinite().all()
+        assert not out[sees][:, 2:, 5].isfinite().any()
+        keep = torch.ones(dim, dtype=torch.bool, device="cuda")
+        keep[5] = False
+        assert torch.equal(out[:, :, keep], want[:, :, keep]) and torch.equal(out[:, :2], want[:, :2])
+
+
+def test_the_largest_numbers_through_the_cache(F):
+    """A stored magnitude from 1.9375 * 2^127 on is held as 2^128; queries that do not see it are as without it, and keep their numbers."""
+    page, dim, n, large = 16, 16, 40, 3.3895313892515355e38
+    k, v = randn(gen(65), 1, n, dim).bfloat16(), randn(gen(66), 1, n, dim).bfloat16()
+    q = randn(gen(67), 2, n, dim).bfloat16()
+    outs = []
+    for x in (0.0, large, -large, 1.875 * 2.0 ** 127):
+        v[0, 33, 7] = x
+        cache, scales = torch.zeros(2, 3, 1, page * dim, dtype=torch.uint8, device="cuda"), torch.zeros(2, 3, 1, dtype=torch.uint8, device="cuda")
+        check_store(F, k, v, list(range(n)), cache, scales, page)
+        outs.append(F.fb4_cache_attention(q, cache, scales, ints([[0, 1, 2]]), ints([n]), ints([0, n]), page))
+    assert all(o[:33].isfinite().all() for o in outs) and not any(o[33:, :, 7].isfinite().any() for o in outs[1:3]) and outs[3].isfinite().all()
+    assert all(torch.equal(o[:32], outs[0][:32]) for o in outs)      # (keys 32 .. share a page, whose scale is another then)
+    assert all(torch.equal(o[32], outs[3][32]) for o in outs[1:3])
