@@ -64,8 +64,8 @@ __device__ __forceinline__ CacheRows rows_of(const int32_t* starts, const int32_
     r.len = (uint32_t)min(max((int64_t)lens[b], (int64_t)0), (int64_t)s.max_pages << s.page_bits);
     return r;
 }
-__device__ __forceinline__ uint32_t tiles_of(uint32_t n, uint32_t group, uint32_t tile_rows) { return (n * group + tile_rows - 1u) / tile_rows; }
-__device__ __forceinline__ uint32_t steps_of(uint32_t len) { return (len + kCacheStep - 1u) / kCacheStep; }
+__host__ __device__ __forceinline__ uint32_t tiles_of(uint32_t n, uint32_t group, uint32_t tile_rows) { return (n * group + tile_rows - 1u) / tile_rows; }
+__host__ __device__ __forceinline__ uint32_t steps_of(uint32_t len) { return (len + kCacheStep - 1u) / kCacheStep; }
 
 // The last sequence whose place is at most `slot`, by a wavefront: 64 candidates at a time.
 __device__ __forceinline__ uint32_t sequence_of(const int32_t* starts, uint32_t slot, uint32_t group, uint32_t tile_rows, const CacheShape& s)
@@ -86,22 +86,38 @@ __device__ __forceinline__ uint32_t sequence_of(const int32_t* starts, uint32_t 
 // 768 and 1024, a token each, us: 32 sequences of up to 8192 keys 99, 88, 96; 16: 52, 47, 48; one of 65536: 30.5, 38, 36).  Tiles of 128: the
 // best number of parts by the times below.  A tile of one part writes its rows itself.
 constexpr uint32_t kCacheLeastShare = 2 * kCacheWaves, kCacheTarget = 768, kTilesTarget = 1536;
-// Parts of each of n tiles of `steps` steps.  512 tiles run at a time, two to a compute unit, and steps take 1.2 times as long then as one by one
+// Parts of each of n tiles of `steps` sixteenths of a step.  512 tiles run at a time, two to a compute unit, and steps take 1.2 times as long then as one by one
 // (1.65 and 2 us of 128 channels); a tile's beginning and end take as long as six; parts, their joining twelve and one more per 256 parts.
 // (24 heads of 128 channels, 128 tokens over 1024 keys: one part 34.9, two 36.8; over 2048: 63.5, four 39.0.  16 heads of 72 channels, 1350 tokens
 // over 2048: one 55, two 61; over 4096: 104, 85; 3500 tokens over 12000: one 373, two 408; 5000: 648, 552.)
-__host__ __device__ inline uint32_t tile_parts(uint32_t n, float steps)
+// In integers (costs in 160ths of a step): the attention's launch and the joining one each compute it, in kernels compiled apart, and where parts lie in the
+// workspace hangs on the same number in both.
+__host__ __device__ inline uint32_t tile_parts(uint32_t n, uint32_t steps)
 {
-    float least = 0.0f;
+    uint64_t least = 0;
     uint32_t best = 1;
-    for (uint32_t p = 1; p <= 16u && (p == 1u || (n * p <= kTilesTarget && steps >= (float)(p * kCacheLeastShare))); ++p) {
-        const float cost = (float)((n * p + 511u) / 512u) * (steps / (float)p + 6.0f) * (n * p > 256u ? 1.2f : 1.0f) + (p > 1u ? 12.0f + (float)(n * p) / 256.0f : 0.0f);
+#pragma unroll
+    for (uint32_t p = 1; p <= 16u; ++p) {
+        if (p > 1u && (n * p > kTilesTarget || steps < 16u * p * kCacheLeastShare)) break;
+        const uint64_t cost = (uint64_t)((n * p + 511u) / 512u) * (steps / p + 96u) * (n * p > 256u ? 12u : 10u) + (p > 1u ? 1920u + n * p * 5u / 8u : 0u);
         if (p == 1u || cost < least) {
             best = p;
             least = cost;
         }
     }
     return best;
+}
+// Steps to a part of `tiles` tiles with `sum` steps.
+__host__ __device__ __forceinline__ uint32_t share_of_tiles(uint64_t sum, uint32_t tiles, uint32_t heads_k, uint32_t tile_rows)
+{
+    uint32_t share;
+    if (tile_rows < kTileRows) {
+        share = (uint32_t)((sum * heads_k + kCacheTarget - 1u) / kCacheTarget);
+    } else {
+        const uint32_t n = tiles ? tiles : 1u, steps = (uint32_t)((sum * 16u + n - 1u) / n), parts = 16u * tile_parts(n * heads_k, steps);
+        share = (steps + parts - 1u) / parts;
+    }
+    return share > kCacheLeastShare ? share : kCacheLeastShare;
 }
 __device__ __forceinline__ uint32_t share_of(const int32_t* starts, const int32_t* lens, uint32_t group, uint32_t tile_rows, const CacheShape& s)
 {
@@ -118,16 +134,13 @@ __device__ __forceinline__ uint32_t share_of(const int32_t* starts, const int32_
         sum += __shfl_xor(sum, d);
         tiles += __shfl_xor(tiles, d);
     }
-    if (tile_rows < kTileRows) {
-        return (uint32_t)max((sum * s.heads_k + kCacheTarget - 1u) / kCacheTarget, (uint64_t)kCacheLeastShare);
-    }
-    const float steps = (float)sum / (float)max(tiles, 1u);
-    return max((uint32_t)ceilf(steps / (float)tile_parts(max(tiles, 1u) * s.heads_k, steps)), kCacheLeastShare);
+    return share_of_tiles(sum, tiles, s.heads_k, tile_rows);
 }
 // (of 128 rows to the nearest number: one more than meant is a round more)
-__device__ __forceinline__ uint32_t parts_of(uint32_t len, uint32_t share, uint32_t tile_rows)
+__host__ __device__ __forceinline__ uint32_t parts_of(uint32_t len, uint32_t share, uint32_t tile_rows)
 {
-    return max((steps_of(len) + (tile_rows < kTileRows ? share - 1u : share / 2u)) / share, 1u);
+    const uint32_t parts = (steps_of(len) + (tile_rows < kTileRows ? share - 1u : share / 2u)) / share;
+    return parts ? parts : 1u;
 }
 
 // Walks the sequences' tiles times parts, by a wavefront: until position `at` (-> its sequence, and `at` from its first one on), or

@@ -54,7 +54,7 @@ int plan_attention(int64_t tokens, int heads, int heads_k, int64_t dim, int page
     p->tile_rows = many ? kTileRows : 16;
     // (at least so many tiles have rows)
     const int64_t tiles = std::max((rows + p->tile_rows - 1) / p->tile_rows, batch) * heads_k, keys = max_pages << bits;
-    p->split = many ? tiles <= (int64_t)kTilesTarget && tile_parts((uint32_t)tiles, (float)((keys + kCacheStep - 1) / kCacheStep)) > 1 : tiles < kCacheFew && keys > kCacheShort;
+    p->split = many ? tiles <= (int64_t)kTilesTarget && tile_parts((uint32_t)tiles, (uint32_t)((keys + kCacheStep - 1) / kCacheStep * 16)) > 1 : tiles < kCacheFew && keys > kCacheShort;
     // (a sequence of S steps has at most S / share + 1 parts to a tile, which over all tiles is the target's number and one more each)
     p->positions = (rows / p->tile_rows + batch) * heads_k + (p->split ? many ? kTilesTarget : kCacheTarget : 0);
     if (p->positions > (1 << 24) - 1) return FB4_ERR_UNSUPPORTED;

@@ -242,3 +242,75 @@ def test_outputs_are_made_on_the_stream_that_the_call_runs_on(monkeypatch):
             one(stream)
             assert len(made) == n and handles[-1] == handle and all(t.made == (kind, name) for t in made)
             assert all(t.kept_for == ([] if stream is None else ["callers"]) for t in made)
+
+
+@pytest.fixture(scope="module")
+def shares(tmp_path_factory):
+    """The attention's rules for its parts, compiled for the host with multiplications and additions fused and not."""
+    import os
+    import shutil
+    import subprocess
+
+    from paper_2603_02883_amd import build
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    if shutil.which(hipcc) is None:
+        pytest.skip("no hipcc")
+    at = tmp_path_factory.mktemp("shares")
+    (at / "shares.hip").write_text('#include "%s/fb4_cache_attention.hpp"\n' % build.CSRC + """
+extern "C" unsigned share(unsigned long long sum, unsigned tiles, unsigned heads_k, unsigned rows) { return fb4::share_of_tiles(sum, tiles, heads_k, rows); }
+extern "C" unsigned parts(unsigned len, unsigned share, unsigned rows) { return fb4::parts_of(len, share, rows); }
+""")
+    libs = []
+    for mode in ("off", "fast-honor-pragmas"):
+        lib = str(at / (mode + ".so"))
+        subprocess.run([hipcc, "--offload-host-only", "-O2", "-std=c++17", "-mfma", "-ffp-contract=" + mode, "-fPIC", "-shared", str(at / "shares.hip"), "-o", lib], check=True,
+                       capture_output=True)
+        libs.append(ctypes.CDLL(lib))
+        libs[-1].share.argtypes = [ctypes.c_ulonglong] + [ctypes.c_uint] * 3
+        libs[-1].parts.argtypes = [ctypes.c_uint] * 3
+        libs[-1].share.restype = libs[-1].parts.restype = ctypes.c_uint
+    return libs
+
+
+def test_both_launches_come_to_the_same_parts(shares):
+    """The attention's launch and the joining one each compute the parts, in kernels that a compiler may treat apart: where two numbers of parts
+    cost nearly the same the choice hangs on no rounding."""
+    plain, fused = shares
+    near = 0
+    for n in range(1, 769):
+        costs = [(p, -(-n * p // 512) * (1.2 if n * p > 256 else 1.0), 12 + n * p / 256 if p > 1 else 0.0) for p in range(1, 17) if p == 1 or n * p <= 1536]
+        for i, (p, a, c) in enumerate(costs):
+            for q, b, d in costs[i + 1:]:
+                if a / p == b / q:
+                    continue
+                steps = (d - c + 6 * b - 6 * a) / (a / p - b / q)      # where p and q parts cost alike
+                if 1 < steps < 2 ** 21:
+                    for total in range(max(1, int(steps * n) - 1), int(steps * n) + 3):
+                        near += 1
+                        assert plain.share(total, n, 1, 128) == fused.share(total, n, 1, 128), (n, total)
+    assert near > 10000
+
+
+def test_parts_fit_their_workspace(shares):
+    """All tiles' parts together are no more than the positions that the workspace and the launch have, whatever the sequences' lengths."""
+    import random
+    r, split = random.Random(5), 0
+    log = lambda lo, hi: int(round(lo * (hi / lo) ** r.random()))
+    for _ in range(3000):
+        batch, heads_k, group, page = log(1, 300), r.choice([1, 2, 8, 24]), r.choice([1, 3, 5]), 64
+        wide = log(17, 40000)
+        counts = [r.choice([1, 1, 0, log(1, 300), log(1, 3000)]) if r.random() < 0.9 else log(1, 9000) for _ in range(batch)] if r.random() < 0.7 else [log(1, 4000)] * batch
+        lens = [r.choice([wide * page, log(1, wide * page), 0, 1, 64]) for _ in range(batch)] if r.random() < 0.8 else [wide * page] * batch
+        tokens, dim = sum(counts) + r.choice([0, 5]), 8
+        size = B.lib().fb4_cache_attention_workspace(tokens, heads_k * group, heads_k, dim, page, wide, batch)
+        if not size:
+            continue
+        split += 1
+        rows = 128 if tokens * group > 40 * batch or tokens * group >= 16384 + batch * group else 16
+        positions = size // (rows * (dim + 2) * 4)
+        tiles = [-(-n * group // rows) for n in counts]
+        steps = [-(-n // 64) for n in lens]
+        share = shares[0].share(sum(t * s for t, s in zip(tiles, steps)), sum(tiles), heads_k, rows)
+        used = sum(t * shares[0].parts(n, share, rows) for t, n in zip(tiles, lens)) * heads_k
+        assert used <= positions, (counts, lens, share)
+    assert split > 300
