@@ -1001,3 +1001,39 @@ def test_the_largest_numbers_through_the_cache(F):
     assert all(o[:33].isfinite().all() for o in outs) and not any(o[33:, :, 7].isfinite().any() for o in outs[1:3]) and outs[3].isfinite().all()
     assert all(torch.equal(o[:32], outs[0][:32]) for o in outs)      # (keys 32 .. share a page, whose scale is another then)
     assert all(torch.equal(o[32], outs[3][32]) for o in outs[1:3])
+
+
+@pytest.mark.parametrize("heads,heads_k,tokens,wide,batch", [(2, 2, 6, 9, 3), (2, 2, 6, 600, 3), (3, 1, 500, 600, 3), (3, 1, 500, 600, 48), (6, 2, 400, 9, 3)])
+def test_nothing_is_written_beside_what_starts_and_lengths_name(F, heads, heads_k, tokens, wide, batch):
+    """Rows past the tensor, falling starts, lengths past the table, between marked margins: whole calls and ones in parts, joined by one
+    wavefront to a row and by several.  What is ascending after clamping is compared with float64."""
+    dim, page, mark, margin = 64, 16, 3.0, 4096
+    long = 100 if wide < 64 else 3000
+    c = Paged(F, 68, [long] * batch, heads_k, dim, page, wide=wide)
+    q = randn(gen(69), heads, tokens, dim).bfloat16()
+    size = F.binding.lib().fb4_cache_attention_workspace(tokens, heads, heads_k, dim, page, wide, batch)
+    assert (size > 0) == (wide > 64)
+    few = tokens // 2
+    spread = [i * few // batch for i in range(batch)]
+    for starts in (spread + [few + 1], spread + [10 ** 6], [-5] + spread[1:] + [few], [few] * batch + [2 ** 31 - 1], [(-1) ** i * i * tokens for i in range(batch + 1)],
+                   [tokens - i for i in range(batch + 1)], [tokens if i % 2 else 0 for i in range(batch + 1)], [-2 ** 31] * (batch + 1), [2 ** 31 - 1] * (batch + 1)):
+        at = [min(max(s, 0), tokens) for s in starts]
+        for n_keys in (long, 2 ** 31 - 1, -5):
+            c.lens[:] = n_keys
+            for causal in (True, False):
+                n = tokens * heads * dim
+                memory, sums = torch.full((n + 2 * margin,), mark, dtype=torch.bfloat16, device="cuda"), torch.full((tokens * heads + 2 * margin,), mark, device="cuda")
+                out, lse = memory[margin:margin + n].view(tokens, heads, dim), sums[margin:margin + tokens * heads].view(tokens, heads)
+                work = torch.full((size + 2 * margin,), 0xA5, dtype=torch.uint8, device="cuda")
+                F.fb4_cache_attention(q, c.cache, c.scales, c.tables, c.lens, ints(starts), page, causal=causal, out=out, lse=lse, workspace=work[margin:margin + size] if size else None)
+                for t in (memory, sums):
+                    assert (t[:margin] == mark).all() and (t[-margin:] == mark).all()
+                assert (work[:margin] == 0xA5).all() and (work[margin + size:] == 0xA5).all()
+                named = torch.zeros(tokens, dtype=torch.bool, device="cuda")
+                for a, b in zip(at, at[1:]):
+                    named[a:b] = True
+                assert (out[~named] == mark).all() and (lse[~named] == mark).all()
+                if at == sorted(at) and n_keys == long:
+                    counts = [b - a for a, b in zip(at, at[1:])]
+                    got, got_lse = check_attention(F, c, q, counts, causal, first=at[0])
+                    assert torch.equal(got, out) and torch.equal(got_lse, lse)
