@@ -610,7 +610,7 @@ int fb4_block_attention(const void* q, const void* k, const void* v, const int64
  *               [n][cols/2], 16-byte aligned, and uint16 [n][cols/block], 4-byte
  *               aligned with block 16 (FB4_ERR_UNSUPPORTED otherwise); a
  *               DID >= n_dialects gives zero magnitudes
- *   n           at least 0, below 2^28 (FB4_ERR_UNSUPPORTED beyond)
+ *   n           at least 0, at most 2^28 - 32 (FB4_ERR_UNSUPPORTED beyond)
  *   cols        a multiple of 32, below 2^25 (FB4_ERR_UNSUPPORTED otherwise); 0:
  *               the bias, or zeros
  *   block       32 or 16

@@ -71,7 +71,8 @@ int fb4_matvec(const fb4_luts* luts, const void* x, int64_t rows, int64_t x_row_
     if (!luts || rows < 0 || n < 0 || cols < 0 || x_row_stride < cols || out_row_stride < n || (block != 32 && block != 16) ||
         (out_dtype != FB4_DTYPE_BF16 && out_dtype != FB4_DTYPE_F32))
         return FB4_ERR_INVALID_ARG;
-    if (rows > kMatvecMaxRows || cols % 32 || n >= 1 << 28 || cols >= 1 << 25) return FB4_ERR_UNSUPPORTED;
+    if (rows > kMatvecMaxRows || cols % 32 || n > (1 << 28) - 32 || cols >= 1 << 25)   // (at most 16 threads to one of so many rows; 2^32 are no launch)
+        return FB4_ERR_UNSUPPORTED;
     if (rows == 0 || n == 0) return FB4_OK;
     if (!out || (cols > 0 && (!x || !codes || !meta))) return FB4_ERR_INVALID_ARG;
     if (!aligned(x, 16) || (rows > 1 && x_row_stride % 8) || x_row_stride / 8 > 0xFFFFFFFFll || !aligned(codes, 16) || !aligned(meta, block == 16 ? 4 : 2) ||

@@ -314,3 +314,14 @@ def test_parts_fit_their_workspace(shares):
         used = sum(t * shares[0].parts(n, share, rows) for t, n in zip(tiles, lens)) * heads_k
         assert used <= positions, (counts, lens, share)
     assert split > 300
+
+
+def test_products_of_too_many_threads_are_refused():
+    """Two tiles of sixteen rows of weights to a workgroup of 512: from 2^28 - 31 rows on a launch would have 2^32 threads."""
+    handle = ctypes.create_string_buffer(1 << 14)
+    call = lambda rows, n: B.lib().fb4_matvec(ctypes.addressof(handle), P(AL), rows, 1024, P(AL), P(AL), n, 1024, 32, None, P(AL + (1 << 45)), 0, n, None)
+    for rows in (1, 33, 64):
+        for n in (2 ** 28 - 31, 2 ** 28 - 1):
+            assert call(rows, n) == F.ERR_UNSUPPORTED, (rows, n)
+        if SERVED is not None:
+            assert call(rows, 2 ** 28 - 32) == SERVED
