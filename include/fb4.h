@@ -617,6 +617,8 @@ int fb4_block_attention(const void* q, const void* k, const void* v, const int64
  *   bias        device, float [n] or NULL
  *   out         device, bf16 or float (out_dtype) [rows][out_row_stride],
  *               aligned to its elements, on no memory of another argument
+ *               (FB4_ERR_INVALID_ARG otherwise); the stride of several rows at most 2^40
+ *               (FB4_ERR_UNSUPPORTED beyond)
  * A result's sums are formed in an order that depends on rows, n and cols (the
  * same call always gives the same results).
  */

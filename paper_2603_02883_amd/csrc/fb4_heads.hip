@@ -27,47 +27,6 @@ int strides_of(const int64_t* strides, T* out)
     return FB4_OK;
 }
 
-// A [batch][heads][tokens] tensor's rows: levels (count, stride in bytes) by falling strides, the row's bytes; whether they lie one
-// upon the other, as an output's.
-struct RowSet {
-    int64_t count[3], stride[3], row;
-    bool dense = true;
-    RowSet(const int64_t* strides, int64_t batch, int64_t heads, int64_t tokens, int64_t row_bytes) : count{batch, heads, tokens}, row(row_bytes)
-    {
-        int64_t next = row;
-        for (int i = 2; i >= 0; --i) {
-            stride[i] = count[i] > 1 ? strides[i] * 2 : 0;
-            dense = dense && (count[i] == 1 || stride[i] == next);
-            next *= count[i];
-        }
-        for (int i : {0, 1, 0}) {
-            if (stride[i] < stride[i + 1]) {
-                std::swap(stride[i], stride[i + 1]);
-                std::swap(count[i], count[i + 1]);
-            }
-        }
-    }
-};
-
-// Whether a row of the set at `base` has bytes of [from, to).
-bool meets(const RowSet& s, uintptr_t base, uintptr_t from, uintptr_t to, int level = 0)
-{
-    if (level == 3) return base < to && base + (uintptr_t)s.row > from;
-    uintptr_t extent = (uintptr_t)s.row;   // of one of this level's parts
-    for (int i = level + 1; i < 3; ++i) extent += (uintptr_t)(s.count[i] - 1) * (uintptr_t)s.stride[i];
-    const uintptr_t stride = (uintptr_t)s.stride[level];
-    if (stride == 0) return meets(s, base, from, to, level + 1);
-    if (base >= to) return false;
-    // the parts that begin before `to` and end behind `from`; one that begins inside has its first row there
-    const uintptr_t last = std::min<uintptr_t>((uintptr_t)s.count[level] - 1, (to - 1 - base) / stride);
-    if (base + last * stride >= from) return true;
-    const uintptr_t first = base + extent > from ? 0 : (from - base - extent) / stride + 1;
-    for (uintptr_t i = first; i <= last; ++i) {
-        if (meets(s, base + i * stride, from, to, level + 1)) return true;
-    }
-    return false;
-}
-
 // What the choice of blocks and the attention have in common.
 int check_blocks(int64_t batch, int heads, int heads_k, int64_t tokens_q, int64_t tokens_k, int64_t dim, int block_q, int block_k, BlockShape* s)
 {

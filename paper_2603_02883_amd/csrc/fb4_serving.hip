@@ -76,8 +76,19 @@ int fb4_matvec(const fb4_luts* luts, const void* x, int64_t rows, int64_t x_row_
     if (rows == 0 || n == 0) return FB4_OK;
     if (!out || (cols > 0 && (!x || !codes || !meta))) return FB4_ERR_INVALID_ARG;
     if (!aligned(x, 16) || (rows > 1 && x_row_stride % 8) || x_row_stride / 8 > 0xFFFFFFFFll || !aligned(codes, 16) || !aligned(meta, block == 16 ? 4 : 2) ||
-        !aligned(bias, 4) || !aligned(out, out_dtype == FB4_DTYPE_F32 ? 4 : 2))
+        !aligned(bias, 4) || !aligned(out, out_dtype == FB4_DTYPE_F32 ? 4 : 2) || (rows > 1 && out_row_stride > 1ll << 40))
         return FB4_ERR_UNSUPPORTED;
+    // Results on memory that other workgroups may still read (beside it, between its rows too, is none).
+    const int64_t halves = out_dtype == FB4_DTYPE_F32 ? 2 : 1, results_strides[3] = {0, 0, out_row_stride * halves};
+    const RowSet results(results_strides, 1, 1, rows, n * halves * 2);
+    if (touches(results, out, codes, (uint64_t)n * cols / 2) || touches(results, out, meta, (uint64_t)n * (cols / block) * 2) ||
+        touches(results, out, bias, (uint64_t)n * 4))
+        return FB4_ERR_INVALID_ARG;
+    if (touches(results, out, x, (uint64_t)(cols ? (rows > 1 ? (rows - 1) * x_row_stride : 0) + cols : 0) * 2)) {
+        for (int64_t r = 0; r < rows; ++r) {
+            if (touches(results, out, static_cast<const uint16_t*>(x) + r * x_row_stride, (uint64_t)cols * 2)) return FB4_ERR_INVALID_ARG;
+        }
+    }
     if (int rc = check_device(luts)) return rc;
     const int sets = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     const int64_t chunks = cols / 32;

@@ -1037,3 +1037,18 @@ def test_nothing_is_written_beside_what_starts_and_lengths_name(F, heads, heads_
                     counts = [b - a for a, b in zip(at, at[1:])]
                     got, got_lse = check_attention(F, c, q, counts, causal, first=at[0])
                     assert torch.equal(got, out) and torch.equal(got_lse, lse)
+
+
+def test_products_into_the_memory_beside_x(F, luts):
+    """Results between the rows of x in one buffer are served; on a row of x they are refused and nothing is written."""
+    g = gen(70)
+    codes, meta = weights(F, luts, g, 96, 256, 32)
+    held = randn(g, 9, 512).bfloat16()
+    x, want = held[:, :256], F.fb4_matvec(luts, held[:, :256], codes, meta)
+    kept = held.clone()
+    for first in (250, 0, 160):
+        with pytest.raises(F.Fb4Error) as e:
+            F.fb4_matvec(luts, x, codes, meta, out=held[:, first:first + 96])
+        assert e.value.code == F.ERR_INVALID_ARG and torch.equal(held, kept)
+    F.fb4_matvec(luts, x, codes, meta, out=held[:, 256:352])
+    assert torch.equal(held[:, 256:352], want) and torch.equal(x, kept[:, :256]) and torch.equal(held[:, 352:], kept[:, 352:])

@@ -325,3 +325,25 @@ def test_products_of_too_many_threads_are_refused():
             assert call(rows, n) == F.ERR_UNSUPPORTED, (rows, n)
         if SERVED is not None:
             assert call(rows, 2 ** 28 - 32) == SERVED
+
+
+def test_products_refuse_results_on_memory_that_is_read():
+    """Rows of x between the results' rows, and the other way round, are beside them; one shared byte is not."""
+    handle = ctypes.create_string_buffer(1 << 14)
+    gig = lambda i: P(AL + (i << 30))
+    call = lambda x=gig(0), sx=64, codes=gig(1), meta=gig(2), bias=gig(3), out=gig(4), so=48, rows=5, n=48, cols=64, dtype=0, block=32: B.lib().fb4_matvec(
+        ctypes.addressof(handle), x, rows, sx, codes, meta, n, cols, block, bias, out, dtype, so, None)
+    at = lambda i, b: P(AL + (i << 30) + b)
+    bad = [dict(out=gig(0)), dict(out=gig(1)), dict(out=gig(2)), dict(out=gig(3)), dict(out=at(0, 4 * 128 + 126)), dict(out=at(0, -4 * 96 - 2)), dict(out=at(1, 48 * 32 - 2)),
+           dict(out=at(2, 48 * 2 * 2 - 2)), dict(out=at(3, 48 * 4 - 2)), dict(out=at(3, -96 * 5 + 2)), dict(out=at(1, -100), so=200), dict(out=at(2, 48 * 4 * 2 - 4), dtype=1, block=16),
+           dict(out=at(0, -5 * 192 + 4), dtype=1), dict(sx=128, so=128, out=at(0, 126)), dict(sx=128, so=128, out=at(0, 128 + 34)), dict(sx=128, so=128, out=at(0, -94)),
+           dict(sx=128, so=64, dtype=1, n=32, out=at(0, 132)), dict(sx=64, so=1 << 20, out=at(0, 500)), dict(rows=1, sx=1 << 30, out=at(0, 126)), dict(sx=1 << 20, out=at(0, (4 << 21) + 64))]
+    good = [dict(), dict(out=at(0, 5 * 128)), dict(out=at(0, -5 * 96)), dict(out=at(1, 48 * 32)), dict(out=at(2, 48 * 4)), dict(out=at(3, 48 * 4)), dict(out=gig(3), bias=None),
+            dict(sx=128, so=128, out=at(0, 128)), dict(sx=128, so=128, out=at(0, -96)), dict(sx=128, so=128, out=at(0, 128 + 32)), dict(sx=128, so=64, dtype=1, n=32, out=at(0, 128)),
+            dict(rows=1, sx=1 << 30, out=at(0, 128)), dict(sx=1 << 20, out=at(0, 3 << 20)), dict(cols=0, sx=0, out=gig(0), codes=gig(0), meta=gig(0))]
+    for case in bad:
+        assert call(**case) == F.ERR_INVALID_ARG, case
+    assert call(so=(1 << 40) + 1) == F.ERR_UNSUPPORTED
+    if SERVED is not None:
+        for case in good:
+            assert call(**case) == SERVED, case
