@@ -683,8 +683,9 @@ int fb4_cache_plan(const int32_t* lens, const int32_t* adds, int64_t batch, int 
  * is forgotten.  Every element is rounded once, to nearest even; Inf and NaN are
  * stored as NaN and do not count for the scale.
  *   k, v        device, bf16 [heads_k][tokens][dim] by strides: the channels
- *               contiguous, rows 16-byte aligned (FB4_ERR_UNSUPPORTED otherwise), on no
- *               memory of cache or scales
+ *               contiguous, rows 16-byte aligned (FB4_ERR_UNSUPPORTED otherwise), like slots
+ *               on no memory of cache or scales, nor these on each other's
+ *               (FB4_ERR_INVALID_ARG otherwise)
  *   *_strides   host, (head, token) in elements, each a multiple of 8, at least
  *               0 and below 2^35 (FB4_ERR_UNSUPPORTED otherwise)
  *   dim         a multiple of 8, at most 128; heads_k 1..65535; at most

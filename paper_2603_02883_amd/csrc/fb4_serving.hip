@@ -164,6 +164,15 @@ int fb4_cache_store(const void* k, const int64_t* k_strides, const void* v, cons
     const int64_t span = std::max<int64_t>(1, std::min<int64_t>(page, tokens / 256));
     const int64_t groups = (tokens + span - 1) / span * heads_k * 2;
     if (groups > (1 << 24) - 1) return FB4_ERR_UNSUPPORTED;
+    // What other workgroups read, on memory that one writes.
+    const int64_t rows_k[3] = {0, k_strides[0], k_strides[1]}, rows_v[3] = {0, v_strides[0], v_strides[1]}, none[3] = {0, 0, 0};
+    const RowSet inputs[3] = {RowSet(rows_k, 1, heads_k, tokens, dim * 2), RowSet(rows_v, 1, heads_k, tokens, dim * 2), RowSet(none, 1, 1, 1, tokens * 4)};
+    const void* const at[3] = {k, v, slots};
+    const uint64_t held = (uint64_t)2 * pages * heads_k * page * dim, sizes = (uint64_t)2 * pages * heads_k;
+    for (int i = 0; i < 3; ++i) {
+        if (touches(inputs[i], at[i], cache, held) || touches(inputs[i], at[i], scales, sizes)) return FB4_ERR_INVALID_ARG;
+    }
+    if (touches(RowSet(none, 1, 1, 1, (int64_t)sizes), scales, cache, held)) return FB4_ERR_INVALID_ARG;
     const StoreShape s = {(uint32_t)tokens, (uint32_t)pages, (uint32_t)span, (uint16_t)heads_k, (uint8_t)bits, (uint8_t)(dim / 8)};
     launch(dim / 8 * page / 4 > kStoreThreads ? cache_store_kernel<2> : cache_store_kernel<1>, dim3((unsigned)groups), dim3(kStoreThreads), 0, static_cast<hipStream_t>(stream), static_cast<const uint16_t*>(k),
            static_cast<const uint16_t*>(v), slots, cache, scales, sk, sv, s);

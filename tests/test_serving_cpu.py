@@ -347,3 +347,21 @@ def test_products_refuse_results_on_memory_that_is_read():
     if SERVED is not None:
         for case in good:
             assert call(**case) == SERVED, case
+
+
+def test_stores_refuse_inputs_on_memory_that_is_written():
+    """[heads 2][tokens 5][64] rows, 4 pages of 16: a cache of 2 * 4 * 2 * 1024 bytes and 16 scales."""
+    at = lambda i, b=0: P(AL + (i << 30) + b)
+    n = 2 * 4 * 2 * 1024
+    base = dict(k=at(0), v=at(1), slots=at(2), cache=at(3), scales=at(4))
+    bad = [dict(k=at(3)), dict(v=at(3)), dict(slots=at(3)), dict(k=at(4, -16 + 16)), dict(v=at(4)), dict(slots=at(4, 12)), dict(scales=at(3)), dict(scales=at(3, n - 1)), dict(scales=at(3, -15)),
+           dict(k=at(3, n - 16)), dict(v=at(3, -4 * 256 - 2 * 64 - 112)), dict(slots=at(3, -16)), dict(slots=at(4, -4 * 5 + 4)), dict(k=at(3, -1024 * 64), sk=strides(1 << 19, 1 << 13)),
+           dict(v=at(4, -4 * 512), sv=strides(64, 256)), dict(scales=at(0, 191), sk=strides(0, 128 * 4), k=at(0, 64))]
+    good = [dict(), dict(k=at(3, n)), dict(k=at(3, -5 * 256)), dict(v=at(4, 16)), dict(slots=at(3, -20)), dict(slots=at(4, 16)), dict(scales=at(3, n)), dict(scales=at(3, -16)), dict(v=at(0)),
+            dict(scales=at(0, 256), sk=strides(64, 256)), dict(cache=at(0, 1 << 16), sk=strides(1 << 19, 64)),
+            dict(scales=at(0, 192), sk=strides(0, 128 * 4), k=at(0, 64))]   # (behind a row of 128 bytes)
+    for case in bad:
+        assert store(**{**base, **case}) == F.ERR_INVALID_ARG, case
+    if SERVED is not None:
+        for case in good:
+            assert store(**{**base, **case}) == SERVED, case
