@@ -75,7 +75,7 @@ int fb4_matvec(const fb4_luts* luts, const void* x, int64_t rows, int64_t x_row_
         return FB4_ERR_UNSUPPORTED;
     if (rows == 0 || n == 0) return FB4_OK;
     if (!out || (cols > 0 && (!x || !codes || !meta))) return FB4_ERR_INVALID_ARG;
-    if (!aligned(x, 16) || (rows > 1 && x_row_stride % 8) || x_row_stride / 8 > 0xFFFFFFFFll || !aligned(codes, 16) || !aligned(meta, block == 16 ? 4 : 2) ||
+    if (!aligned(x, 16) || (rows > 1 && cols > 0 && x_row_stride % 8) || (cols > 0 && x_row_stride / 8 > 0xFFFFFFFFll) || !aligned(codes, 16) || !aligned(meta, block == 16 ? 4 : 2) ||
         !aligned(bias, 4) || !aligned(out, out_dtype == FB4_DTYPE_F32 ? 4 : 2) || (rows > 1 && out_row_stride > 1ll << 40))
         return FB4_ERR_UNSUPPORTED;
     // Results on memory that other workgroups may still read (beside it, between its rows too, is none).

@@ -1052,3 +1052,12 @@ def test_products_into_the_memory_beside_x(F, luts):
         assert e.value.code == F.ERR_INVALID_ARG and torch.equal(held, kept)
     F.fb4_matvec(luts, x, codes, meta, out=held[:, 256:352])
     assert torch.equal(held[:, 256:352], want) and torch.equal(x, kept[:, :256]) and torch.equal(held[:, 352:], kept[:, 352:])
+
+
+def test_products_of_no_channels(F, luts):
+    """Of empty tensors as torch makes them: the bias, or zeros."""
+    none = lambda *shape, t=torch.bfloat16: torch.empty(*shape, 0, dtype=t, device="cuda")
+    bias = randn(gen(71), 33)
+    for rows in (1, 4, 64):
+        for b, want in ((bias, bias), (None, torch.zeros(33, device="cuda"))):
+            assert torch.equal(F.fb4_matvec(luts, none(rows), none(33, t=torch.uint8), none(33, t=torch.int16), bias=b, out_dtype=F.DTYPE_F32), want.expand(rows, 33))

@@ -365,3 +365,14 @@ def test_stores_refuse_inputs_on_memory_that_is_written():
     if SERVED is not None:
         for case in good:
             assert store(**{**base, **case}) == SERVED, case
+
+
+def test_products_of_no_channels_have_rows_without_a_place():
+    """An empty tensor's rows lie one element apart: of no channels no stride counts."""
+    x = torch.empty(4, 0, dtype=torch.bfloat16)
+    handle = ctypes.create_string_buffer(1 << 14)
+    call = lambda rows, stride: B.lib().fb4_matvec(ctypes.addressof(handle), None, rows, stride, None, None, 5, 0, 32, None, P(AL), 0, 5, None)
+    assert x.stride(0) % 8
+    if SERVED is not None:
+        assert call(4, x.stride(0)) == call(1, 0) == call(4, 0) == call(4, 2 ** 50 + 1) == SERVED
+    assert call(4, -1) == F.ERR_INVALID_ARG
