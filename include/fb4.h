@@ -733,7 +733,9 @@ int fb4_cache_store(const void* k, const int64_t* k_strides, const void* v, cons
  *               again when the call's work on the stream is done
  * A query without a key, infinite and NaN scores: as in fb4_block_attention.  A
  * value behind a query's last key never touches its result, NaN, Inf or not; one that it
- * sees makes its channel Inf or NaN then.  Rows of no sequence keep what
+ * sees makes its channel Inf or NaN then.  Weights are up to 2^8 before their sum divides
+ * them and sums are fp32, so values of about 2^120 over the number of keys and more may
+ * add up to Inf.  Rows of no sequence keep what
  * they held, in out and in lse.  A row's sums are formed in an order that depends on
  * the call's sizes and all sequences' lengths (the same call always gives the
  * same results); the launch does not depend on what lens, starts and tables hold, so a

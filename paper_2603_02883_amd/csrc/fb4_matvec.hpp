@@ -5,7 +5,8 @@
 // E4M3 bytes by a byte permutation of the dialect's eight magnitudes (LDS, 8 bytes a dialect), and the converter to bf16 takes the
 // block's scale along.  The channels of a product may come in any order as long as both operands have the same: a lane holds 32
 // successive channels of one row (16 bytes of codes, one block's scale and dialect, or two's), eight for each of four MFMAs, and of
-// eight the even ones come before the odd ones, as the nibbles' extraction leaves them.  Nothing is rounded but the result.
+// eight the even ones come before the odd ones, as the nibbles' extraction leaves them.  The weights are exact and so is every product; the sums are fp32,
+// and the result is rounded to its type once.
 //
 // What bounds it: the reads of the codes.  49152 x 8192, one row (227 MB): 52.6 us, 4.3 TB/s (46 where part of the weights is still in the last cache);
 // 16384 x 4096, 16 rows: 14.5, of which x through the L2s -- 16 rows are read by each of 256 workgroups -- and the first reads' latency are half; 6912 x
